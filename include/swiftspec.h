@@ -75,10 +75,13 @@ enum {
 #define SWIFTSPEC_DEVERR_BAD_TREE 1u     /* parent[0] != -1 or parent[i] outside [0, i) */
 #define SWIFTSPEC_DEVERR_BAD_PREFIX 2u   /* prefix length < 0 or prefix + T > S_max */
 #define SWIFTSPEC_DEVERR_BAD_ACCEPTED 4u /* accepted node outside [0, T) */
+#define SWIFTSPEC_DEVERR_BAD_GROUPS 8u   /* expert groups whose offsets, rows or positions are out of range */
 
 #define SWIFTSPEC_WS_HEADER_BYTES 65536u
 #define SWIFTSPEC_MAX_TREE 64 /* one 64-lane wavefront builds the ancestor masks */
-#define SWIFTSPEC_MAX_M 64    /* GEMM rows (tree tokens) per call */
+#define SWIFTSPEC_MAX_M 64    /* W4A16 GEMM rows (tree tokens) per call */
+#define SWIFTSPEC_MAX_EXPERTS 512
+#define SWIFTSPEC_MAX_TOPK 16 /* experts of a token */
 
 const char* swiftspec_status_string(int status);
 /* hipError_t of the last failing HIP call on this thread (0 if none). */
@@ -443,6 +446,118 @@ int swiftspec_greedy_accept(const uint16_t* logits, int32_t ldl, int32_t T, int3
                             const int32_t* d_tokens, const int32_t* d_parent, int32_t* d_argmax,
                             int32_t* d_accepted, int32_t* d_bonus, int32_t* d_path_len, void* ws,
                             size_t ws_bytes, void* stream);
+
+/* ------------------------------------------- microscaled 4-bit matrices
+ * MXFP4 matrices (OCP microscaling formats): each row is cut into blocks of
+ * 32 consecutive k; a block has 32 codes of one sign, two exponent and one
+ * mantissa bit (0, 0.5, 1, 1.5, 2, 3, 4, 6; bit 3 is the sign) and one scale
+ * byte s, standing for 2^(s - 127) (255: NaN).  E matrices of the same shape
+ * (the experts of a mixture; E = 1: one matrix) lie one after the other:
+ *   codes : [E][N][K/2] bytes, byte b of a row holds k = 2b (low nibble) and
+ *           k = 2b + 1 (high nibble);
+ *   scales: [E][N][K/32] bytes;
+ *   packed: kernel-native copy written once by swiftspec_mx4_prepack
+ *           (swiftspec_mx4_packed_bytes(K, N, E) bytes, 16-byte aligned, owned
+ *           by the caller), the only one that the products read.
+ * K % 32 == 0 (K is padded to whole groups of 128 in the packed copy),
+ * N % 16 == 0, 1 <= E <= SWIFTSPEC_MAX_EXPERTS, one matrix's packed copy below
+ * 4 GiB (UNSUPPORTED otherwise).
+ * Products take fp16 activations and quantise them by the same blocks first:
+ * both operands are in 4 bits, the sums in fp32. */
+typedef struct {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  int32_t K, N, E;
+  const void* packed;
+} swiftspec_mx4;
+
+size_t swiftspec_mx4_packed_bytes(int32_t K, int32_t N, int32_t E);
+int swiftspec_mx4_prepack(const swiftspec_mx4* W, void* packed, size_t packed_bytes, void* stream);
+
+/* Quantise M rows x [M][ldx] fp16 (16-byte aligned, ldx % 8 == 0) of K columns
+ * into codes [M][K/2] (4-byte aligned) and scales [M][K/32].  With a block's
+ * largest magnitude a: s - 127 = floor(log2 a) - 2, every value goes to the
+ * nearest code of v / 2^(s - 127), ties to the even code, saturating at 6;
+ * a = 0: s = 127.  A block that holds an infinity or a NaN gets s = 255 and
+ * codes 0: it stands for NaN. */
+int swiftspec_mx4_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx, uint8_t* codes, uint8_t* scales,
+                           void* stream);
+/* y [M][ldy] fp16 (16-byte aligned, ldy % 8 == 0): the values that codes and
+ * scales stand for, rounded to nearest even; above the fp16 range infinity. */
+int swiftspec_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int32_t K, uint16_t* y,
+                             int64_t ldy, void* stream);
+
+/* y[m][n] = fp16( sum_k Q(x)[m][k] * W'[n][k] + residual[m][n] ), Q(x) as
+ * swiftspec_mx4_quantize gives it, fp32 sums; W->E == 1.  Any M >= 0 (a draft
+ * tree, a prompt) with M rows of K/2 code bytes, K rounded up to 128, below
+ * 2 GiB (UNSUPPORTED otherwise).  residual may be NULL; it may alias y only if
+ * ldr == ldy; y may overlap x.  x [M][ldx]: 16-byte aligned, ldx % 8 == 0; y and
+ * residual 8-byte aligned, ldy and ldr multiples of 4.  A row that holds an
+ * infinity or a NaN comes out as NaN.  Workspace for these sizes:
+ * swiftspec_mx4_gemm_workspace_bytes (it serves fewer rows too). */
+int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int32_t ldx, uint16_t* y, int32_t ldy,
+                       const uint16_t* residual, int32_t ldr, void* ws, size_t ws_bytes, void* stream);
+size_t swiftspec_mx4_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N);
+
+/* ------------------------------------------------- mixture of experts
+ * The feed-forward block of a target model whose tokens each go through k of
+ * E experts: route, then swiglu and down over the groups that it made.  T
+ * tokens with k slots each make T k pairs, pair p = t k + j.  The groups are
+ * device arrays of the caller:
+ *   offsets [E + 1]: expert e owns the sorted places offsets[e] .. offsets[e+1];
+ *   rows [T k]     : the pair at each place; -1 past the last, offsets[E];
+ *   pos [T k]      : the place of each pair, -1 for a pair without an expert.
+ * Within an expert the pairs ascend.  T >= 0, 1 <= E <= SWIFTSPEC_MAX_EXPERTS,
+ * 1 <= k <= min(E, SWIFTSPEC_MAX_TOPK), T k < 2^28. */
+typedef struct {
+  int32_t T, k, E;
+  int32_t* offsets;
+  int32_t* rows;
+  int32_t* pos;
+} swiftspec_moe_groups;
+
+/* Router: for each of T rows of scores (logits [T][ldl] fp16, E columns) the k
+ * experts of largest score (equal scores: lower index first) into d_experts
+ * [T][k], and into d_weights [T][k] (float) their softmax probabilities over
+ * all E experts, computed in fp32; with renormalize != 0 divided by the sum of
+ * the k.  A score of -inf or NaN is masked: it has no probability and is never
+ * chosen; slots left without an expert (a token of padding) get expert -1,
+ * weight 0 and no place in a group.  +inf counts as 65504.  Then the groups, as
+ * swiftspec_moe_group makes them.  logits 2-byte aligned, ldl >= E. */
+int swiftspec_moe_route(const uint16_t* logits, int32_t ldl, int32_t renormalize, int32_t* d_experts,
+                        float* d_weights, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
+                        void* stream);
+/* The groups of experts that were chosen otherwise: d_experts [T][k]; an index
+ * outside [0, E) means no expert, one that a token names twice counts twice. */
+int swiftspec_moe_group(const int32_t* d_experts, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
+                        void* stream);
+size_t swiftspec_moe_route_workspace_bytes(int32_t T, int32_t E, int32_t k);
+
+/* First half of the experts' feed-forward block: for every place i of a group
+ * of expert e, with token t = rows[i] / k,
+ *   h[i][n] = fp16( silu(Q(x[t]) . Wg'[e][n]) * (Q(x[t]) . Wu'[e][n]) )
+ * (Q, sums and alignment as swiftspec_mx4_gemm; x [T][ldx], h [T k][ldh]; Wg and
+ * Wu share K, N and E = groups->E).  Rows of h past offsets[E] are left as they
+ * were.  h must not overlap x.  Offsets that do not ascend from 0 to at most T k
+ * set SWIFTSPEC_DEVERR_BAD_GROUPS and nothing is written; a row outside
+ * [0, T k) sets it and its row of h is not written. */
+int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, const uint16_t* x, int32_t ldx,
+                             const swiftspec_moe_groups* groups, uint16_t* h, int32_t ldh, void* ws, size_t ws_bytes,
+                             void* stream);
+size_t swiftspec_moe_mx4_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N);
+
+/* Second half: y[t][n] = fp16( residual[t][n] + sum_j d_weights[t][j] *
+ * (Q(h[pos[t k + j]]) . Wd'[e][n]) ) over the slots j with an expert, in slot
+ * order, each product rounded to fp32 only; every row of y is written (a token
+ * without experts gets its residual, or 0).  h [T k][ldh] as swiglu wrote it
+ * (all T k rows must be readable; those past offsets[E] do not enter), y and
+ * residual [T][ld*] as in swiftspec_mx4_gemm.  Invalid offsets set
+ * SWIFTSPEC_DEVERR_BAD_GROUPS and nothing is written; a place outside
+ * [0, offsets[E]) sets it and does not enter. */
+int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
+                           const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr,
+                           void* ws, size_t ws_bytes, void* stream);
+size_t swiftspec_moe_mx4_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N);
 
 /* -------------------------------------------------------- decoder layer */
 typedef struct {

@@ -25,10 +25,12 @@ i32, i64, f32, f64, vp, sz = (ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ct
                               ctypes.c_void_p, ctypes.c_size_t)
 
 OK, INVALID_ARG, UNSUPPORTED, MISALIGNED, WORKSPACE_TOO_SMALL, BAD_TREE, HIP_ERROR, CAPACITY = range(8)
-DEVERR_BAD_TREE, DEVERR_BAD_PREFIX, DEVERR_BAD_ACCEPTED = 1, 2, 4
+DEVERR_BAD_TREE, DEVERR_BAD_PREFIX, DEVERR_BAD_ACCEPTED, DEVERR_BAD_GROUPS = 1, 2, 4, 8
 WS_HEADER_BYTES = 65536
 MAX_TREE = 64
 MAX_M = 64
+MAX_EXPERTS = 512
+MAX_TOPK = 16
 
 
 class SwiftSpecError(RuntimeError):
@@ -42,6 +44,14 @@ class SwiftSpecError(RuntimeError):
 
 class W4(ctypes.Structure):
     _fields_ = [("qweight", vp), ("scales", vp), ("zeros", vp), ("K", i32), ("N", i32), ("packed", vp)]
+
+
+class MX4(ctypes.Structure):
+    _fields_ = [("codes", vp), ("scales", vp), ("K", i32), ("N", i32), ("E", i32), ("packed", vp)]
+
+
+class _Groups(ctypes.Structure):
+    _fields_ = [("T", i32), ("k", i32), ("E", i32), ("offsets", vp), ("rows", vp), ("pos", vp)]
 
 
 class Dims(ctypes.Structure):
@@ -115,6 +125,21 @@ _SIGS = {
     "swiftspec_verify_step_workspace_bytes": ([ctypes.POINTER(Dims), i32, i32], sz),
     "swiftspec_w4a16_gemm_valu": ([ctypes.POINTER(W4), vp, i32, i32, vp, i32, vp, i32, vp, sz, vp], ctypes.c_int),
     "swiftspec_w4a16_gemm_valu_workspace_bytes": ([i32, i32, i32], sz),
+    "swiftspec_mx4_packed_bytes": ([i32, i32, i32], sz),
+    "swiftspec_mx4_prepack": ([ctypes.POINTER(MX4), vp, sz, vp], ctypes.c_int),
+    "swiftspec_mx4_quantize": ([vp, i64, i32, i64, vp, vp, vp], ctypes.c_int),
+    "swiftspec_mx4_dequantize": ([vp, vp, i64, i32, vp, i64, vp], ctypes.c_int),
+    "swiftspec_mx4_gemm": ([ctypes.POINTER(MX4), vp, i32, i32, vp, i32, vp, i32, vp, sz, vp], ctypes.c_int),
+    "swiftspec_mx4_gemm_workspace_bytes": ([i32, i32, i32], sz),
+    "swiftspec_moe_route": ([vp, i32, i32, vp, vp, ctypes.POINTER(_Groups), vp, sz, vp], ctypes.c_int),
+    "swiftspec_moe_group": ([vp, ctypes.POINTER(_Groups), vp, sz, vp], ctypes.c_int),
+    "swiftspec_moe_route_workspace_bytes": ([i32, i32, i32], sz),
+    "swiftspec_moe_mx4_swiglu": ([ctypes.POINTER(MX4), ctypes.POINTER(MX4), vp, i32, ctypes.POINTER(_Groups), vp, i32,
+                                  vp, sz, vp], ctypes.c_int),
+    "swiftspec_moe_mx4_swiglu_workspace_bytes": ([i32, i32, i32, i32, i32], sz),
+    "swiftspec_moe_mx4_down": ([ctypes.POINTER(MX4), vp, i32, ctypes.POINTER(_Groups), vp, vp, i32, vp, i32, vp, sz,
+                                vp], ctypes.c_int),
+    "swiftspec_moe_mx4_down_workspace_bytes": ([i32, i32, i32, i32, i32], sz),
     "swiftspec_graph_begin": ([vp], ctypes.c_int),
     "swiftspec_graph_end": ([vp, ctypes.POINTER(vp)], ctypes.c_int),
     "swiftspec_graph_launch": ([vp, vp], ctypes.c_int),
@@ -527,6 +552,196 @@ class DraftTree:
                                                    self._p(out[3:4])), "draft_tree_reroot")
         return {"last": int(out[0]), "path_rows": int(out[1]), "keep": int(out[2]),
                 "pending": [int(x) for x in pend[:out[3]]]}
+
+
+# ------------------------- microscaled 4-bit matrices, mixture of experts
+
+def _rows(t, what, cols=None, dtype_bytes=2):
+    """(rows, columns, row stride) of a matrix whose rows are contiguous: the
+    library takes a pointer and a leading dimension, so a tensor that it would
+    read differently is refused here."""
+    if t.dim() != 2 or t.element_size() != dtype_bytes or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise SwiftSpecError(INVALID_ARG, what)
+    if cols is not None and t.shape[1] != cols:
+        raise SwiftSpecError(INVALID_ARG, what)
+    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _dense(t, what, shape, dtype_bytes):
+    if t is None or tuple(t.shape) != tuple(shape) or t.element_size() != dtype_bytes or not t.is_contiguous():
+        raise SwiftSpecError(INVALID_ARG, what)
+    return t
+
+
+class _On:
+    """The device of a call's tensors, current while the call is made (they
+    must all be on it), and the stream to enqueue on: the caller's, or that
+    device's current one."""
+
+    def __init__(self, where, stream, *tensors):
+        import torch
+        used = [t for t in tensors if t is not None]
+        self._dev = used[0].device
+        if any(t.device != self._dev for t in used) or self._dev.type != "cuda":
+            raise SwiftSpecError(INVALID_ARG, where)
+        self._guard = torch.cuda.device(self._dev)
+        self._stream = stream
+
+    def __enter__(self):
+        import torch
+        self._guard.__enter__()
+        s = self._stream if self._stream is not None else torch.cuda.current_stream(self._dev)
+        return ctypes.c_void_p(s.cuda_stream)
+
+    def __exit__(self, *a):
+        self._guard.__exit__(*a)
+
+
+def make_mx4(codes, scales, packed=None) -> MX4:
+    """Describe an MXFP4 matrix held in device tensors codes [N][K/2] u8 and
+    scales [N][K/32] u8, or E of them (codes [E][N][K/2], scales [E][N][K/32]),
+    and optionally its kernel-native copy `packed` (see prepack_mx4)."""
+    if codes.dim() not in (2, 3) or not codes.is_contiguous() or codes.element_size() != 1:
+        raise SwiftSpecError(INVALID_ARG, "make_mx4")
+    _dense(scales, "make_mx4", (*codes.shape[:-1], codes.shape[-1] // 16), 1)
+    E = codes.shape[0] if codes.dim() == 3 else 1
+    return MX4(codes.data_ptr(), scales.data_ptr(), 2 * codes.shape[-1], codes.shape[-2], E,
+               packed.data_ptr() if packed is not None else None)
+
+
+def mx4_packed_bytes(K: int, N: int, E: int = 1) -> int:
+    return int(_load().swiftspec_mx4_packed_bytes(K, N, E))
+
+
+def prepack_mx4(W: MX4, device="cuda", stream=None):
+    """Allocate and fill the kernel-native copy of W on `device` (the one that
+    holds its codes); returns the uint8 device tensor and sets W.packed to it
+    (keep the tensor alive)."""
+    import torch
+    t = torch.empty(mx4_packed_bytes(W.K, W.N, W.E), dtype=torch.uint8, device=device)
+    with _On("mx4_prepack", stream, t) as st:
+        _check(_load().swiftspec_mx4_prepack(ctypes.byref(W), _ptr(t), t.numel(), st), "mx4_prepack")
+    W.packed = t.data_ptr()
+    return t
+
+
+def mx4_quantize(x, codes, scales, stream=None):
+    """x [M][K] fp16 (rows contiguous) -> codes [M][K/2], scales [M][K/32] u8."""
+    M, K, ld = _rows(x, "mx4_quantize")
+    _dense(codes, "mx4_quantize", (M, K // 2), 1)
+    _dense(scales, "mx4_quantize", (M, K // 32), 1)
+    with _On("mx4_quantize", stream, x, codes, scales) as st:
+        _check(_load().swiftspec_mx4_quantize(_ptr(x), M, K, ld, _ptr(codes), _ptr(scales), st), "mx4_quantize")
+
+
+def mx4_dequantize(codes, scales, y, stream=None):
+    """codes [M][K/2], scales [M][K/32] u8 -> y [M][K] fp16 (rows contiguous)."""
+    M, K, ld = _rows(y, "mx4_dequantize")
+    _dense(codes, "mx4_dequantize", (M, K // 2), 1)
+    _dense(scales, "mx4_dequantize", (M, K // 32), 1)
+    with _On("mx4_dequantize", stream, codes, scales, y) as st:
+        _check(_load().swiftspec_mx4_dequantize(_ptr(codes), _ptr(scales), M, K, _ptr(y), ld, st), "mx4_dequantize")
+
+
+def mx4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
+    return int(_load().swiftspec_mx4_gemm_workspace_bytes(M, K, N))
+
+
+def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
+    """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
+    M, _, ldx = _rows(x, "mx4_gemm", W.K)
+    m, _, ldy = _rows(y, "mx4_gemm", W.N)
+    r, ldr = M, 0
+    if residual is not None:
+        r, _, ldr = _rows(residual, "mx4_gemm", W.N)
+    if m != M or r != M:
+        raise SwiftSpecError(INVALID_ARG, "mx4_gemm")
+    with _On("mx4_gemm", stream, x, y, ws, residual) as st:
+        _check(_load().swiftspec_mx4_gemm(ctypes.byref(W), _ptr(x), M, ldx, _ptr(y), ldy, _ptr(residual), ldr,
+                                          _ptr(ws), ws.numel() * ws.element_size(), st), "mx4_gemm")
+
+
+class MoeGroups:
+    """The groups of a mixture's (token, slot) pairs by expert: device int32
+    tensors offsets [E + 1], rows [T k] and pos [T k] (allocated if not given),
+    written by moe_route or moe_group and read by the experts' products."""
+
+    def __init__(self, T: int, k: int, E: int, offsets=None, rows=None, pos=None, device="cuda"):
+        import torch
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
+        self.T, self.k, self.E = T, k, E
+        self.offsets = _dense(new(E + 1) if offsets is None else offsets, "MoeGroups", (E + 1,), 4)
+        self.rows = _dense(new(T * k) if rows is None else rows, "MoeGroups", (T * k,), 4)
+        self.pos = _dense(new(T * k) if pos is None else pos, "MoeGroups", (T * k,), 4)
+        self._c = _Groups(T, k, E, self.offsets.data_ptr(), self.rows.data_ptr() or None, self.pos.data_ptr() or None)
+
+    def _ref(self):
+        return ctypes.byref(self._c)
+
+    def _tensors(self):
+        return self.offsets, self.rows, self.pos
+
+
+def moe_route_workspace_bytes(T: int, E: int, k: int) -> int:
+    return int(_load().swiftspec_moe_route_workspace_bytes(T, E, k))
+
+
+def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True, stream=None):
+    """logits [T][E] fp16 -> experts [T][k] int32 and weights [T][k] float32 of
+    the k largest scores of each token, and the groups."""
+    T, _, ldl = _rows(logits, "moe_route", groups.E)
+    if T != groups.T:
+        raise SwiftSpecError(INVALID_ARG, "moe_route")
+    _dense(experts, "moe_route", (T, groups.k), 4)
+    _dense(weights, "moe_route", (T, groups.k), 4)
+    with _On("moe_route", stream, logits, experts, weights, ws, *groups._tensors()) as st:
+        _check(_load().swiftspec_moe_route(_ptr(logits), ldl, int(bool(renormalize)), _ptr(experts), _ptr(weights),
+                                           groups._ref(), _ptr(ws), ws.numel() * ws.element_size(), st), "moe_route")
+
+
+def moe_group(experts, groups: MoeGroups, ws, stream=None):
+    """The groups of given experts [T][k] int32 (outside [0, E): none)."""
+    _dense(experts, "moe_group", (groups.T, groups.k), 4)
+    with _On("moe_group", stream, experts, ws, *groups._tensors()) as st:
+        _check(_load().swiftspec_moe_group(_ptr(experts), groups._ref(), _ptr(ws), ws.numel() * ws.element_size(), st),
+               "moe_group")
+
+
+def moe_mx4_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
+    return int(_load().swiftspec_moe_mx4_swiglu_workspace_bytes(T, k, E, K, N))
+
+
+def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
+    """x [T][K] fp16 -> h [T k][N] fp16, a row for each place of the groups."""
+    T, _, ldx = _rows(x, "moe_mx4_swiglu", Wg.K)
+    P, _, ldh = _rows(h, "moe_mx4_swiglu", Wg.N)
+    if T != groups.T or P != groups.T * groups.k:
+        raise SwiftSpecError(INVALID_ARG, "moe_mx4_swiglu")
+    with _On("moe_mx4_swiglu", stream, x, h, ws, *groups._tensors()) as st:
+        _check(_load().swiftspec_moe_mx4_swiglu(ctypes.byref(Wg), ctypes.byref(Wu), _ptr(x), ldx, groups._ref(),
+                                                _ptr(h), ldh, _ptr(ws), ws.numel() * ws.element_size(), st),
+               "moe_mx4_swiglu")
+
+
+def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
+    return int(_load().swiftspec_moe_mx4_down_workspace_bytes(T, k, E, K, N))
+
+
+def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, stream=None):
+    """h [T k][K] fp16 (as moe_mx4_swiglu wrote it), weights [T][k] float32 ->
+    y [T][N] fp16, the weighted sum of each token's experts plus residual."""
+    P, _, ldh = _rows(h, "moe_mx4_down", Wd.K)
+    T, _, ldy = _rows(y, "moe_mx4_down", Wd.N)
+    r, ldr = T, 0
+    if residual is not None:
+        r, _, ldr = _rows(residual, "moe_mx4_down", Wd.N)
+    if T != groups.T or r != T or P != T * groups.k:
+        raise SwiftSpecError(INVALID_ARG, "moe_mx4_down")
+    _dense(weights, "moe_mx4_down", (T, groups.k), 4)
+    with _On("moe_mx4_down", stream, h, weights, y, ws, residual, *groups._tensors()) as st:
+        _check(_load().swiftspec_moe_mx4_down(ctypes.byref(Wd), _ptr(h), ldh, groups._ref(), _ptr(weights), _ptr(y),
+                                              ldy, _ptr(residual), ldr, _ptr(ws), ws.numel() * ws.element_size(), st),
+               "moe_mx4_down")
 
 
 def make_dims(H, Hq, Hkv, D, F, S_max, eps=1e-5, rope_theta=500000.0) -> Dims:

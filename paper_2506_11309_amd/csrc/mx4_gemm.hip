@@ -1,0 +1,355 @@
+// Products with microscaled 4-bit matrices (MXFP4 x MXFP4, fp32 sums), for one
+// matrix or for the experts of a mixture with ragged groups of rows.
+//
+// y[m][n] = sum_k A[m][k] W[n][k]; both operands stay in 4 bits up to the
+// block-scaled matrix instruction v_mfma_scale_f32_16x16x128_f8f6f4, whose lane
+// kq*16 + i takes the 32 codes of row i in k block kq and that block's scale
+// byte.  The weights are its first operand, so that a lane ends up with four
+// consecutive columns of one output row.
+#include "ss_device.h"
+#include "ss_internal.h"
+
+namespace ss {
+
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr uint32_t kOutside = 0x80000000u;  // a buffer offset past every operand (they stay below 2 GiB or 4 GiB - 2 GiB)
+
+// c += W (16 columns x 128) . A (16 rows x 128); byte J of each scale word
+template <int J>
+__device__ __forceinline__ f32x4 mfma_mx4(const u32x4& w, uint32_t ws, const u32x4& a, uint32_t as, const f32x4& c) {
+  const i32x8 w8 = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+  const i32x8 a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, J, (int)ws, J, (int)as);
+}
+
+struct Mx4Args {
+  const uint8_t *w0, *w1;    // codes; the scales follow all codes
+  const uint8_t *s0, *s1;
+  int64_t w_stride, s_stride;  // bytes of one expert
+  int G, G4, Nt, N;
+  const uint8_t *a, *as;
+  uint32_t a_bytes, as_bytes;
+  int M, a_rows;
+  const int32_t* map;   // {expert, first row, rows, 0} per row block, or null
+  const int32_t* rows;
+  int div;
+  uint16_t* y;
+  int64_t ldy;
+  const uint16_t* res;
+  int64_t ldr;
+  float* part;
+  void* ws;
+  int col_blocks;
+};
+
+__device__ __forceinline__ float silu(float g) { return g / (1.f + __expf(-g)); }
+
+// the row block of a workgroup: expert, first output row, number of rows
+struct RowBlock {
+  int e, m0, n;
+};
+__device__ __forceinline__ RowBlock row_block(const Mx4Args& a, int rb, int TM) {
+  if (!a.map) return RowBlock{0, rb * TM, min(TM, a.M - rb * TM)};
+  const int32_t* p = a.map + 4 * ((int64_t)rb + 1);
+  return RowBlock{__builtin_amdgcn_readfirstlane(p[0]), __builtin_amdgcn_readfirstlane(p[1]),
+                  __builtin_amdgcn_readfirstlane(p[2])};
+}
+
+// activation row that output row m reads, or -1 where the caller's list is wrong
+__device__ __forceinline__ int source_row(const Mx4Args& a, int m) {
+  if (!a.rows) return m;
+  const int r = a.rows[m];
+  if (r < 0 || r >= a.M) {
+    report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+    return -1;
+  }
+  return r / a.div;
+}
+
+// ------------------------------------------------------------ few rows
+// W waves of a workgroup own NT column tiles (SwiGLU: NT/2 gate and NT/2 up
+// tiles) over all of K and split K between them; sums meet in LDS and are
+// added in wave order.  Nothing is staged: a weight block is one coalesced
+// kilobyte, read once from memory by the wave that multiplies it.
+template <int W, int MT, int NT, int U, Mx4Epilogue EPI>
+__global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
+  constexpr bool SW = EPI == MX4_SWIGLU;
+  constexpr int kC = SW ? NT / 2 : NT;
+  __shared__ f32x4 red[W][MT * NT][kWave];
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int rb = blockIdx.x / a.col_blocks, cb = blockIdx.x - rb * a.col_blocks;
+  const RowBlock b = row_block(a, rb, 16 * MT);
+  if (b.n <= 0) return;
+  const int t0 = cb * kC;
+  const int C = (a.G + U - 1) / U;  // chunks of U groups
+  const int c0 = wave * C / W, c1 = (wave + 1) * C / W;
+  const uint32_t wb = (uint32_t)a.w_stride, sb = (uint32_t)a.s_stride;
+  const auto rw0 = buffer_rsrc(a.w0 + b.e * a.w_stride, wb), rs0 = buffer_rsrc(a.s0 + b.e * a.s_stride, sb);
+  const auto rw1 = buffer_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
+  const auto rs1 = buffer_rsrc((SW ? a.s1 : a.s0) + b.e * a.s_stride, sb);
+  const auto ra = buffer_rsrc(a.a, a.a_bytes), ras = buffer_rsrc(a.as, a.as_bytes);
+  uint32_t va[MT], vs[MT];
+  bool live[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int m = 16 * mt + r16;
+    live[mt] = m < b.n;
+    const int src = live[mt] ? source_row(a, b.m0 + m) : -1;
+    live[mt] = src >= 0;
+    va[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)kq * 16u : kOutside;
+    vs[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
+  }
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Stage {
+    u32x4 w[U][NT], x[U][MT];
+    uint32_t ws[NT], xs[MT];
+  };
+  auto load = [&](Stage& s, int c) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      // tiles past the last repeat it (their sums are not written)
+      const uint32_t t = (uint32_t)min(t0 + nt % kC, a.Nt - 1);
+      const bool up = SW && nt >= kC;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t g = (uint32_t)(c * U + u);
+        s.w[u][nt] = buffer_load_x4(up ? rw1 : rw0, g < (uint32_t)a.G ? (uint32_t)lane * 16u : kOutside, (t * a.G + g) * 1024u);
+      }
+      s.ws[nt] = buffer_load_x1(up ? rs1 : rs0, (uint32_t)lane * 4u, (t * a.G4 + (uint32_t)(c * U / 4)) * 256u);
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t g = (uint32_t)(c * U + u);
+        s.x[u][mt] = buffer_load_x4(ra, g < (uint32_t)a.G ? va[mt] : kOutside, g * 64u);
+      }
+      s.xs[mt] = buffer_load_x1(ras, vs[mt], (uint32_t)(c * U / 4) * 16u);
+    }
+  };
+  auto multiply = [&](Stage& s, int c) {
+    const int sh = U == 4 ? 0 : 8 * ((c * U) & 3);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) s.ws[nt] >>= sh;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) s.xs[mt] >>= sh;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        acc[mt][nt] = mfma_mx4<0>(s.w[0][nt], s.ws[nt], s.x[0][mt], s.xs[mt], acc[mt][nt]);
+        if constexpr (U > 1) acc[mt][nt] = mfma_mx4<1>(s.w[1][nt], s.ws[nt], s.x[1][mt], s.xs[mt], acc[mt][nt]);
+        if constexpr (U > 2) acc[mt][nt] = mfma_mx4<2>(s.w[2][nt], s.ws[nt], s.x[2][mt], s.xs[mt], acc[mt][nt]);
+        if constexpr (U > 3) acc[mt][nt] = mfma_mx4<3>(s.w[3][nt], s.ws[nt], s.x[3][mt], s.xs[mt], acc[mt][nt]);
+      }
+  };
+  for (int c = c0; c < c1; ++c) {
+    Stage s;
+    load(s, c);
+    multiply(s, c);
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) red[wave][mt * NT + nt][lane] = acc[mt][nt];
+  __syncthreads();
+  auto total = [&](int f) {
+    f32x4 v = red[0][f][lane];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v += red[w][f][lane];
+    return v;
+  };
+  for (int f = wave; f < MT * kC; f += W) {
+    const int mt = f / kC, c = f - mt * kC;
+    const int t = t0 + c;
+    f32x4 v = total(mt * NT + c);
+    if constexpr (SW) {
+      const f32x4 u = total(mt * NT + kC + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = silu(v[i]) * u[i];
+    }
+    bool ok = t < a.Nt;
+#pragma unroll
+    for (int j = 0; j < MT; ++j) ok = ok && (j != mt || live[j]);
+    if (!ok) continue;
+    const int64_t m = b.m0 + 16 * mt + r16;
+    const int n = 16 * t + 4 * kq;
+    if constexpr (EPI == MX4_ROWS) {
+      *reinterpret_cast<f32x4*>(a.part + m * a.N + n) = v;
+    } else {
+      if constexpr (EPI == MX4_PLAIN)
+        if (a.res) {
+          const uint16_t* rp = a.res + m * a.ldr + n;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] += h2f(rp[i]);
+        }
+      uint16_t* yp = a.y + m * a.ldy + n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) yp[i] = f2h(v[i]);
+    }
+  }
+}
+
+// ------------------------------------------------------ blocks of rows
+// map[0] = {offsets are valid, rows of all experts}; map[1 + i] = {expert, first
+// row, rows} of the i-th block of TM rows, experts in order; the blocks past
+// the last have no rows.  Offsets that do not ascend from 0 to at most `most`
+// set the error word and leave every block empty.
+__global__ __launch_bounds__(1024) void mx4_map_kernel(const int32_t* __restrict__ offsets, int E, int most, int TM,
+                                                       int blocks, int32_t* __restrict__ map, void* ws) {
+  __shared__ int first[1025];  // blocks before expert e
+  __shared__ int wave_sum[16];
+  __shared__ int bad;
+  const int e = threadIdx.x, lane = lane_id(), wave = e >> 6;
+  if (e == 0) bad = 0;
+  __syncthreads();
+  int n = 0;
+  if (e < E) {
+    const int lo = offsets[e], hi = offsets[e + 1];
+    if (lo < 0 || hi < lo || hi > most || (e == 0 && lo != 0)) bad = 1;
+    else n = (hi - lo + TM - 1) / TM;
+  }
+  int s = n;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(s, d, kWave);
+    if (lane >= d) s += o;
+  }
+  if (lane == 63) wave_sum[wave] = s;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) s += wave_sum[w];
+  if (e < E) first[e + 1] = s;
+  if (e == 0) first[0] = 0;
+  __syncthreads();
+  if (e == 0) {
+    if (bad) report_error(ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+    map[0] = !bad;
+    map[1] = bad ? 0 : offsets[E];
+  }
+  const int used = bad ? 0 : first[E];
+  for (int i = e; i < blocks; i += 1024) {
+    int lo = 0, hi = E - 1;
+    if (i < used) {
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (first[mid] <= i) lo = mid;
+        else hi = mid - 1;
+      }
+      const int m0 = offsets[lo] + (i - first[lo]) * TM;
+      *reinterpret_cast<u32x4*>(map + 4 * ((int64_t)i + 1)) =
+          u32x4{(uint32_t)lo, (uint32_t)m0, (uint32_t)min(TM, offsets[lo + 1] - m0), 0u};
+    } else {
+      *reinterpret_cast<u32x4*>(map + 4 * ((int64_t)i + 1)) = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+}
+
+// ---------------------------------------------------------------- combine
+// One thread per 4 columns of a token; the addends in slot order.  Nothing is
+// written where the offsets were invalid (map[0]).
+__global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restrict__ part, int T, int k, int N,
+                                                          const int32_t* __restrict__ pos,
+                                                          const int32_t* __restrict__ map,
+                                                          const float* __restrict__ weights, uint16_t* y, int64_t ldy,
+                                                          const uint16_t* res, int64_t ldr, void* ws) {
+  const int per = N / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t t = i / per;
+  if (t >= T || !map[0]) return;
+  const int n = (int)(i - t * per) * 4;
+  const int used = map[1];
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (res) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = h2f(res[t * ldr + n + j]);
+  }
+  for (int j = 0; j < k; ++j) {
+    const int p = pos[t * k + j];
+    if (p < 0) continue;
+    if (p >= used) {
+      report_error(ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+      continue;
+    }
+    const float w = weights[t * k + j];
+    const f32x4 o = *reinterpret_cast<const f32x4*>(part + (int64_t)p * N + n);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(w, o[c], v[c]);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[t * ldy + n + j] = f2h(v[j]);
+}
+
+// the most row blocks of TM rows that M rows of E experts can make
+int row_blocks(int M, int E, int TM) { return (int)((int64_t)M / TM + (E < M ? E : M)); }
+
+template <int MT, Mx4Epilogue EPI>
+void launch_stream(Mx4Args a, int blocks, hipStream_t st) {
+  constexpr int NT = 2, kC = EPI == MX4_SWIGLU ? 1 : 2;
+  a.col_blocks = (a.Nt + kC - 1) / kC;
+  hipLaunchKernelGGL((mx4_stream_kernel<8, MT, NT, 2, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(512), 0, st, a);
+}
+
+template <Mx4Epilogue EPI>
+void launch_epi(const Mx4Launch& L, Mx4Args& a, hipStream_t st) {
+  const int TM = 64;
+  int blocks = (L.M + TM - 1) / TM;
+  if (L.offsets) {
+    blocks = row_blocks(L.M, L.E, TM);
+    hipLaunchKernelGGL(mx4_map_kernel, dim3(1), dim3(1024), 0, st, L.offsets, L.E, L.M, TM, blocks, L.map, L.ws);
+  }
+  launch_stream<4, EPI>(a, blocks, st);
+}
+
+}  // namespace
+
+size_t mx4_map_bytes(int M, int E) { return ((size_t)row_blocks(M, E, 16) + 1) * 16; }
+
+void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
+  Mx4Args a = {};
+  const size_t wq = mx4_code_bytes(L.N, L.K), wsb = mx4_scale_bytes(L.N, L.K);
+  a.w0 = static_cast<const uint8_t*>(L.w0);
+  a.s0 = a.w0 + L.E * wq;
+  a.w1 = static_cast<const uint8_t*>(L.w1);
+  a.s1 = a.w1 ? a.w1 + L.E * wq : nullptr;
+  a.w_stride = (int64_t)wq;
+  a.s_stride = (int64_t)wsb;
+  a.G = mx4_groups(L.K);
+  a.G4 = (a.G + 3) / 4;
+  a.N = L.N;
+  a.Nt = L.N / 16;
+  a.a = L.a;
+  a.as = L.a_scales;
+  a.a_bytes = (uint32_t)mx4_code_bytes(L.a_rows, L.K);
+  a.as_bytes = (uint32_t)mx4_scale_bytes(L.a_rows, L.K);
+  a.M = L.M;
+  a.map = L.offsets ? L.map : nullptr;
+  a.rows = L.rows;
+  a.div = L.div;
+  a.y = L.y;
+  a.ldy = L.ldy;
+  a.res = L.res;
+  a.ldr = L.ldr;
+  a.part = L.part;
+  a.ws = L.ws;
+  if (L.epi == MX4_SWIGLU) launch_epi<MX4_SWIGLU>(L, a, st);
+  else if (L.epi == MX4_ROWS) launch_epi<MX4_ROWS>(L, a, st);
+  else launch_epi<MX4_PLAIN>(L, a, st);
+}
+
+void launch_moe_combine(const float* part, int T, int k, int N, const int32_t* pos, const int32_t* map,
+                        const float* weights, uint16_t* y, int64_t ldy, const uint16_t* res, int64_t ldr, void* ws,
+                        hipStream_t st) {
+  hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)(((int64_t)T * (N / 4) + 255) / 256)), dim3(256), 0, st, part, T, k, N,
+                     pos, map, weights, y, ldy, res, ldr, ws);
+}
+
+}  // namespace ss

@@ -315,6 +315,73 @@ size_t layer_ws_query(const swiftspec_dims* d, int T) {
   return most;
 }
 
+// ---- microscaled 4-bit matrices
+int check_mx4_shape(const swiftspec_mx4* W) {
+  if (!W || W->K <= 0 || W->N <= 0 || W->E <= 0) return SWIFTSPEC_INVALID_ARG;
+  if (W->K % 32 || W->N % 16 || W->E > SWIFTSPEC_MAX_EXPERTS) return SWIFTSPEC_UNSUPPORTED;
+  // the kernels address one matrix through a 32-bit buffer range
+  if (ss::mx4_packed_bytes(W->K, W->N, 1) > 0xFFFFFFFFull) return SWIFTSPEC_UNSUPPORTED;
+  return SWIFTSPEC_OK;
+}
+
+int check_mx4(const swiftspec_mx4* W) {
+  int rc = check_mx4_shape(W);
+  if (rc) return rc;
+  if (!W->packed) return SWIFTSPEC_INVALID_ARG;
+  if (!aligned16(W->packed)) return SWIFTSPEC_MISALIGNED;
+  return SWIFTSPEC_OK;
+}
+
+inline bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// the quantised activations of a product lie in one 2 GiB buffer range
+bool mx4_rows_fit(int64_t M, int K) { return ss::mx4_code_bytes(M, K) < 0x80000000ull; }
+
+// Workspace of a product: the header, the activations in operand form, the map
+// of row blocks (experts), the experts' rows of the down product.
+struct Mx4Ws {
+  size_t codes, scales, map, part, total;
+};
+Mx4Ws mx4_ws(int64_t a_rows, int64_t M, int E, int K, int N, bool part) {
+  Mx4Ws w;
+  size_t off = kHeader;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += align_up(bytes);
+    return o;
+  };
+  w.codes = take(ss::mx4_code_bytes(a_rows, K));
+  w.scales = take(ss::mx4_scale_bytes(a_rows, K));
+  w.map = take(E ? ss::mx4_map_bytes((int)M, E) : 0);
+  w.part = take(part ? (size_t)M * N * sizeof(float) : 0);
+  w.total = off;
+  return w;
+}
+
+int check_groups(const swiftspec_moe_groups* g) {
+  if (!g || g->T < 0 || g->E < 1 || g->k < 1 || g->k > g->E) return SWIFTSPEC_INVALID_ARG;
+  if (g->E > SWIFTSPEC_MAX_EXPERTS || g->k > SWIFTSPEC_MAX_TOPK || (int64_t)g->T * g->k >= (1 << 28)) return SWIFTSPEC_UNSUPPORTED;
+  if (!g->offsets || (g->T > 0 && (!g->rows || !g->pos))) return SWIFTSPEC_INVALID_ARG;
+  if (!aligned4(g->offsets) || !aligned4(g->rows) || !aligned4(g->pos)) return SWIFTSPEC_MISALIGNED;
+  return SWIFTSPEC_OK;
+}
+
+int run_route(ss::RouteLaunch& L, const swiftspec_moe_groups* g, void* ws, size_t ws_bytes, hipStream_t st) {
+  if (!ws) return SWIFTSPEC_INVALID_ARG;
+  if (!aligned4(ws)) return SWIFTSPEC_MISALIGNED;
+  if (ws_bytes < kHeader + align_up(ss::route_hist_bytes(g->T, g->E, g->k))) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  L.T = g->T;
+  L.E = g->E;
+  L.k = g->k;
+  L.offsets = g->offsets;
+  L.rows = g->rows;
+  L.pos = g->pos;
+  L.hist = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kHeader);
+  ss::launch_moe_route(L, st);
+  return check_launch();
+}
+
 }  // namespace
 
 extern "C" {
@@ -493,6 +560,217 @@ int swiftspec_rmsnorm_w4a16_swiglu(const swiftspec_w4* Wg, const swiftspec_w4* W
   run_norm_gemm(Wg, Wu, NormIn{x, ldx, gamma, eps}, M, y, ldy, nullptr,
                 reinterpret_cast<uint16_t*>(base + kHeader),
                 reinterpret_cast<float*>(base + kHeader + align_up(p.prep_bytes)), S(stream));
+  return check_launch();
+}
+
+// ---- microscaled 4-bit matrices and mixtures of experts
+
+size_t swiftspec_mx4_packed_bytes(int32_t K, int32_t N, int32_t E) {
+  if (K <= 0 || N <= 0 || E <= 0) return 0;
+  return ss::mx4_packed_bytes(K, N, E);
+}
+
+int swiftspec_mx4_prepack(const swiftspec_mx4* W, void* packed, size_t packed_bytes, void* stream) {
+  int rc = check_mx4_shape(W);
+  if (rc) return rc;
+  if (!W->codes || !W->scales || !packed) return SWIFTSPEC_INVALID_ARG;
+  if (!aligned16(W->codes) || !aligned16(packed)) return SWIFTSPEC_MISALIGNED;
+  if (packed_bytes < ss::mx4_packed_bytes(W->K, W->N, W->E)) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  ss::launch_mx4_prepack(W->codes, W->scales, W->K, (int64_t)W->E * W->N, packed, S(stream));
+  return check_launch();
+}
+
+// rows of K columns: at most 2^40 values, so that the launch's block count fits
+static int check_mx4_rows(int64_t M, int32_t K, int64_t ld) {
+  if (M < 0 || K <= 0 || ld < K) return SWIFTSPEC_INVALID_ARG;
+  if (K % 32 || (M > 0 && M > ((int64_t)1 << 40) / K)) return SWIFTSPEC_UNSUPPORTED;
+  return SWIFTSPEC_OK;
+}
+
+int swiftspec_mx4_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx, uint8_t* codes, uint8_t* scales,
+                           void* stream) {
+  if (M && (!x || !codes || !scales)) return SWIFTSPEC_INVALID_ARG;
+  int rc = check_mx4_rows(M, K, ldx);
+  if (rc) return rc;
+  if (!aligned16(x) || ldx % 8 || !aligned4(codes)) return SWIFTSPEC_MISALIGNED;
+  if (M == 0) return SWIFTSPEC_OK;
+  ss::launch_mx4_quantize(x, M, K, ldx, codes, scales, S(stream));
+  return check_launch();
+}
+
+int swiftspec_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int32_t K, uint16_t* y,
+                             int64_t ldy, void* stream) {
+  if (M && (!codes || !scales || !y)) return SWIFTSPEC_INVALID_ARG;
+  int rc = check_mx4_rows(M, K, ldy);
+  if (rc) return rc;
+  if (!aligned16(y) || ldy % 8 || !aligned4(codes)) return SWIFTSPEC_MISALIGNED;
+  if (M == 0) return SWIFTSPEC_OK;
+  ss::launch_mx4_dequantize(codes, scales, M, K, y, ldy, S(stream));
+  return check_launch();
+}
+
+size_t swiftspec_mx4_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N) {
+  if (M < 1 || K < 1 || N < 1) return kHeader;
+  return mx4_ws(M, M, 0, K, N, false).total;
+}
+
+int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int32_t ldx, uint16_t* y, int32_t ldy,
+                       const uint16_t* residual, int32_t ldr, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_mx4(W);
+  if (rc) return rc;
+  if ((M && (!x || !y || !ws)) || W->E != 1) return SWIFTSPEC_INVALID_ARG;
+  if (M < 0 || ldx < W->K || ldy < W->N || (residual && ldr < W->N)) return SWIFTSPEC_INVALID_ARG;
+  if (!mx4_rows_fit(M, W->K)) return SWIFTSPEC_UNSUPPORTED;
+  if (!aligned16(x) || ldx % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
+  if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
+  if (M == 0) return SWIFTSPEC_OK;
+  if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
+  const Mx4Ws w = mx4_ws(M, M, 0, W->K, W->N, false);
+  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  hipStream_t st = S(stream);
+  ss::launch_mx4_prepare(x, M, W->K, ldx, base + w.codes, base + w.scales, st);
+  ss::Mx4Launch L = {};
+  L.epi = ss::MX4_PLAIN;
+  L.w0 = W->packed;
+  L.K = W->K;
+  L.N = W->N;
+  L.E = 1;
+  L.a = base + w.codes;
+  L.a_scales = base + w.scales;
+  L.a_rows = L.M = M;
+  L.div = 1;
+  L.y = y;
+  L.ldy = ldy;
+  L.res = residual;
+  L.ldr = ldr;
+  L.ws = ws;
+  ss::launch_mx4_gemm(L, st);
+  return check_launch();
+}
+
+size_t swiftspec_moe_route_workspace_bytes(int32_t T, int32_t E, int32_t k) {
+  if (T < 1 || E < 1 || k < 1 || k > SWIFTSPEC_MAX_TOPK) return kHeader;
+  return kHeader + align_up(ss::route_hist_bytes(T, E, k));
+}
+
+int swiftspec_moe_route(const uint16_t* logits, int32_t ldl, int32_t renormalize, int32_t* d_experts,
+                        float* d_weights, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
+                        void* stream) {
+  int rc = check_groups(groups);
+  if (rc) return rc;
+  if ((groups->T && (!logits || !d_experts || !d_weights)) || ldl < groups->E) return SWIFTSPEC_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(logits) & 1u) || !aligned4(d_experts) || !aligned4(d_weights)) return SWIFTSPEC_MISALIGNED;
+  ss::RouteLaunch L = {};
+  L.logits = logits;
+  L.ldl = ldl;
+  L.renormalize = renormalize;
+  L.experts = d_experts;
+  L.weights = d_weights;
+  return run_route(L, groups, ws, ws_bytes, S(stream));
+}
+
+int swiftspec_moe_group(const int32_t* d_experts, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
+                        void* stream) {
+  int rc = check_groups(groups);
+  if (rc) return rc;
+  if (groups->T && !d_experts) return SWIFTSPEC_INVALID_ARG;
+  if (!aligned4(d_experts)) return SWIFTSPEC_MISALIGNED;
+  ss::RouteLaunch L = {};
+  L.experts = const_cast<int32_t*>(d_experts);  // only read without scores
+  return run_route(L, groups, ws, ws_bytes, S(stream));
+}
+
+size_t swiftspec_moe_mx4_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
+  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1) return kHeader;
+  return mx4_ws(T, (int64_t)T * k, E, K, N, false).total;
+}
+
+int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, const uint16_t* x, int32_t ldx,
+                             const swiftspec_moe_groups* groups, uint16_t* h, int32_t ldh, void* ws, size_t ws_bytes,
+                             void* stream) {
+  int rc = check_mx4(Wg);
+  if (rc) return rc;
+  if ((rc = check_mx4(Wu))) return rc;
+  if ((rc = check_groups(groups))) return rc;
+  if (Wg->K != Wu->K || Wg->N != Wu->N || Wg->E != Wu->E || Wg->E != groups->E) return SWIFTSPEC_INVALID_ARG;
+  if ((groups->T && (!x || !h || !ws)) || ldx < Wg->K || ldh < Wg->N) return SWIFTSPEC_INVALID_ARG;
+  if (!mx4_rows_fit(groups->T, Wg->K)) return SWIFTSPEC_UNSUPPORTED;
+  if (!aligned16(x) || ldx % 8 || !aligned8(h) || ldh % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
+  if (groups->T == 0) return SWIFTSPEC_OK;
+  const int64_t pairs = (int64_t)groups->T * groups->k;
+  const Mx4Ws w = mx4_ws(groups->T, pairs, Wg->E, Wg->K, Wg->N, false);
+  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  hipStream_t st = S(stream);
+  ss::launch_mx4_prepare(x, groups->T, Wg->K, ldx, base + w.codes, base + w.scales, st);
+  ss::Mx4Launch L = {};
+  L.epi = ss::MX4_SWIGLU;
+  L.w0 = Wg->packed;
+  L.w1 = Wu->packed;
+  L.K = Wg->K;
+  L.N = Wg->N;
+  L.E = Wg->E;
+  L.a = base + w.codes;
+  L.a_scales = base + w.scales;
+  L.a_rows = groups->T;
+  L.M = (int)pairs;
+  L.offsets = groups->offsets;
+  L.rows = groups->rows;
+  L.div = groups->k;
+  L.map = reinterpret_cast<int32_t*>(base + w.map);
+  L.y = h;
+  L.ldy = ldh;
+  L.ws = ws;
+  ss::launch_mx4_gemm(L, st);
+  return check_launch();
+}
+
+size_t swiftspec_moe_mx4_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
+  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1) return kHeader;
+  const int64_t pairs = (int64_t)T * k;
+  return mx4_ws(pairs, pairs, E, K, N, true).total;
+}
+
+int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
+                           const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr,
+                           void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_mx4(Wd);
+  if (rc) return rc;
+  if ((rc = check_groups(groups))) return rc;
+  if (Wd->E != groups->E) return SWIFTSPEC_INVALID_ARG;
+  if (groups->T && (!h || !d_weights || !y || !ws)) return SWIFTSPEC_INVALID_ARG;
+  if (ldh < Wd->K || ldy < Wd->N || (residual && ldr < Wd->N)) return SWIFTSPEC_INVALID_ARG;
+  const int64_t pairs = (int64_t)groups->T * groups->k;
+  if (!mx4_rows_fit(pairs, Wd->K)) return SWIFTSPEC_UNSUPPORTED;
+  if (!aligned16(h) || ldh % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws) || !aligned4(d_weights)) return SWIFTSPEC_MISALIGNED;
+  if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
+  if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
+  if (groups->T == 0) return SWIFTSPEC_OK;
+  const Mx4Ws w = mx4_ws(pairs, pairs, Wd->E, Wd->K, Wd->N, true);
+  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  float* part = reinterpret_cast<float*>(base + w.part);
+  hipStream_t st = S(stream);
+  ss::launch_mx4_prepare(h, pairs, Wd->K, ldh, base + w.codes, base + w.scales, st);
+  ss::Mx4Launch L = {};
+  L.epi = ss::MX4_ROWS;
+  L.w0 = Wd->packed;
+  L.K = Wd->K;
+  L.N = Wd->N;
+  L.E = Wd->E;
+  L.a = base + w.codes;
+  L.a_scales = base + w.scales;
+  L.a_rows = pairs;
+  L.M = (int)pairs;
+  L.offsets = groups->offsets;
+  L.div = 1;
+  L.map = reinterpret_cast<int32_t*>(base + w.map);
+  L.part = part;
+  L.ws = ws;
+  ss::launch_mx4_gemm(L, st);
+  ss::launch_moe_combine(part, groups->T, groups->k, Wd->N, groups->pos, L.map, d_weights, y, ldy,
+                         residual, ldr, ws, st);
   return check_launch();
 }
 
