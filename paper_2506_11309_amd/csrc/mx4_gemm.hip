@@ -9,6 +9,8 @@
 #include "ss_device.h"
 #include "ss_internal.h"
 
+#include <type_traits>
+
 namespace ss {
 
 namespace {
@@ -67,6 +69,25 @@ __device__ __forceinline__ int source_row(const Mx4Args& a, int m) {
     return -1;
   }
   return r / a.div;
+}
+
+// four columns n .. n + 3 of output row m
+template <Mx4Epilogue EPI>
+__device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f32x4 v) {
+  if constexpr (EPI == MX4_ROWS) {
+    *reinterpret_cast<f32x4*>(a.part + m * a.N + n) = v;
+  } else {
+    if constexpr (EPI == MX4_PLAIN)
+      if (a.res) {
+        const u32x2 r = *reinterpret_cast<const u32x2*>(a.res + m * a.ldr + n);
+        v[0] += h2f((uint16_t)r[0]);
+        v[1] += h2f((uint16_t)(r[0] >> 16));
+        v[2] += h2f((uint16_t)r[1]);
+        v[3] += h2f((uint16_t)(r[1] >> 16));
+      }
+    *reinterpret_cast<u32x2*>(a.y + m * a.ldy + n) =
+        u32x2{f2h(v[0]) | (uint32_t)f2h(v[1]) << 16, f2h(v[2]) | (uint32_t)f2h(v[3]) << 16};
+  }
 }
 
 // ------------------------------------------------------------ few rows
@@ -181,20 +202,159 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) ok = ok && (j != mt || live[j]);
     if (!ok) continue;
-    const int64_t m = b.m0 + 16 * mt + r16;
-    const int n = 16 * t + 4 * kq;
-    if constexpr (EPI == MX4_ROWS) {
-      *reinterpret_cast<f32x4*>(a.part + m * a.N + n) = v;
-    } else {
-      if constexpr (EPI == MX4_PLAIN)
-        if (a.res) {
-          const uint16_t* rp = a.res + m * a.ldr + n;
+    write_out<EPI>(a, b.m0 + 16 * mt + r16, 16 * t + 4 * kq, v);
+  }
+}
+
+// ----------------------------------------------------------- many rows
+// 4 waves (WM x WN) own a tile of 16 WM MTW rows and 16 WN NTW columns; each
+// wave multiplies MTW x NTW blocks.  Both operands pass through LDS in the
+// instruction's own order (a block is 64 lanes x 16 bytes, so every access is
+// one 16-byte piece per lane without bank conflicts), loaded there directly:
+// slot g % 4 holds group g, loads run four groups ahead.  A step multiplies
+// group g out of registers while it reads group g + 1 from LDS, so neither
+// latency shows; one barrier a step.  Scale words cover four groups and are
+// loaded once per four steps.
+// The waits count this wave's loads in issue order: per step kL operand loads,
+// in the first of four steps kS scale loads before them.
+template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
+__global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
+  constexpr bool SW = EPI == MX4_SWIGLU;
+  constexpr int AT = WM * MTW, WT = WN * NTW, TM = 16 * AT;
+  constexpr int kA = AT / 4, kW = WT / 4, kL = kA + kW, kS = kA + kW;
+  constexpr int kC = SW ? WT / 2 : WT;   // output column tiles of the workgroup
+  constexpr int kCW = SW ? NTW / 2 : NTW;  // and of a wave
+  static_assert(WM * WN == 4 && AT % 4 == 0 && WT % 4 == 0, "four waves load alike");
+  __shared__ u32x4 op[4][AT + WT][kWave];
+  __shared__ uint32_t sc[2][AT + WT][kWave];
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave - wm * WN;
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int rb = blockIdx.x / a.col_blocks, cb = blockIdx.x - rb * a.col_blocks;
+  const RowBlock b = row_block(a, rb, TM);
+  if (b.n <= 0) return;
+  const int t0 = cb * kC;
+  const int G = a.G, G4 = a.G4;
+  const uint32_t wb = (uint32_t)a.w_stride, sb = (uint32_t)a.s_stride;
+  const i32x4 rw0 = raw_rsrc(a.w0 + b.e * a.w_stride, wb), rs0 = raw_rsrc(a.s0 + b.e * a.s_stride, sb);
+  const i32x4 rw1 = raw_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
+  const i32x4 rs1 = raw_rsrc((SW ? a.s1 : a.s0) + b.e * a.s_stride, sb);
+  const i32x4 ra = raw_rsrc(a.a, a.a_bytes), ras = raw_rsrc(a.as, a.as_bytes);
+  // this wave loads row blocks wave kA .. and weight tiles wave kW ..
+  uint32_t va[kA], vs[kA];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] += h2f(rp[i]);
-        }
-      uint16_t* yp = a.y + m * a.ldy + n;
+  for (int i = 0; i < kA; ++i) {
+    const int m = 16 * (wave * kA + i) + r16;
+    const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
+    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G * 64) + (uint32_t)kq * 16u : kOutside;
+    vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G4 * 16) + (uint32_t)kq * 4u : kOutside;
+  }
+  uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, its gate tiles, then its up tiles
 #pragma unroll
-      for (int i = 0; i < 4; ++i) yp[i] = f2h(v[i]);
+  for (int i = 0; i < kW; ++i) {
+    const int w = wave * kW + i, own = w / NTW, j = w - own * NTW;
+    wt[i] = (uint32_t)min(t0 + own * kCW + (SW ? j % kCW : j), a.Nt - 1);
+  }
+  auto is_up = [&](int i) { return SW && (wave * kW + i) % NTW >= kCW; };
+  const uint32_t op_lds = lds_address(&op[0][0][0]), sc_lds = lds_address(&sc[0][0][0]);
+  constexpr uint32_t kSlot = (AT + WT) * 1024, kScSlot = (AT + WT) * 256;
+  auto load_ops = [&](int g) {
+    const uint32_t to = op_lds + (uint32_t)(g & 3) * kSlot;
+    const bool in = g < G;
+#pragma unroll
+    for (int i = 0; i < kA; ++i)
+      buffer_load_lds16(ra, in ? va[i] : kOutside, (uint32_t)g * 64u, to + (uint32_t)(wave * kA + i) * 1024u);
+#pragma unroll
+    for (int i = 0; i < kW; ++i)
+      buffer_load_lds16(is_up(i) ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (wt[i] * G + g) * 1024u : 0u,
+                        to + (uint32_t)(AT + wave * kW + i) * 1024u);
+  };
+  auto load_scales = [&](int c) {
+    const uint32_t to = sc_lds + (uint32_t)(c & 1) * kScSlot;
+    const bool in = c < G4;
+#pragma unroll
+    for (int i = 0; i < kA; ++i)
+      buffer_load_lds4(ras, in ? vs[i] : kOutside, (uint32_t)c * 16u, to + (uint32_t)(wave * kA + i) * 256u);
+#pragma unroll
+    for (int i = 0; i < kW; ++i)
+      buffer_load_lds4(is_up(i) ? rs1 : rs0, in ? (uint32_t)lane * 4u : kOutside, in ? (wt[i] * G4 + c) * 256u : 0u,
+                       to + (uint32_t)(AT + wave * kW + i) * 256u);
+  };
+  struct Ops {
+    u32x4 x[MTW], w[NTW];
+  };
+  struct Scales {
+    uint32_t x[MTW], w[NTW];
+  };
+  auto read_scales = [&](Scales& s, int c) {
+#pragma unroll
+    for (int i = 0; i < MTW; ++i) s.x[i] = sc[c & 1][wm * MTW + i][lane];
+#pragma unroll
+    for (int i = 0; i < NTW; ++i) s.w[i] = sc[c & 1][AT + wn * NTW + i][lane];
+  };
+  f32x4 acc[MTW][NTW];
+#pragma unroll
+  for (int i = 0; i < MTW; ++i)
+#pragma unroll
+    for (int j = 0; j < NTW; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  load_scales(0);
+#pragma unroll
+  for (int g = 0; g < 4; ++g) load_ops(g);
+  vm_wait<3 * kL>();
+  lds_barrier();
+  Ops ops[2];
+  Scales s[2];
+  read_scales(s[0], 0);
+#pragma unroll
+  for (int i = 0; i < MTW; ++i) ops[0].x[i] = op[0][wm * MTW + i][lane];
+#pragma unroll
+  for (int j = 0; j < NTW; ++j) ops[0].w[j] = op[0][AT + wn * NTW + j][lane];
+  // group 4 c + J; P: register set of the scales
+  auto step = [&](auto jc, int c, Scales& now, Scales& next) {
+    constexpr int J = decltype(jc)::value;
+    const int g = 4 * c + J;
+    vm_wait<2 * kL + (J == 1 || J == 2 ? kS : 0)>();
+    lds_barrier();
+    if constexpr (J == 0) load_scales(c + 1);
+    load_ops(g + 4);
+    if constexpr (J == 3) read_scales(next, c + 1);
+    const Ops& o = ops[J & 1];
+    Ops& n = ops[(J & 1) ^ 1];
+#pragma unroll
+    for (int i = 0; i < MTW; ++i) n.x[i] = op[(J + 1) & 3][wm * MTW + i][lane];
+#pragma unroll
+    for (int j = 0; j < NTW; ++j) n.w[j] = op[(J + 1) & 3][AT + wn * NTW + j][lane];
+#pragma unroll
+    for (int j = 0; j < NTW; ++j)
+#pragma unroll
+      for (int i = 0; i < MTW; ++i) acc[i][j] = mfma_mx4<J>(o.w[j], now.w[j], o.x[i], now.x[i], acc[i][j]);
+  };
+  for (int c = 0; c < G4; c += 2) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (4 * (c + h) < G) step(std::integral_constant<int, 0>{}, c + h, s[h], s[h ^ 1]);
+      if (4 * (c + h) + 1 < G) step(std::integral_constant<int, 1>{}, c + h, s[h], s[h ^ 1]);
+      if (4 * (c + h) + 2 < G) step(std::integral_constant<int, 2>{}, c + h, s[h], s[h ^ 1]);
+      if (4 * (c + h) + 3 < G) step(std::integral_constant<int, 3>{}, c + h, s[h], s[h ^ 1]);
+    }
+  }
+  vm_wait<0>();  // loads past the last group still write LDS
+#pragma unroll
+  for (int i = 0; i < MTW; ++i) {
+    const int ml = 16 * (wm * MTW + i) + r16;
+    if (ml >= b.n || (a.rows && (uint32_t)a.rows[b.m0 + ml] >= (uint32_t)a.M)) continue;
+    const int64_t m = b.m0 + ml;
+#pragma unroll
+    for (int j = 0; j < kCW; ++j) {
+      const int t = t0 + wn * kCW + j;
+      if (t >= a.Nt) continue;
+      f32x4 v = acc[i][j];
+      if constexpr (SW) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = silu(v[q]) * acc[i][j + kCW][q];
+      }
+      write_out<EPI>(a, m, 16 * t + 4 * kq, v);
     }
   }
 }
@@ -298,15 +458,25 @@ void launch_stream(Mx4Args a, int blocks, hipStream_t st) {
   hipLaunchKernelGGL((mx4_stream_kernel<8, MT, NT, 2, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(512), 0, st, a);
 }
 
+template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
+void launch_tile(Mx4Args a, int blocks, hipStream_t st) {
+  constexpr int kC = EPI == MX4_SWIGLU ? WN * NTW / 2 : WN * NTW;
+  a.col_blocks = (a.Nt + kC - 1) / kC;
+  hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(256), 0, st, a);
+}
+
 template <Mx4Epilogue EPI>
 void launch_epi(const Mx4Launch& L, Mx4Args& a, hipStream_t st) {
-  const int TM = 64;
+  const int avg = L.offsets ? L.M / L.E : L.M;
+  const int TM = avg <= 64 ? 64 : avg <= 256 ? 128 : 256;
   int blocks = (L.M + TM - 1) / TM;
   if (L.offsets) {
     blocks = row_blocks(L.M, L.E, TM);
     hipLaunchKernelGGL(mx4_map_kernel, dim3(1), dim3(1024), 0, st, L.offsets, L.E, L.M, TM, blocks, L.map, L.ws);
   }
-  launch_stream<4, EPI>(a, blocks, st);
+  if (TM == 64) launch_stream<4, EPI>(a, blocks, st);
+  else if (TM == 128) launch_tile<2, 2, 4, 4, EPI>(a, blocks, st);
+  else launch_tile<2, 2, 8, 8, EPI>(a, blocks, st);
 }
 
 }  // namespace

@@ -137,6 +137,16 @@ __device__ __forceinline__ void buffer_load_lds16(i32x4 rsrc, uint32_t voff, uin
       : "v"(voff), "s"(rsrc), "s"(soff), "s"(lds_addr)
       : "memory");
 }
+// the same with 4 bytes a lane, landing at lds_addr + 4 l
+__device__ __forceinline__ void buffer_load_lds4(i32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds_addr) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\t"
+      "buffer_load_dword %1, %2, %3 offen lds\n\ts_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(voff), "s"(rsrc), "s"(soff), "s"(lds_addr)
+      : "memory");
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
