@@ -72,22 +72,22 @@ __device__ __forceinline__ int source_row(const Mx4Args& a, int m) {
 }
 
 // four columns n .. n + 3 of output row m
+__device__ __forceinline__ u32x2 residual(const Mx4Args& a, int64_t m, int n) {
+  return *reinterpret_cast<const u32x2*>(a.res + m * a.ldr + n);
+}
+__device__ __forceinline__ void add_residual(f32x4& v, u32x2 r) {
+  v[0] += h2f((uint16_t)r[0]);
+  v[1] += h2f((uint16_t)(r[0] >> 16));
+  v[2] += h2f((uint16_t)r[1]);
+  v[3] += h2f((uint16_t)(r[1] >> 16));
+}
 template <Mx4Epilogue EPI>
 __device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f32x4 v) {
-  if constexpr (EPI == MX4_ROWS) {
+  if constexpr (EPI == MX4_ROWS)
     *reinterpret_cast<f32x4*>(a.part + m * a.N + n) = v;
-  } else {
-    if constexpr (EPI == MX4_PLAIN)
-      if (a.res) {
-        const u32x2 r = *reinterpret_cast<const u32x2*>(a.res + m * a.ldr + n);
-        v[0] += h2f((uint16_t)r[0]);
-        v[1] += h2f((uint16_t)(r[0] >> 16));
-        v[2] += h2f((uint16_t)r[1]);
-        v[3] += h2f((uint16_t)(r[1] >> 16));
-      }
+  else
     *reinterpret_cast<u32x2*>(a.y + m * a.ldy + n) =
         u32x2{f2h(v[0]) | (uint32_t)f2h(v[1]) << 16, f2h(v[2]) | (uint32_t)f2h(v[3]) << 16};
-  }
 }
 
 // ------------------------------------------------------------ few rows
@@ -202,7 +202,10 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) ok = ok && (j != mt || live[j]);
     if (!ok) continue;
-    write_out<EPI>(a, b.m0 + 16 * mt + r16, 16 * t + 4 * kq, v);
+    const int64_t m = b.m0 + 16 * mt + r16;
+    if constexpr (EPI == MX4_PLAIN)
+      if (a.res) add_residual(v, residual(a, m, 16 * t + 4 * kq));
+    write_out<EPI>(a, m, 16 * t + 4 * kq, v);
   }
 }
 
@@ -259,27 +262,24 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   auto is_up = [&](int i) { return SW && (wave * kW + i) % NTW >= kCW; };
   const uint32_t op_lds = lds_address(&op[0][0][0]), sc_lds = lds_address(&sc[0][0][0]);
   constexpr uint32_t kSlot = (AT + WT) * 1024, kScSlot = (AT + WT) * 256;
-  auto load_ops = [&](int g) {
+  // operand load i of group g, scale load i of groups 4 c .. 4 c + 3
+  auto load_op = [&](int i, int g) {
     const uint32_t to = op_lds + (uint32_t)(g & 3) * kSlot;
     const bool in = g < G;
-#pragma unroll
-    for (int i = 0; i < kA; ++i)
+    if (i < kA)
       buffer_load_lds16(ra, in ? va[i] : kOutside, (uint32_t)g * 64u, to + (uint32_t)(wave * kA + i) * 1024u);
-#pragma unroll
-    for (int i = 0; i < kW; ++i)
-      buffer_load_lds16(is_up(i) ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (wt[i] * G + g) * 1024u : 0u,
-                        to + (uint32_t)(AT + wave * kW + i) * 1024u);
+    else
+      buffer_load_lds16(is_up(i - kA) ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (wt[i - kA] * G + g) * 1024u : 0u,
+                        to + (uint32_t)(AT + wave * kW + i - kA) * 1024u);
   };
-  auto load_scales = [&](int c) {
+  auto load_scale = [&](int i, int c) {
     const uint32_t to = sc_lds + (uint32_t)(c & 1) * kScSlot;
     const bool in = c < G4;
-#pragma unroll
-    for (int i = 0; i < kA; ++i)
+    if (i < kA)
       buffer_load_lds4(ras, in ? vs[i] : kOutside, (uint32_t)c * 16u, to + (uint32_t)(wave * kA + i) * 256u);
-#pragma unroll
-    for (int i = 0; i < kW; ++i)
-      buffer_load_lds4(is_up(i) ? rs1 : rs0, in ? (uint32_t)lane * 4u : kOutside, in ? (wt[i] * G4 + c) * 256u : 0u,
-                       to + (uint32_t)(AT + wave * kW + i) * 256u);
+    else
+      buffer_load_lds4(is_up(i - kA) ? rs1 : rs0, in ? (uint32_t)lane * 4u : kOutside, in ? (wt[i - kA] * G4 + c) * 256u : 0u,
+                       to + (uint32_t)(AT + wave * kW + i - kA) * 256u);
   };
   struct Ops {
     u32x4 x[MTW], w[NTW];
@@ -287,48 +287,60 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   struct Scales {
     uint32_t x[MTW], w[NTW];
   };
-  auto read_scales = [&](Scales& s, int c) {
-#pragma unroll
-    for (int i = 0; i < MTW; ++i) s.x[i] = sc[c & 1][wm * MTW + i][lane];
-#pragma unroll
-    for (int i = 0; i < NTW; ++i) s.w[i] = sc[c & 1][AT + wn * NTW + i][lane];
+  constexpr int kR = MTW + NTW;  // blocks that a wave reads
+  auto read_op = [&](Ops& o, int i, int slot) {
+    if (i < MTW) o.x[i] = op[slot][wm * MTW + i][lane];
+    else o.w[i - MTW] = op[slot][AT + wn * NTW + i - MTW][lane];
+  };
+  auto read_scale = [&](Scales& s, int i, int c) {
+    if (i < MTW) s.x[i] = sc[c & 1][wm * MTW + i][lane];
+    else s.w[i - MTW] = sc[c & 1][AT + wn * NTW + i - MTW][lane];
   };
   f32x4 acc[MTW][NTW];
 #pragma unroll
   for (int i = 0; i < MTW; ++i)
 #pragma unroll
     for (int j = 0; j < NTW; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  load_scales(0);
 #pragma unroll
-  for (int g = 0; g < 4; ++g) load_ops(g);
-  vm_wait<3 * kL>();
-  lds_barrier();
+  for (int i = 0; i < kS; ++i) load_scale(i, 0);
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+#pragma unroll
+    for (int i = 0; i < kL; ++i) load_op(i, g);
+  vm_lds_barrier<3 * kL>();
   Ops ops[2];
   Scales s[2];
-  read_scales(s[0], 0);
 #pragma unroll
-  for (int i = 0; i < MTW; ++i) ops[0].x[i] = op[0][wm * MTW + i][lane];
-#pragma unroll
-  for (int j = 0; j < NTW; ++j) ops[0].w[j] = op[0][AT + wn * NTW + j][lane];
-  // group 4 c + J; P: register set of the scales
+  for (int i = 0; i < kR; ++i) {
+    read_scale(s[0], i, 0);
+    read_op(ops[0], i, 0);
+  }
+  // Group 4 c + J.  The loads and LDS reads stand between the matrix
+  // instructions, a few to each, where their issue costs nothing.
   auto step = [&](auto jc, int c, Scales& now, Scales& next) {
     constexpr int J = decltype(jc)::value;
+    constexpr int kScale = J == 0 ? kS : 0, kNext = J == 3 ? kR : 0;
+    constexpr int kMfma = MTW * NTW, kAux = kScale + kNext + kR + kL, kPer = (kAux + kMfma - 1) / kMfma;
     const int g = 4 * c + J;
-    vm_wait<2 * kL + (J == 1 || J == 2 ? kS : 0)>();
-    lds_barrier();
-    if constexpr (J == 0) load_scales(c + 1);
-    load_ops(g + 4);
-    if constexpr (J == 3) read_scales(next, c + 1);
+    vm_lds_barrier<2 * kL + (J == 1 || J == 2 ? kS : 0)>();
     const Ops& o = ops[J & 1];
     Ops& n = ops[(J & 1) ^ 1];
+    auto aux = [&](int q) {
+      if (q < kScale) load_scale(q, c + 1);
+      else if (q < kScale + kNext) read_scale(next, q - kScale, c + 1);
+      else if (q < kScale + kNext + kR) read_op(n, q - kScale - kNext, (J + 1) & 3);
+      else if (q < kAux) load_op(q - kScale - kNext - kR, g + 4);
+    };
 #pragma unroll
-    for (int i = 0; i < MTW; ++i) n.x[i] = op[(J + 1) & 3][wm * MTW + i][lane];
+    for (int k = 0; k < kMfma; ++k) {
+      const int j = k / MTW, i = k - j * MTW;
+      acc[i][j] = mfma_mx4<J>(o.w[j], now.w[j], o.x[i], now.x[i], acc[i][j]);
+      if (k * kPer < kAux) {
 #pragma unroll
-    for (int j = 0; j < NTW; ++j) n.w[j] = op[(J + 1) & 3][AT + wn * NTW + j][lane];
-#pragma unroll
-    for (int j = 0; j < NTW; ++j)
-#pragma unroll
-      for (int i = 0; i < MTW; ++i) acc[i][j] = mfma_mx4<J>(o.w[j], now.w[j], o.x[i], now.x[i], acc[i][j]);
+        for (int q = 0; q < kPer; ++q) aux(k * kPer + q);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   };
   for (int c = 0; c < G4; c += 2) {
 #pragma unroll
@@ -345,6 +357,12 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     const int ml = 16 * (wm * MTW + i) + r16;
     if (ml >= b.n || (a.rows && (uint32_t)a.rows[b.m0 + ml] >= (uint32_t)a.M)) continue;
     const int64_t m = b.m0 + ml;
+    u32x2 r[kCW] = {};
+    if constexpr (EPI == MX4_PLAIN)
+      if (a.res) {
+#pragma unroll
+        for (int j = 0; j < kCW; ++j) r[j] = residual(a, m, 16 * min(t0 + wn * kCW + j, a.Nt - 1) + 4 * kq);
+      }
 #pragma unroll
     for (int j = 0; j < kCW; ++j) {
       const int t = t0 + wn * kCW + j;
@@ -354,6 +372,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = silu(v[q]) * acc[i][j + kCW][q];
       }
+      if constexpr (EPI == MX4_PLAIN) add_residual(v, r[j]);
       write_out<EPI>(a, m, 16 * t + 4 * kq, v);
     }
   }

@@ -159,6 +159,18 @@ __device__ __forceinline__ void vm_wait() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
 
+// Workgroup barrier after this wave's LDS traffic and all but N of its vector-
+// memory operations.  The compiler sees the wait, so that values read from LDS
+// before it need no other.
+template <int N>
+__device__ __forceinline__ void vm_lds_barrier() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (0x7 << 4));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 }  // namespace ss
 
 namespace ss {
