@@ -16,6 +16,7 @@ namespace ss {
 namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kOutside = 0x80000000u;  // a buffer offset past every operand (they stay below 2 GiB or 4 GiB - 2 GiB)
 
@@ -25,6 +26,14 @@ __device__ __forceinline__ f32x4 mfma_mx4(const u32x4& w, uint32_t ws, const u32
   const i32x8 w8 = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
   const i32x8 a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, J, (int)ws, J, (int)as);
+}
+
+// c += W (32 columns x 64) . A (32 rows x 64): lane h*32 + i holds block h of row i
+template <int J>
+__device__ __forceinline__ f32x16 mfma_mx4_32(const u32x4& w, uint32_t ws, const u32x4& a, uint32_t as, const f32x16& c) {
+  const i32x8 w8 = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+  const i32x8 a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w8, a8, c, 4, 4, J, (int)ws, J, (int)as);
 }
 
 struct Mx4Args {
@@ -60,6 +69,21 @@ __device__ __forceinline__ RowBlock row_block(const Mx4Args& a, int rb, int TM) 
                   __builtin_amdgcn_readfirstlane(p[2])};
 }
 
+// Workgroup -> row and column block of a tile.  Tiles are taken in bands of 4 row
+// blocks, column by column, and stretches of 32 of them (what a chiplet's
+// compute units run at one time) go to the 8 chiplets in turn, as workgroups do:
+// what a chiplet reads is then a few row blocks and 8 column blocks, out of its
+// own L2, and the empty row blocks at the end of a list of experts (they come
+// last) are no chiplet's alone.
+__device__ __forceinline__ void place_of(const Mx4Args& a, int& rb, int& cb) {
+  const int all = gridDim.x, x = blockIdx.x & 7, s = blockIdx.x >> 3;
+  const int id = (int)blockIdx.x < (all & ~255) ? (((s >> 5) << 3) + x) * 32 + (s & 31) : (int)blockIdx.x;
+  const int band = id / (4 * a.col_blocks), in = id - band * 4 * a.col_blocks;
+  const int high = min(4, all / a.col_blocks - 4 * band);
+  rb = 4 * band + in % high;
+  cb = in / high;
+}
+
 // activation row that output row m reads, or -1 where the caller's list is wrong
 __device__ __forceinline__ int source_row(const Mx4Args& a, int m) {
   if (!a.rows) return m;
@@ -81,13 +105,22 @@ __device__ __forceinline__ void add_residual(f32x4& v, u32x2 r) {
   v[2] += h2f((uint16_t)r[1]);
   v[3] += h2f((uint16_t)(r[1] >> 16));
 }
+__device__ __forceinline__ u32x2 pack4(const f32x4& v) {
+  return u32x2{f2h(v[0]) | (uint32_t)f2h(v[1]) << 16, f2h(v[2]) | (uint32_t)f2h(v[3]) << 16};
+}
+// 16 bytes to an address of 8-byte alignment
+__device__ __forceinline__ void store_rows16(uint16_t* p, const u32x4& v) {
+  struct __attribute__((packed, aligned(8))) Line {
+    u32x4 v;
+  };
+  reinterpret_cast<Line*>(p)->v = v;
+}
 template <Mx4Epilogue EPI>
 __device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f32x4 v) {
   if constexpr (EPI == MX4_ROWS)
     *reinterpret_cast<f32x4*>(a.part + m * a.N + n) = v;
   else
-    *reinterpret_cast<u32x2*>(a.y + m * a.ldy + n) =
-        u32x2{f2h(v[0]) | (uint32_t)f2h(v[1]) << 16, f2h(v[2]) | (uint32_t)f2h(v[3]) << 16};
+    *reinterpret_cast<u32x2*>(a.y + m * a.ldy + n) = pack4(v);
 }
 
 // ------------------------------------------------------------ few rows
@@ -203,38 +236,46 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
     for (int j = 0; j < MT; ++j) ok = ok && (j != mt || live[j]);
     if (!ok) continue;
     const int64_t m = b.m0 + 16 * mt + r16;
-    if constexpr (EPI == MX4_PLAIN)
-      if (a.res) add_residual(v, residual(a, m, 16 * t + 4 * kq));
+    if constexpr (EPI == MX4_RESIDUAL) add_residual(v, residual(a, m, 16 * t + 4 * kq));
     write_out<EPI>(a, m, 16 * t + 4 * kq, v);
   }
 }
 
 // ----------------------------------------------------------- many rows
 // 4 waves (WM x WN) own a tile of 16 WM MTW rows and 16 WN NTW columns; each
-// wave multiplies MTW x NTW blocks.  Both operands pass through LDS in the
-// instruction's own order (a block is 64 lanes x 16 bytes, so every access is
-// one 16-byte piece per lane without bank conflicts), loaded there directly:
-// slot g % 4 holds group g, loads run four groups ahead.  A step multiplies
-// group g out of registers while it reads group g + 1 from LDS, so neither
-// latency shows; one barrier a step.  Scale words cover four groups and are
-// loaded once per four steps.
-// The waits count this wave's loads in issue order: per step kL operand loads,
-// in the first of four steps kS scale loads before them.
+// wave multiplies MTW x NTW blocks of 16, two by two through the 32 x 32 x 64
+// form of the instruction (one wave a SIMD issues it at 9.0 PFLOP/s, the
+// 16 x 16 x 128 form at 5.1).  Both operands pass through LDS, loaded there
+// directly: the weights group by group as they are packed, four groups ahead;
+// the activations two groups at a time, so that a row's piece is a whole
+// 128-byte line however the rows are gathered.  The 16-byte pieces of a line
+// stand in LDS at piece ^ (row % 8), so that a column of rows has no bank
+// conflicts.  A step multiplies group g out of registers while it reads group
+// g + 1 from LDS, so neither latency shows; one barrier a step.  Scale words
+// cover four groups: they are loaded in the first of four steps, when every
+// wave has the present ones in registers, and read in the last.
+// The waits count this wave's loads in issue order.  Step g loads, in order,
+// the scales of the next four groups (g % 4 == 0), the activations of groups
+// g + 3 and g + 4 (g odd), the weights of group g + 4.
+constexpr int kTurnRow = 144;  // bytes of a 128-byte line with its padding
+
 template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
 __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   constexpr bool SW = EPI == MX4_SWIGLU;
   constexpr int AT = WM * MTW, WT = WN * NTW, TM = 16 * AT;
-  constexpr int kA = AT / 4, kW = WT / 4, kL = kA + kW, kS = kA + kW;
+  constexpr int kA = 2 * AT / 4, kW = WT / 4, kS = (AT + WT) / 4;  // loads of a wave: two groups of rows, a group of weights, scales
   constexpr int kC = SW ? WT / 2 : WT;   // output column tiles of the workgroup
   constexpr int kCW = SW ? NTW / 2 : NTW;  // and of a wave
   static_assert(WM * WN == 4 && AT % 4 == 0 && WT % 4 == 0, "four waves load alike");
-  __shared__ u32x4 op[4][AT + WT][kWave];
-  __shared__ uint32_t sc[2][AT + WT][kWave];
+  __shared__ u32x4 ax[2][TM * 8];          // two groups of the rows
+  __shared__ u32x4 wx[4][WT][kWave];
+  __shared__ uint32_t sc[AT + WT][kWave];
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave - wm * WN;
   const int r16 = lane & 15, kq = lane >> 4;
-  const int rb = blockIdx.x / a.col_blocks, cb = blockIdx.x - rb * a.col_blocks;
+  int rb, cb;
+  place_of(a, rb, cb);
   const RowBlock b = row_block(a, rb, TM);
   if (b.n <= 0) return;
   const int t0 = cb * kC;
@@ -244,13 +285,19 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   const i32x4 rw1 = raw_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
   const i32x4 rs1 = raw_rsrc((SW ? a.s1 : a.s0) + b.e * a.s_stride, sb);
   const i32x4 ra = raw_rsrc(a.a, a.a_bytes), ras = raw_rsrc(a.as, a.as_bytes);
-  // this wave loads row blocks wave kA .. and weight tiles wave kW ..
-  uint32_t va[kA], vs[kA];
+  // This wave's loads: rows 8 i .. 8 i + 7 of its quarter of the rows, its quarter
+  // of the weight tiles, the scales of its quarter of the row blocks.
+  uint32_t va[kA], vs[AT / 4];
 #pragma unroll
   for (int i = 0; i < kA; ++i) {
-    const int m = 16 * (wave * kA + i) + r16;
+    const int m = 8 * (wave * kA + i) + (lane >> 3);
     const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
-    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G * 64) + (uint32_t)kq * 16u : kOutside;
+    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G * 64) + (uint32_t)((lane & 7) ^ (lane >> 3)) * 16u : kOutside;
+  }
+#pragma unroll
+  for (int i = 0; i < AT / 4; ++i) {
+    const int m = 16 * (wave * (AT / 4) + i) + r16;
+    const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
     vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G4 * 16) + (uint32_t)kq * 4u : kOutside;
   }
   uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, its gate tiles, then its up tiles
@@ -260,81 +307,93 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     wt[i] = (uint32_t)min(t0 + own * kCW + (SW ? j % kCW : j), a.Nt - 1);
   }
   auto is_up = [&](int i) { return SW && (wave * kW + i) % NTW >= kCW; };
-  const uint32_t op_lds = lds_address(&op[0][0][0]), sc_lds = lds_address(&sc[0][0][0]);
-  constexpr uint32_t kSlot = (AT + WT) * 1024, kScSlot = (AT + WT) * 256;
-  // operand load i of group g, scale load i of groups 4 c .. 4 c + 3
-  auto load_op = [&](int i, int g) {
-    const uint32_t to = op_lds + (uint32_t)(g & 3) * kSlot;
+  const uint32_t ax_lds = lds_address(&ax[0][0]), wx_lds = lds_address(&wx[0][0][0]), sc_lds = lds_address(&sc[0][0]);
+  // load i of the rows' groups 2 p and 2 p + 1, of the weights' group g, of the
+  // scales of groups 4 c .. 4 c + 3; nothing past the last group
+  auto load_rows = [&](int i, int p) {
+    buffer_load_lds16(ra, 2 * p < G ? va[i] : kOutside, (uint32_t)p * 128u,
+                      ax_lds + (uint32_t)(p & 1) * (TM * 128u) + (uint32_t)(wave * kA + i) * 1024u);
+  };
+  auto load_weights = [&](int i, int g) {
     const bool in = g < G;
-    if (i < kA)
-      buffer_load_lds16(ra, in ? va[i] : kOutside, (uint32_t)g * 64u, to + (uint32_t)(wave * kA + i) * 1024u);
-    else
-      buffer_load_lds16(is_up(i - kA) ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (wt[i - kA] * G + g) * 1024u : 0u,
-                        to + (uint32_t)(AT + wave * kW + i - kA) * 1024u);
+    buffer_load_lds16(is_up(i) ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (wt[i] * G + g) * 1024u : 0u,
+                      wx_lds + (uint32_t)(g & 3) * (WT * 1024u) + (uint32_t)(wave * kW + i) * 1024u);
   };
   auto load_scale = [&](int i, int c) {
-    const uint32_t to = sc_lds + (uint32_t)(c & 1) * kScSlot;
     const bool in = c < G4;
-    if (i < kA)
-      buffer_load_lds4(ras, in ? vs[i] : kOutside, (uint32_t)c * 16u, to + (uint32_t)(wave * kA + i) * 256u);
+    if (i < AT / 4)
+      buffer_load_lds4(ras, in ? vs[i] : kOutside, (uint32_t)c * 16u, sc_lds + (uint32_t)(wave * (AT / 4) + i) * 256u);
     else
-      buffer_load_lds4(is_up(i - kA) ? rs1 : rs0, in ? (uint32_t)lane * 4u : kOutside, in ? (wt[i - kA] * G4 + c) * 256u : 0u,
-                       to + (uint32_t)(AT + wave * kW + i - kA) * 256u);
+      buffer_load_lds4(is_up(i - AT / 4) ? rs1 : rs0, in ? (uint32_t)lane * 4u : kOutside,
+                       in ? (wt[i - AT / 4] * G4 + c) * 256u : 0u, sc_lds + (uint32_t)(AT + wave * kW + i - AT / 4) * 256u);
   };
+  // [2 p + h]: half h of the group (k blocks 2 h, 2 h + 1) of the blocks 2 p, 2 p + 1
   struct Ops {
     u32x4 x[MTW], w[NTW];
   };
   struct Scales {
     uint32_t x[MTW], w[NTW];
   };
-  constexpr int kR = MTW + NTW;  // blocks that a wave reads
-  auto read_op = [&](Ops& o, int i, int slot) {
-    if (i < MTW) o.x[i] = op[slot][wm * MTW + i][lane];
-    else o.w[i - MTW] = op[slot][AT + wn * NTW + i - MTW][lane];
+  constexpr int kR = MTW + NTW;  // pieces that a wave reads
+  const int r32 = lane & 31;
+  const int piece = (lane >> 5) * 16 + r16, second = r32 >> 4;  // of which block of the pair
+  const int row0 = 16 * wm * MTW + r32, twist = r32 & 7;
+  auto read_op = [&](Ops& o, int i, int g) {  // g: the group modulo 4
+    if (i < MTW) o.x[i] = ax[(g >> 1) & 1][(row0 + 16 * (i & ~1)) * 8 + (((g & 1) * 4 + (i & 1) * 2 + (lane >> 5)) ^ twist)];
+    else o.w[i - MTW] = wx[g][wn * NTW + ((i - MTW) & ~1) + second][(i & 1) * 32 + piece];
   };
-  auto read_scale = [&](Scales& s, int i, int c) {
-    if (i < MTW) s.x[i] = sc[c & 1][wm * MTW + i][lane];
-    else s.w[i - MTW] = sc[c & 1][AT + wn * NTW + i - MTW][lane];
+  auto read_scale = [&](Scales& s, int i) {
+    if (i < MTW) s.x[i] = sc[wm * MTW + (i & ~1) + second][(i & 1) * 32 + piece];
+    else s.w[i - MTW] = sc[AT + wn * NTW + ((i - MTW) & ~1) + second][(i & 1) * 32 + piece];
   };
-  f32x4 acc[MTW][NTW];
+  constexpr int kMP = MTW / 2, kNP = NTW / 2;
+  static_assert(MTW % 2 == 0 && kCW % 2 == 0, "blocks go two by two");
+  f32x16 acc[kMP][kNP];
 #pragma unroll
-  for (int i = 0; i < MTW; ++i)
+  for (int i = 0; i < kMP; ++i)
 #pragma unroll
-    for (int j = 0; j < NTW; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < kNP; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 #pragma unroll
   for (int i = 0; i < kS; ++i) load_scale(i, 0);
 #pragma unroll
-  for (int g = 0; g < 4; ++g)
+  for (int p = 0; p < 2; ++p) {
 #pragma unroll
-    for (int i = 0; i < kL; ++i) load_op(i, g);
-  vm_lds_barrier<3 * kL>();
+    for (int i = 0; i < kA; ++i) load_rows(i, p);
+#pragma unroll
+    for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, 2 * p + i / kW);
+  }
+  vm_lds_barrier<kA + 3 * kW>();
   Ops ops[2];
   Scales s[2];
 #pragma unroll
   for (int i = 0; i < kR; ++i) {
-    read_scale(s[0], i, 0);
+    read_scale(s[0], i);
     read_op(ops[0], i, 0);
   }
   // Group 4 c + J.  The loads and LDS reads stand between the matrix
   // instructions, a few to each, where their issue costs nothing.
   auto step = [&](auto jc, int c, Scales& now, Scales& next) {
     constexpr int J = decltype(jc)::value;
-    constexpr int kScale = J == 0 ? kS : 0, kNext = J == 3 ? kR : 0;
-    constexpr int kMfma = MTW * NTW, kAux = kScale + kNext + kR + kL, kPer = (kAux + kMfma - 1) / kMfma;
+    constexpr int kScale = J == 0 ? kS : 0, kNext = J == 3 ? kR : 0, kRows = J & 1 ? kA : 0;
+    constexpr int kMfma = 2 * kMP * kNP, kAux = kScale + kNext + kR + kRows + kW, kPer = (kAux + kMfma - 1) / kMfma;
     const int g = 4 * c + J;
-    vm_lds_barrier<2 * kL + (J == 1 || J == 2 ? kS : 0)>();
+    // what was loaded after the weights of g + 1 (J even) or the rows of g + 1 (J odd)
+    vm_lds_barrier<(J & 1 ? 2 * kW : 2 * kW + kA) + (J == 1 || J == 2 ? kS : 0)>();
     const Ops& o = ops[J & 1];
     Ops& n = ops[(J & 1) ^ 1];
     auto aux = [&](int q) {
       if (q < kScale) load_scale(q, c + 1);
-      else if (q < kScale + kNext) read_scale(next, q - kScale, c + 1);
-      else if (q < kScale + kNext + kR) read_op(n, q - kScale - kNext, (J + 1) & 3);
-      else if (q < kAux) load_op(q - kScale - kNext - kR, g + 4);
+      else if ((q -= kScale) < kNext) read_scale(next, q);
+      else if ((q -= kNext) < kR) read_op(n, q, (J + 1) & 3);
+      else if ((q -= kR) < kRows) load_rows(q, (g + 3) / 2);
+      else if ((q -= kRows) < kW) load_weights(q, g + 4);
     };
 #pragma unroll
     for (int k = 0; k < kMfma; ++k) {
-      const int j = k / MTW, i = k - j * MTW;
-      acc[i][j] = mfma_mx4<J>(o.w[j], now.w[j], o.x[i], now.x[i], acc[i][j]);
+      const int h = k / (kMP * kNP), j = k / kMP % kNP, i = k % kMP;
+      acc[i][j] = mfma_mx4_32<J>(o.w[2 * j + h], now.w[2 * j + h], o.x[2 * i + h], now.x[2 * i + h], acc[i][j]);
       if (k * kPer < kAux) {
 #pragma unroll
         for (int q = 0; q < kPer; ++q) aux(k * kPer + q);
@@ -351,29 +410,54 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
       if (4 * (c + h) + 3 < G) step(std::integral_constant<int, 3>{}, c + h, s[h], s[h ^ 1]);
     }
   }
-  vm_wait<0>();  // loads past the last group still write LDS
+  vm_lds_barrier<0>();  // loads past the last group still write LDS, other waves read theirs
+  // Register 4 q + c of a pair of blocks holds column 8 q + 4 (lane / 32) + c of
+  // row lane % 32.  Through LDS the rows come out as whole 128-byte lines: 64
+  // fp16 columns, or 32 fp32 ones (results that a residual or another sum awaits).
+  constexpr bool wide = EPI == MX4_ROWS || EPI == MX4_RESIDUAL;
+  uint8_t* my = reinterpret_cast<uint8_t*>(&wx[0][0][0]) + wave * (32 * kTurnRow);
+  static_assert(sizeof(wx) >= 4 * 32 * kTurnRow, "the lines' room");
+  const int tr = lane >> 3, tc = lane & 7;  // row (of 8) and 16-byte piece of a line
 #pragma unroll
-  for (int i = 0; i < MTW; ++i) {
-    const int ml = 16 * (wm * MTW + i) + r16;
-    if (ml >= b.n || (a.rows && (uint32_t)a.rows[b.m0 + ml] >= (uint32_t)a.M)) continue;
-    const int64_t m = b.m0 + ml;
-    u32x2 r[kCW] = {};
-    if constexpr (EPI == MX4_PLAIN)
-      if (a.res) {
+  for (int i = 0; i < kMP; ++i) {
+    const int ml = 16 * (wm * MTW + 2 * i);
 #pragma unroll
-        for (int j = 0; j < kCW; ++j) r[j] = residual(a, m, 16 * min(t0 + wn * kCW + j, a.Nt - 1) + 4 * kq);
+    for (int j = 0; j < kCW / 2; ++j) {
+      const int n = 16 * (t0 + wn * kCW + 2 * j);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          v[c] = acc[i][j][4 * q + c];
+          if constexpr (SW) v[c] = silu(v[c]) * acc[i][j + kNP / 2][4 * q + c];
+        }
+        const int col = 8 * q + 4 * (lane >> 5);
+        if constexpr (wide) *reinterpret_cast<f32x4*>(my + r32 * kTurnRow + 4 * col) = v;
+        else *reinterpret_cast<u32x2*>(my + r32 * kTurnRow + 2 * (32 * (j & 1) + col)) = pack4(v);
       }
+      if (!wide && (j & 1) == 0 && j + 1 < kCW / 2) continue;  // the line's other half
+      const int first = wide ? n : n - 32 * (j & 1);
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int j = 0; j < kCW; ++j) {
-      const int t = t0 + wn * kCW + j;
-      if (t >= a.Nt) continue;
-      f32x4 v = acc[i][j];
-      if constexpr (SW) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = silu(v[q]) * acc[i][j + kCW][q];
+      for (int u = 0; u < 4; ++u) {
+        const int r = 8 * u + tr;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(my + r * kTurnRow + 16 * tc);
+        if (ml + r >= b.n || (a.rows && (uint32_t)a.rows[b.m0 + ml + r] >= (uint32_t)a.M)) continue;
+        const int64_t m = b.m0 + ml + r;
+        const int col = first + (wide ? 4 : 8) * tc;
+        if (col >= a.N || (!wide && (j & 1) == 0 && tc >= 4)) continue;
+        if constexpr (EPI == MX4_ROWS) {
+          *reinterpret_cast<u32x4*>(a.part + m * a.N + col) = v;
+        } else if constexpr (EPI == MX4_RESIDUAL) {
+          f32x4 f = bitcast<f32x4>(v);
+          add_residual(f, residual(a, m, col));
+          *reinterpret_cast<u32x2*>(a.y + m * a.ldy + col) = pack4(f);
+        } else {
+          store_rows16(a.y + m * a.ldy + col, v);
+        }
       }
-      if constexpr (EPI == MX4_PLAIN) add_residual(v, r[j]);
-      write_out<EPI>(a, m, 16 * t + 4 * kq, v);
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
@@ -531,6 +615,7 @@ void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   a.ws = L.ws;
   if (L.epi == MX4_SWIGLU) launch_epi<MX4_SWIGLU>(L, a, st);
   else if (L.epi == MX4_ROWS) launch_epi<MX4_ROWS>(L, a, st);
+  else if (L.res) launch_epi<MX4_RESIDUAL>(L, a, st);
   else launch_epi<MX4_PLAIN>(L, a, st);
 }
 

@@ -153,7 +153,7 @@ void launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t 
 void launch_mx4_prepare(const uint16_t* x, int64_t M, int K, int64_t ldx, uint8_t* codes, uint8_t* scales,
                         hipStream_t st);
 
-enum Mx4Epilogue { MX4_PLAIN, MX4_SWIGLU, MX4_ROWS };
+enum Mx4Epilogue { MX4_PLAIN, MX4_RESIDUAL, MX4_SWIGLU, MX4_ROWS };  // a launch asks for PLAIN, with res or without
 struct Mx4Launch {
   Mx4Epilogue epi;
   const void* w0;  // packed matrices of E experts (E = 1: one matrix)
