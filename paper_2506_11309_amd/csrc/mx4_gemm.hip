@@ -56,7 +56,7 @@ struct Mx4Args {
   int col_blocks;
 };
 
-__device__ __forceinline__ float silu(float g) { return g / (1.f + __expf(-g)); }
+__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 
 // the row block of a workgroup: expert, first output row, number of rows
 struct RowBlock {
@@ -249,8 +249,8 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 // directly: the weights group by group as they are packed, four groups ahead;
 // the activations two groups at a time, so that a row's piece is a whole
 // 128-byte line however the rows are gathered.  The 16-byte pieces of a line
-// stand in LDS at piece ^ (row % 8), so that a column of rows has no bank
-// conflicts.  A step multiplies group g out of registers while it reads group
+// stand in LDS at piece ^ (row / 2 % 8), so that a column of 16 rows covers the
+// 64 banks once.  A step multiplies group g out of registers while it reads group
 // g + 1 from LDS, so neither latency shows; one barrier a step.  Scale words
 // cover four groups: they are loaded in the first of four steps, when every
 // wave has the present ones in registers, and read in the last.
@@ -266,10 +266,11 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   constexpr int kA = 2 * AT / 4, kW = WT / 4, kS = (AT + WT) / 4;  // loads of a wave: two groups of rows, a group of weights, scales
   constexpr int kC = SW ? WT / 2 : WT;   // output column tiles of the workgroup
   constexpr int kCW = SW ? NTW / 2 : NTW;  // and of a wave
-  static_assert(WM * WN == 4 && AT % 4 == 0 && WT % 4 == 0, "four waves load alike");
+  static_assert(WM * WN == 4 && AT % 4 == 0 && WT % 4 == 0, "four waves load alike, rows in whole 16s");
   __shared__ u32x4 ax[2][TM * 8];          // two groups of the rows
   __shared__ u32x4 wx[4][WT][kWave];
   __shared__ uint32_t sc[AT + WT][kWave];
+  __shared__ uint8_t live[TM];  // rows that are written
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave - wm * WN;
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   for (int i = 0; i < kA; ++i) {
     const int m = 8 * (wave * kA + i) + (lane >> 3);
     const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
-    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G * 64) + (uint32_t)((lane & 7) ^ (lane >> 3)) * 16u : kOutside;
+    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
   }
 #pragma unroll
   for (int i = 0; i < AT / 4; ++i) {
@@ -300,6 +301,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
     vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G4 * 16) + (uint32_t)kq * 4u : kOutside;
   }
+  for (int m = threadIdx.x; m < TM; m += 256) live[m] = m < b.n && (!a.rows || (uint32_t)a.rows[b.m0 + m] < (uint32_t)a.M);
   uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, its gate tiles, then its up tiles
 #pragma unroll
   for (int i = 0; i < kW; ++i) {
@@ -337,7 +339,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   constexpr int kR = MTW + NTW;  // pieces that a wave reads
   const int r32 = lane & 31;
   const int piece = (lane >> 5) * 16 + r16, second = r32 >> 4;  // of which block of the pair
-  const int row0 = 16 * wm * MTW + r32, twist = r32 & 7;
+  const int row0 = 16 * wm * MTW + r32, twist = (r32 >> 1) & 7;
   auto read_op = [&](Ops& o, int i, int g) {  // g: the group modulo 4
     if (i < MTW) o.x[i] = ax[(g >> 1) & 1][(row0 + 16 * (i & ~1)) * 8 + (((g & 1) * 4 + (i & 1) * 2 + (lane >> 5)) ^ twist)];
     else o.w[i - MTW] = wx[g][wn * NTW + ((i - MTW) & ~1) + second][(i & 1) * 32 + piece];
@@ -376,29 +378,33 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   // instructions, a few to each, where their issue costs nothing.
   auto step = [&](auto jc, int c, Scales& now, Scales& next) {
     constexpr int J = decltype(jc)::value;
-    constexpr int kScale = J == 0 ? kS : 0, kNext = J == 3 ? kR : 0, kRows = J & 1 ? kA : 0;
-    constexpr int kMfma = 2 * kMP * kNP, kAux = kScale + kNext + kR + kRows + kW, kPer = (kAux + kMfma - 1) / kMfma;
+    constexpr int kScale = J == 0 ? kS : 0, kRows = J & 1 ? kA : 0, kLoads = kScale + kRows + kW;
+    constexpr int kReads = kR + (J == 3 ? kR : 0), kMfma = 2 * kMP * kNP;
     const int g = 4 * c + J;
     // what was loaded after the weights of g + 1 (J even) or the rows of g + 1 (J odd)
     vm_lds_barrier<(J & 1 ? 2 * kW : 2 * kW + kA) + (J == 1 || J == 2 ? kS : 0)>();
     const Ops& o = ops[J & 1];
     Ops& n = ops[(J & 1) ^ 1];
-    auto aux = [&](int q) {
+    auto load = [&](int q) {
       if (q < kScale) load_scale(q, c + 1);
-      else if ((q -= kScale) < kNext) read_scale(next, q);
-      else if ((q -= kNext) < kR) read_op(n, q, (J + 1) & 3);
-      else if ((q -= kR) < kRows) load_rows(q, (g + 3) / 2);
-      else if ((q -= kRows) < kW) load_weights(q, g + 4);
+      else if ((q -= kScale) < kRows) load_rows(q, (g + 3) / 2);
+      else load_weights(q - kRows, g + 4);
     };
+    auto read = [&](int q) {
+      if (q < kR) read_op(n, q, (J + 1) & 3);
+      else read_scale(next, q - kR);
+    };
+    // one LDS read to a matrix instruction, the loads spread evenly: a burst of
+    // them would fill the address unit's queue and hold up the wave
 #pragma unroll
     for (int k = 0; k < kMfma; ++k) {
       const int h = k / (kMP * kNP), j = k / kMP % kNP, i = k % kMP;
       acc[i][j] = mfma_mx4_32<J>(o.w[2 * j + h], now.w[2 * j + h], o.x[2 * i + h], now.x[2 * i + h], acc[i][j]);
-      if (k * kPer < kAux) {
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) aux(k * kPer + q);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int q = k * kReads / kMfma; q < (k + 1) * kReads / kMfma; ++q) read(q);
+#pragma unroll
+      for (int q = k * kLoads / kMfma; q < (k + 1) * kLoads / kMfma; ++q) load(q);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   for (int c = 0; c < G4; c += 2) {
@@ -443,7 +449,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
       for (int u = 0; u < 4; ++u) {
         const int r = 8 * u + tr;
         const u32x4 v = *reinterpret_cast<const u32x4*>(my + r * kTurnRow + 16 * tc);
-        if (ml + r >= b.n || (a.rows && (uint32_t)a.rows[b.m0 + ml + r] >= (uint32_t)a.M)) continue;
+        if (!live[ml + r]) continue;
         const int64_t m = b.m0 + ml + r;
         const int col = first + (wide ? 4 : 8) * tc;
         if (col >= a.N || (!wide && (j & 1) == 0 && tc >= 4)) continue;
