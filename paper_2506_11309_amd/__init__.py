@@ -556,45 +556,41 @@ class DraftTree:
 
 # ------------------------- microscaled 4-bit matrices, mixture of experts
 
-def _rows(t, what, cols=None, dtype_bytes=2):
-    """(rows, columns, row stride) of a matrix whose rows are contiguous: the
-    library takes a pointer and a leading dimension, so a tensor that it would
-    read differently is refused here."""
-    if t.dim() != 2 or t.element_size() != dtype_bytes or (t.shape[1] > 1 and t.stride(1) != 1):
+def _rows(t, what, cols=None):
+    """(rows, columns, row stride) of a 16-bit matrix whose rows are contiguous:
+    the library takes a pointer and a leading dimension, so a tensor that it
+    would read differently is refused here."""
+    try:
+        (M, K), (ld, step) = t.shape, t.stride()
+    except ValueError:
+        raise SwiftSpecError(INVALID_ARG, what) from None
+    if t.element_size() != 2 or (step != 1 and K > 1) or (cols is not None and K != cols):
         raise SwiftSpecError(INVALID_ARG, what)
-    if cols is not None and t.shape[1] != cols:
-        raise SwiftSpecError(INVALID_ARG, what)
-    return t.shape[0], t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return M, K, ld if M > 1 or ld > K else K
 
 
 def _dense(t, what, shape, dtype_bytes):
-    if t is None or tuple(t.shape) != tuple(shape) or t.element_size() != dtype_bytes or not t.is_contiguous():
+    if t is None or t.shape != shape or t.element_size() != dtype_bytes or not t.is_contiguous():
         raise SwiftSpecError(INVALID_ARG, what)
     return t
 
 
-class _On:
-    """The device of a call's tensors, current while the call is made (they
-    must all be on it), and the stream to enqueue on: the caller's, or that
-    device's current one."""
-
-    def __init__(self, where, stream, *tensors):
-        import torch
-        used = [t for t in tensors if t is not None]
-        self._dev = used[0].device
-        if any(t.device != self._dev for t in used) or self._dev.type != "cuda":
+def _run(where, fn, stream, tensors, *args):
+    """Call fn(*args, stream handle) with the tensors' device current (they must
+    all be on it) on `stream`, or on that device's current stream."""
+    import torch
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
             raise SwiftSpecError(INVALID_ARG, where)
-        self._guard = torch.cuda.device(self._dev)
-        self._stream = stream
-
-    def __enter__(self):
-        import torch
-        self._guard.__enter__()
-        s = self._stream if self._stream is not None else torch.cuda.current_stream(self._dev)
-        return ctypes.c_void_p(s.cuda_stream)
-
-    def __exit__(self, *a):
-        self._guard.__exit__(*a)
+    if dev < 0:
+        raise SwiftSpecError(INVALID_ARG, where)
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if torch._C._cuda_getDevice() == dev:
+        _check(fn(*args, s), where)
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, s), where)
 
 
 def make_mx4(codes, scales, packed=None) -> MX4:
@@ -619,8 +615,7 @@ def prepack_mx4(W: MX4, device="cuda", stream=None):
     (keep the tensor alive)."""
     import torch
     t = torch.empty(mx4_packed_bytes(W.K, W.N, W.E), dtype=torch.uint8, device=device)
-    with _On("mx4_prepack", stream, t) as st:
-        _check(_load().swiftspec_mx4_prepack(ctypes.byref(W), _ptr(t), t.numel(), st), "mx4_prepack")
+    _run("mx4_prepack", _load().swiftspec_mx4_prepack, stream, (t,), ctypes.byref(W), t.data_ptr(), t.numel())
     W.packed = t.data_ptr()
     return t
 
@@ -630,8 +625,8 @@ def mx4_quantize(x, codes, scales, stream=None):
     M, K, ld = _rows(x, "mx4_quantize")
     _dense(codes, "mx4_quantize", (M, K // 2), 1)
     _dense(scales, "mx4_quantize", (M, K // 32), 1)
-    with _On("mx4_quantize", stream, x, codes, scales) as st:
-        _check(_load().swiftspec_mx4_quantize(_ptr(x), M, K, ld, _ptr(codes), _ptr(scales), st), "mx4_quantize")
+    _run("mx4_quantize", _load().swiftspec_mx4_quantize, stream, (x, codes, scales), x.data_ptr(), M, K, ld,
+         codes.data_ptr(), scales.data_ptr())
 
 
 def mx4_dequantize(codes, scales, y, stream=None):
@@ -639,8 +634,8 @@ def mx4_dequantize(codes, scales, y, stream=None):
     M, K, ld = _rows(y, "mx4_dequantize")
     _dense(codes, "mx4_dequantize", (M, K // 2), 1)
     _dense(scales, "mx4_dequantize", (M, K // 32), 1)
-    with _On("mx4_dequantize", stream, codes, scales, y) as st:
-        _check(_load().swiftspec_mx4_dequantize(_ptr(codes), _ptr(scales), M, K, _ptr(y), ld, st), "mx4_dequantize")
+    _run("mx4_dequantize", _load().swiftspec_mx4_dequantize, stream, (codes, scales, y), codes.data_ptr(),
+         scales.data_ptr(), M, K, y.data_ptr(), ld)
 
 
 def mx4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
@@ -651,14 +646,14 @@ def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
     """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
     M, _, ldx = _rows(x, "mx4_gemm", W.K)
     m, _, ldy = _rows(y, "mx4_gemm", W.N)
-    r, ldr = M, 0
+    r, ldr, res = M, 0, None
     if residual is not None:
         r, _, ldr = _rows(residual, "mx4_gemm", W.N)
+        res = residual.data_ptr()
     if m != M or r != M:
         raise SwiftSpecError(INVALID_ARG, "mx4_gemm")
-    with _On("mx4_gemm", stream, x, y, ws, residual) as st:
-        _check(_load().swiftspec_mx4_gemm(ctypes.byref(W), _ptr(x), M, ldx, _ptr(y), ldy, _ptr(residual), ldr,
-                                          _ptr(ws), ws.numel() * ws.element_size(), st), "mx4_gemm")
+    _run("mx4_gemm", _load().swiftspec_mx4_gemm, stream, (x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M, ldx,
+         y.data_ptr(), ldy, res, ldr, ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 class MoeGroups:
@@ -694,17 +689,16 @@ def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True,
         raise SwiftSpecError(INVALID_ARG, "moe_route")
     _dense(experts, "moe_route", (T, groups.k), 4)
     _dense(weights, "moe_route", (T, groups.k), 4)
-    with _On("moe_route", stream, logits, experts, weights, ws, *groups._tensors()) as st:
-        _check(_load().swiftspec_moe_route(_ptr(logits), ldl, int(bool(renormalize)), _ptr(experts), _ptr(weights),
-                                           groups._ref(), _ptr(ws), ws.numel() * ws.element_size(), st), "moe_route")
+    _run("moe_route", _load().swiftspec_moe_route, stream, (logits, experts, weights, ws, *groups._tensors()),
+         logits.data_ptr(), ldl, int(bool(renormalize)), experts.data_ptr(), weights.data_ptr(), groups._ref(),
+         ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def moe_group(experts, groups: MoeGroups, ws, stream=None):
     """The groups of given experts [T][k] int32 (outside [0, E): none)."""
     _dense(experts, "moe_group", (groups.T, groups.k), 4)
-    with _On("moe_group", stream, experts, ws, *groups._tensors()) as st:
-        _check(_load().swiftspec_moe_group(_ptr(experts), groups._ref(), _ptr(ws), ws.numel() * ws.element_size(), st),
-               "moe_group")
+    _run("moe_group", _load().swiftspec_moe_group, stream, (experts, ws, *groups._tensors()), experts.data_ptr(),
+         groups._ref(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def moe_mx4_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
@@ -717,10 +711,9 @@ def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
     P, _, ldh = _rows(h, "moe_mx4_swiglu", Wg.N)
     if T != groups.T or P != groups.T * groups.k:
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_swiglu")
-    with _On("moe_mx4_swiglu", stream, x, h, ws, *groups._tensors()) as st:
-        _check(_load().swiftspec_moe_mx4_swiglu(ctypes.byref(Wg), ctypes.byref(Wu), _ptr(x), ldx, groups._ref(),
-                                                _ptr(h), ldh, _ptr(ws), ws.numel() * ws.element_size(), st),
-               "moe_mx4_swiglu")
+    _run("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, stream, (x, h, ws, *groups._tensors()), ctypes.byref(Wg),
+         ctypes.byref(Wu), x.data_ptr(), ldx, groups._ref(), h.data_ptr(), ldh, ws.data_ptr(),
+         ws.numel() * ws.element_size())
 
 
 def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
@@ -732,16 +725,16 @@ def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, s
     y [T][N] fp16, the weighted sum of each token's experts plus residual."""
     P, _, ldh = _rows(h, "moe_mx4_down", Wd.K)
     T, _, ldy = _rows(y, "moe_mx4_down", Wd.N)
-    r, ldr = T, 0
+    r, ldr, res = T, 0, None
     if residual is not None:
         r, _, ldr = _rows(residual, "moe_mx4_down", Wd.N)
+        res = residual.data_ptr()
     if T != groups.T or r != T or P != T * groups.k:
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_down")
     _dense(weights, "moe_mx4_down", (T, groups.k), 4)
-    with _On("moe_mx4_down", stream, h, weights, y, ws, residual, *groups._tensors()) as st:
-        _check(_load().swiftspec_moe_mx4_down(ctypes.byref(Wd), _ptr(h), ldh, groups._ref(), _ptr(weights), _ptr(y),
-                                              ldy, _ptr(residual), ldr, _ptr(ws), ws.numel() * ws.element_size(), st),
-               "moe_mx4_down")
+    _run("moe_mx4_down", _load().swiftspec_moe_mx4_down, stream, (h, weights, y, ws, residual, *groups._tensors()),
+         ctypes.byref(Wd), h.data_ptr(), ldh, groups._ref(), weights.data_ptr(), y.data_ptr(), ldy, res, ldr,
+         ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def make_dims(H, Hq, Hkv, D, F, S_max, eps=1e-5, rope_theta=500000.0) -> Dims:

@@ -127,7 +127,8 @@ __device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f3
 // W waves of a workgroup own NT column tiles (SwiGLU: NT/2 gate and NT/2 up
 // tiles) over all of K and split K between them; sums meet in LDS and are
 // added in wave order.  Nothing is staged: a weight block is one coalesced
-// kilobyte, read once from memory by the wave that multiplies it.
+// kilobyte, read once from memory by the wave that multiplies it, U groups of
+// each tile at a time and the next U on their way.
 template <int W, int MT, int NT, int U, Mx4Epilogue EPI>
 __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   constexpr bool SW = EPI == MX4_SWIGLU;
@@ -206,10 +207,14 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
         if constexpr (U > 3) acc[mt][nt] = mfma_mx4<3>(s.w[3][nt], s.ws[nt], s.x[3][mt], s.xs[mt], acc[mt][nt]);
       }
   };
-  for (int c = c0; c < c1; ++c) {
-    Stage s;
-    load(s, c);
-    multiply(s, c);
+  Stage s[2];
+  if (c0 < c1) load(s[0], c0);
+  for (int c = c0; c < c1; c += 2) {
+    if (c + 1 < c1) load(s[1], c + 1);
+    multiply(s[0], c);
+    if (c + 1 >= c1) break;
+    if (c + 2 < c1) load(s[0], c + 2);
+    multiply(s[1], c + 1);
   }
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
@@ -468,63 +473,11 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   }
 }
 
-// ------------------------------------------------------ blocks of rows
-// map[0] = {offsets are valid, rows of all experts}; map[1 + i] = {expert, first
-// row, rows} of the i-th block of TM rows, experts in order; the blocks past
-// the last have no rows.  Offsets that do not ascend from 0 to at most `most`
-// set the error word and leave every block empty.
-__global__ __launch_bounds__(1024) void mx4_map_kernel(const int32_t* __restrict__ offsets, int E, int most, int TM,
-                                                       int blocks, int32_t* __restrict__ map, void* ws) {
-  __shared__ int first[1025];  // blocks before expert e
-  __shared__ int wave_sum[16];
-  __shared__ int bad;
-  const int e = threadIdx.x, lane = lane_id(), wave = e >> 6;
-  if (e == 0) bad = 0;
-  __syncthreads();
-  int n = 0;
-  if (e < E) {
-    const int lo = offsets[e], hi = offsets[e + 1];
-    if (lo < 0 || hi < lo || hi > most || (e == 0 && lo != 0)) bad = 1;
-    else n = (hi - lo + TM - 1) / TM;
-  }
-  int s = n;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(s, d, kWave);
-    if (lane >= d) s += o;
-  }
-  if (lane == 63) wave_sum[wave] = s;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) s += wave_sum[w];
-  if (e < E) first[e + 1] = s;
-  if (e == 0) first[0] = 0;
-  __syncthreads();
-  if (e == 0) {
-    if (bad) report_error(ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-    map[0] = !bad;
-    map[1] = bad ? 0 : offsets[E];
-  }
-  const int used = bad ? 0 : first[E];
-  for (int i = e; i < blocks; i += 1024) {
-    int lo = 0, hi = E - 1;
-    if (i < used) {
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (first[mid] <= i) lo = mid;
-        else hi = mid - 1;
-      }
-      const int m0 = offsets[lo] + (i - first[lo]) * TM;
-      *reinterpret_cast<u32x4*>(map + 4 * ((int64_t)i + 1)) =
-          u32x4{(uint32_t)lo, (uint32_t)m0, (uint32_t)min(TM, offsets[lo + 1] - m0), 0u};
-    } else {
-      *reinterpret_cast<u32x4*>(map + 4 * ((int64_t)i + 1)) = u32x4{0u, 0u, 0u, 0u};
-    }
-  }
-}
-
 // ---------------------------------------------------------------- combine
-// One thread per 4 columns of a token; the addends in slot order.  Nothing is
-// written where the offsets were invalid (map[0]).
+// One thread per 4 columns of a token; the addends in slot order, KU of them
+// loaded at a time.  Nothing is written where the offsets were invalid (map[0]).
+// Bound by the fp32 rows that it reads.
+template <int KU>
 __global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restrict__ part, int T, int k, int N,
                                                           const int32_t* __restrict__ pos,
                                                           const int32_t* __restrict__ map,
@@ -537,34 +490,38 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restric
   const int n = (int)(i - t * per) * 4;
   const int used = map[1];
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (res) {
+  if (res) add_residual(v, *reinterpret_cast<const u32x2*>(res + t * ldr + n));
+  for (int j0 = 0; j0 < k; j0 += KU) {
+    int p[KU];
+    float w[KU];
+    f32x4 o[KU];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = h2f(res[t * ldr + n + j]);
-  }
-  for (int j = 0; j < k; ++j) {
-    const int p = pos[t * k + j];
-    if (p < 0) continue;
-    if (p >= used) {
-      report_error(ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-      continue;
+    for (int j = 0; j < KU; ++j) {
+      p[j] = j0 + j < k ? pos[t * k + j0 + j] : -1;
+      if (p[j] >= used) {
+        report_error(ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+        p[j] = -1;
+      }
+      w[j] = p[j] >= 0 ? weights[t * k + j0 + j] : 0.f;
     }
-    const float w = weights[t * k + j];
-    const f32x4 o = *reinterpret_cast<const f32x4*>(part + (int64_t)p * N + n);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(w, o[c], v[c]);
+    for (int j = 0; j < KU; ++j)
+      if (p[j] >= 0) o[j] = *reinterpret_cast<const f32x4*>(part + (int64_t)p[j] * N + n);
+#pragma unroll
+    for (int j = 0; j < KU; ++j)
+      if (p[j] >= 0) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(w[j], o[j][c], v[c]);
+      }
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) y[t * ldy + n + j] = f2h(v[j]);
+  *reinterpret_cast<u32x2*>(y + t * ldy + n) = pack4(v);
 }
 
-// the most row blocks of TM rows that M rows of E experts can make
-int row_blocks(int M, int E, int TM) { return (int)((int64_t)M / TM + (E < M ? E : M)); }
-
-template <int MT, Mx4Epilogue EPI>
+template <int W, int MT, int NT, Mx4Epilogue EPI>
 void launch_stream(Mx4Args a, int blocks, hipStream_t st) {
-  constexpr int NT = 2, kC = EPI == MX4_SWIGLU ? 1 : 2;
+  constexpr int kC = EPI == MX4_SWIGLU ? NT / 2 : NT;
   a.col_blocks = (a.Nt + kC - 1) / kC;
-  hipLaunchKernelGGL((mx4_stream_kernel<8, MT, NT, 2, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(512), 0, st, a);
+  hipLaunchKernelGGL((mx4_stream_kernel<W, MT, NT, 2, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(64 * W), 0, st, a);
 }
 
 template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
@@ -574,25 +531,44 @@ void launch_tile(Mx4Args a, int blocks, hipStream_t st) {
   hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(256), 0, st, a);
 }
 
-template <Mx4Epilogue EPI>
-void launch_epi(const Mx4Launch& L, Mx4Args& a, hipStream_t st) {
+// The form of a product and the rows of its row blocks.
+struct Plan {
+  int form, tm;
+};
+enum { STREAM_1, STREAM_2, STREAM_4, TILE_64, TILE_128, TILE_256 };
+constexpr int kRowsOf[] = {16, 32, 64, 64, 128, 256};
+
+Plan plan_of(const Mx4Launch& L) {
   const int avg = L.offsets ? L.M / L.E : L.M;
-  const int TM = avg <= 64 ? 64 : avg <= 256 ? 128 : 256;
-  int blocks = (L.M + TM - 1) / TM;
-  if (L.offsets) {
-    blocks = row_blocks(L.M, L.E, TM);
-    hipLaunchKernelGGL(mx4_map_kernel, dim3(1), dim3(1024), 0, st, L.offsets, L.E, L.M, TM, blocks, L.map, L.ws);
+  const int form = avg <= 16 ? STREAM_1 : avg <= 32 ? STREAM_2 : avg <= 64 ? STREAM_4 : avg <= 256 ? TILE_128 : TILE_256;
+  return Plan{form, kRowsOf[form]};
+}
+
+template <Mx4Epilogue EPI>
+void launch_form(int form, const Mx4Args& a, int blocks, hipStream_t st) {
+  switch (form) {
+    case STREAM_1: return launch_stream<8, 1, 2, EPI>(a, blocks, st);
+    case STREAM_2: return launch_stream<8, 2, 2, EPI>(a, blocks, st);
+    case STREAM_4: return launch_stream<8, 4, 2, EPI>(a, blocks, st);
+    case TILE_64: return launch_tile<1, 4, 4, 4, EPI>(a, blocks, st);
+    case TILE_128: return launch_tile<2, 2, 4, 4, EPI>(a, blocks, st);
+    default: return launch_tile<2, 2, 8, 8, EPI>(a, blocks, st);
   }
-  if (TM == 64) launch_stream<4, EPI>(a, blocks, st);
-  else if (TM == 128) launch_tile<2, 2, 4, 4, EPI>(a, blocks, st);
-  else launch_tile<2, 2, 8, 8, EPI>(a, blocks, st);
 }
 
 }  // namespace
 
-size_t mx4_map_bytes(int M, int E) { return ((size_t)row_blocks(M, E, 16) + 1) * 16; }
-
 void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
+  const Plan p = plan_of(L);
+  Mx4Map map = {};
+  map.offsets = L.offsets;
+  map.E = L.E;
+  map.M = L.M;
+  map.tm = p.tm;
+  map.blocks = L.offsets ? mx4_row_blocks(L.M, L.E, p.tm) : (L.M + p.tm - 1) / p.tm;
+  map.map = L.map;
+  map.ws = L.ws;
+  launch_mx4_prepare(L.x, L.a_rows, L.K, L.ldx, L.a, L.a_scales, L.rows ? nullptr : L.offsets, map, st);
   Mx4Args a = {};
   const size_t wq = mx4_code_bytes(L.N, L.K), wsb = mx4_scale_bytes(L.N, L.K);
   a.w0 = static_cast<const uint8_t*>(L.w0);
@@ -619,17 +595,19 @@ void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   a.ldr = L.ldr;
   a.part = L.part;
   a.ws = L.ws;
-  if (L.epi == MX4_SWIGLU) launch_epi<MX4_SWIGLU>(L, a, st);
-  else if (L.epi == MX4_ROWS) launch_epi<MX4_ROWS>(L, a, st);
-  else if (L.res) launch_epi<MX4_RESIDUAL>(L, a, st);
-  else launch_epi<MX4_PLAIN>(L, a, st);
+  if (L.epi == MX4_SWIGLU) launch_form<MX4_SWIGLU>(p.form, a, map.blocks, st);
+  else if (L.epi == MX4_ROWS) launch_form<MX4_ROWS>(p.form, a, map.blocks, st);
+  else if (L.res) launch_form<MX4_RESIDUAL>(p.form, a, map.blocks, st);
+  else launch_form<MX4_PLAIN>(p.form, a, map.blocks, st);
 }
 
 void launch_moe_combine(const float* part, int T, int k, int N, const int32_t* pos, const int32_t* map,
                         const float* weights, uint16_t* y, int64_t ldy, const uint16_t* res, int64_t ldr, void* ws,
                         hipStream_t st) {
-  hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)(((int64_t)T * (N / 4) + 255) / 256)), dim3(256), 0, st, part, T, k, N,
-                     pos, map, weights, y, ldy, res, ldr, ws);
+  const dim3 grid((unsigned)(((int64_t)T * (N / 4) + 255) / 256));
+  if (k <= 2) hipLaunchKernelGGL(moe_combine_kernel<2>, grid, dim3(256), 0, st, part, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
+  else if (k <= 4) hipLaunchKernelGGL(moe_combine_kernel<4>, grid, dim3(256), 0, st, part, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
+  else hipLaunchKernelGGL(moe_combine_kernel<8>, grid, dim3(256), 0, st, part, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
 }
 
 }  // namespace ss

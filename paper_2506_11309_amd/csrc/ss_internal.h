@@ -149,9 +149,24 @@ void launch_mx4_quantize(const uint16_t* x, int64_t M, int K, int64_t ldx, uint8
                          hipStream_t st);
 void launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int K, uint16_t* y, int64_t ldy,
                            hipStream_t st);
-// x [M][ldx] fp16 -> the activations' operand form
+// The row blocks of a product, which the preparation of its activations writes
+// for experts (offsets not null):  map[0] = {offsets are valid, rows of all
+// experts}; map[1 + i] = {expert, first row, rows} of the i-th block of tm rows,
+// experts in order; the blocks past the last have no rows.  Offsets that do not
+// ascend from 0 to at most M set the error word and leave every block empty.
+struct Mx4Map {
+  const int32_t* offsets;
+  int E, M, tm, blocks;
+  int32_t* map;
+  void* ws;
+};
+// the most blocks of tm rows that M rows of E experts can make
+inline int mx4_row_blocks(int M, int E, int tm) { return M / tm + (E < M ? E : M); }
+inline size_t mx4_map_bytes(int M, int E) { return ((size_t)mx4_row_blocks(M, E, 16) + 1) * 16; }
+// x [M][ldx] fp16 -> the activations' operand form; with experts whose rows are
+// in order (last not null) only the first last[E] rows
 void launch_mx4_prepare(const uint16_t* x, int64_t M, int K, int64_t ldx, uint8_t* codes, uint8_t* scales,
-                        hipStream_t st);
+                        const int32_t* last, const Mx4Map& map, hipStream_t st);
 
 enum Mx4Epilogue { MX4_PLAIN, MX4_RESIDUAL, MX4_SWIGLU, MX4_ROWS };  // a launch asks for PLAIN, with res or without
 struct Mx4Launch {
@@ -159,9 +174,10 @@ struct Mx4Launch {
   const void* w0;  // packed matrices of E experts (E = 1: one matrix)
   const void* w1;  // up projections of the SwiGLU
   int K, N, E;
-  const uint8_t* a;         // activations, operand form
-  const uint8_t* a_scales;
-  int64_t a_rows;           // rows of a
+  const uint16_t* x;        // activations [a_rows][ldx] fp16
+  int64_t ldx, a_rows;
+  uint8_t* a;               // and room for their operand form
+  uint8_t* a_scales;
   int M;                    // output rows: of the matrix, or the most that the experts share (T k)
   // experts: row i of the output belongs to the expert e with offsets[e] <= i < offsets[e + 1]
   const int32_t* offsets;   // null: one matrix, rows 0 .. M-1
@@ -175,7 +191,7 @@ struct Mx4Launch {
   float* part;              // fp32 output [M][N] (ROWS)
   void* ws;                 // error word
 };
-size_t mx4_map_bytes(int M, int E);
+// quantises the activations, then multiplies
 void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st);
 // y[t] = fp16(res[t] + sum over j < k with pos[t][j] >= 0 of weights[t][j] part[pos[t][j]]);
 // map as the product's launch left it

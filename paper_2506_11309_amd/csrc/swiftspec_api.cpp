@@ -629,13 +629,14 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
   if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   uint8_t* base = static_cast<uint8_t*>(ws);
   hipStream_t st = S(stream);
-  ss::launch_mx4_prepare(x, M, W->K, ldx, base + w.codes, base + w.scales, st);
   ss::Mx4Launch L = {};
   L.epi = ss::MX4_PLAIN;
   L.w0 = W->packed;
   L.K = W->K;
   L.N = W->N;
   L.E = 1;
+  L.x = x;
+  L.ldx = ldx;
   L.a = base + w.codes;
   L.a_scales = base + w.scales;
   L.a_rows = L.M = M;
@@ -703,7 +704,6 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
   if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   uint8_t* base = static_cast<uint8_t*>(ws);
   hipStream_t st = S(stream);
-  ss::launch_mx4_prepare(x, groups->T, Wg->K, ldx, base + w.codes, base + w.scales, st);
   ss::Mx4Launch L = {};
   L.epi = ss::MX4_SWIGLU;
   L.w0 = Wg->packed;
@@ -711,6 +711,8 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
   L.K = Wg->K;
   L.N = Wg->N;
   L.E = Wg->E;
+  L.x = x;
+  L.ldx = ldx;
   L.a = base + w.codes;
   L.a_scales = base + w.scales;
   L.a_rows = groups->T;
@@ -752,13 +754,14 @@ int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t l
   uint8_t* base = static_cast<uint8_t*>(ws);
   float* part = reinterpret_cast<float*>(base + w.part);
   hipStream_t st = S(stream);
-  ss::launch_mx4_prepare(h, pairs, Wd->K, ldh, base + w.codes, base + w.scales, st);
   ss::Mx4Launch L = {};
   L.epi = ss::MX4_ROWS;
   L.w0 = Wd->packed;
   L.K = Wd->K;
   L.N = Wd->N;
   L.E = Wd->E;
+  L.x = h;
+  L.ldx = ldh;
   L.a = base + w.codes;
   L.a_scales = base + w.scales;
   L.a_rows = pairs;
