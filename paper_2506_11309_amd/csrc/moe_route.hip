@@ -7,7 +7,7 @@
 // their key is 0 and they have no share of the softmax.
 // The grouping is a counting sort: each workgroup counts its stretch of pairs
 // per expert; a second launch adds the counts of the stretches before it and
-// ranks its own pairs in order.  Counts are integers, so the order of the LDS
+// ranks its own pairs in order (up to 1024 pairs: one workgroup, one launch).  Counts are integers, so the order of the LDS
 // atomics that add them does not show.
 #include "ss_device.h"
 #include "ss_internal.h"
@@ -27,15 +27,22 @@ __host__ __device__ inline int stretch_tokens(int T, int k) {
   return need > least ? need : least;
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d, kWave));
-  return v;
+// Over the 16 lanes of a row (rotations within it): every lane gets the result.
+template <int kRotate>
+__device__ __forceinline__ uint32_t rotated(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x120 + kRotate, 0xF, 0xF, true);  // row_ror
 }
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, kWave);
-  return v;
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max(v, rotated<8>(v));
+  v = max(v, rotated<4>(v));
+  v = max(v, rotated<2>(v));
+  return max(v, rotated<1>(v));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += bitcast<float>(rotated<8>(bitcast<uint32_t>(v)));
+  v += bitcast<float>(rotated<4>(bitcast<uint32_t>(v)));
+  v += bitcast<float>(rotated<2>(bitcast<uint32_t>(v)));
+  return v + bitcast<float>(rotated<1>(bitcast<uint32_t>(v)));
 }
 
 // ascending 16-bit key of an fp16 score, 0 where masked (-inf, NaN); +inf counts as 65504
@@ -49,37 +56,74 @@ __device__ __forceinline__ float key_score(uint32_t key) {
   return h2f((uint16_t)(key & 0x8000u ? key - 0x8000u : 0xFFFFu - key));
 }
 
-// One wave: top k of the token's row.  Lane j < k gets the j-th expert and weight.
+struct RouteArgs {
+  const uint16_t* logits;
+  int64_t ldl;
+  int T, E, k, renormalize, tokens;
+  bool lines;  // rows can be read 16 bytes at a time
+  int32_t* experts;
+  float* weights;
+  int32_t *offsets, *rows, *pos, *hist;
+};
+
+// 16 lanes take the top k of a token's row, V scores each (from 8 on in whole
+// 16-byte pieces, 8 (16 q + lane) .. + 7), so that a wave routes four tokens and
+// its reductions stay within the rows of 16 lanes that the ALU shifts in.  Lane
+// j < k keeps the j-th expert; every lane follows the sums.  Where t >= T nothing
+// is written.
 template <int V>
-__device__ __forceinline__ void route_token(const uint16_t* row, int E, int k, bool renormalize, int32_t* experts, float* weights,
-                                            int* counts) {
-  const int lane = lane_id();
+__device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* counts) {
+  const int l = lane_id() & 15;
+  const bool there = t < a.T;
+  const uint16_t* row = a.logits + (int64_t)(there ? t : 0) * a.ldl;
   uint32_t key[V];
+  if constexpr (V < 8) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int e = l + 16 * i;
+      key[i] = e < a.E ? row[e] : 0xFC00u;
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < V / 8; ++q) {
+      const int e = 8 * (16 * q + l);
+      u32x4 v = {0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
+      if (a.lines && e + 8 <= a.E) {
+        v = *reinterpret_cast<const u32x4*>(row + e);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (e + i < a.E) v[i >> 1] = i & 1 ? (v[i >> 1] & 0xFFFFu) | (uint32_t)row[e + i] << 16 : (v[i >> 1] & 0xFFFF0000u) | row[e + i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) key[8 * q + i] = i & 1 ? v[i >> 1] >> 16 : v[i >> 1] & 0xFFFFu;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int e = lane + 64 * i;
-    const uint32_t s = e < E ? score_key(row[e]) : 0u;
+    const int e = V < 8 ? l + 16 * i : 8 * (16 * (i >> 3) + l) + (i & 7);
+    const uint32_t s = score_key(key[i]);
     key[i] = s ? s << 16 | (0xFFFFu - (uint32_t)e) : 0u;
   }
   uint32_t best = 0;
   float top = 0.f, mine = 0.f, chosen = 0.f, all = 0.f;
-  for (int j = 0; j < k; ++j) {
+  for (int j = 0; j < a.k; ++j) {
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) m = max(m, key[i]);
-    m = wave_max(m);
+    m = row_max(m);
     if (j == 0) {
       top = m ? key_score(m >> 16) : 0.f;
-      if (!renormalize) {
+      if (!a.renormalize) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
           if (key[i]) all += expf(key_score(key[i] >> 16) - top);
-        all = wave_sum(all);
+        all = row_sum(all);
       }
     }
     const float p = m ? expf(key_score(m >> 16) - top) : 0.f;
     chosen += p;
-    if (lane == j) {
+    if (l == j) {
       best = m;
       mine = p;
     }
@@ -87,36 +131,25 @@ __device__ __forceinline__ void route_token(const uint16_t* row, int E, int k, b
     for (int i = 0; i < V; ++i)
       if (key[i] == m) key[i] = 0;
   }
-  if (lane < k) {
+  if (l < a.k && there) {
     const int e = best ? (int)(0xFFFFu - (best & 0xFFFFu)) : -1;
-    const float total = renormalize ? chosen : all;
-    experts[lane] = e;
-    weights[lane] = best ? mine / total : 0.f;
+    const float total = a.renormalize ? chosen : all;
+    a.experts[(int64_t)t * a.k + l] = e;
+    a.weights[(int64_t)t * a.k + l] = best ? mine / total : 0.f;
     if (e >= 0) atomicAdd(counts + e, 1);
   }
 }
 
-struct RouteArgs {
-  const uint16_t* logits;
-  int64_t ldl;
-  int T, E, k, renormalize, tokens;
-  int32_t* experts;
-  float* weights;
-  int32_t *offsets, *rows, *pos, *hist;
-};
-
-// Choose (or read) a stretch's experts and count them.
+// Choose (or read) the experts of tokens t0 .. t1 and count them.
 template <int V>
-__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
-  __shared__ int counts[kMaxE];
-  const int wave = threadIdx.x >> 6;
+__device__ __forceinline__ void route_stretch(const RouteArgs& a, int t0, int t1, int* counts) {
   for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
   __syncthreads();
-  const int t0 = blockIdx.x * a.tokens, t1 = min(a.T, t0 + a.tokens);
   if (a.logits) {
-    for (int t = t0 + wave; t < t1; t += kWaves)
-      route_token<V>(a.logits + t * a.ldl, a.E, a.k, a.renormalize != 0, a.experts + (int64_t)t * a.k,
-                     a.weights + (int64_t)t * a.k, counts);
+    for (int t = t0 + 4 * (int)(threadIdx.x >> 6); t < t1; t += 4 * kWaves) {
+      const int mine = t + (lane_id() >> 4);
+      route_token<V>(a, mine < t1 ? mine : a.T, counts);
+    }
   } else {
     for (int i = t0 * a.k + (int)threadIdx.x; i < t1 * a.k; i += kThreads) {
       const int e = a.experts[i];
@@ -124,51 +157,50 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += kThreads) a.hist[(int64_t)blockIdx.x * a.E + e] = counts[e];
 }
 
-// Offsets, and the places of this stretch's pairs.
-__global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int stretches) {
-  __shared__ int base[kMaxE];           // next place of each expert's pairs in this stretch
-  __shared__ int count[kWaves][kMaxE];  // pairs of each wave
-  __shared__ int wave_total[kWaves];
+struct GroupLds {
+  int base[kMaxE];           // next place of each expert's pairs in this stretch
+  int count[kWaves][kMaxE];  // pairs of each wave
+  int wave_total[kWaves];
+};
+
+// The places of the pairs of tokens t0 .. t1.  Thread e brings expert e's pairs
+// in all stretches and in those before this one.
+__device__ __forceinline__ void group_stretch(const RouteArgs& a, int t0, int t1, int all, int before, bool writes_offsets,
+                                              GroupLds& s) {
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
-  // totals of all stretches, and of those before this one
-  int all = 0, before = 0;
-  if (tid < a.E)
-    for (int s = 0; s < stretches; ++s) {
-      const int c = a.hist[(int64_t)s * a.E + tid];
-      all += c;
-      before += s < (int)blockIdx.x ? c : 0;
-    }
   int scan = all;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int o = __shfl_up(scan, d, kWave);
     if (lane >= d) scan += o;
   }
-  if (lane == 63) wave_total[wave] = scan;
+  if (lane == 63) s.wave_total[wave] = scan;
   __syncthreads();
   int lead = 0, used = 0;
+#pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    lead += w < wave ? wave_total[w] : 0;
-    used += wave_total[w];
+    const int n = s.wave_total[w];
+    lead += w < wave ? n : 0;
+    used += n;
   }
   if (tid < a.E) {
     const int off = lead + scan - all;
-    base[tid] = off + before;
-    if (blockIdx.x == 0) {
+    s.base[tid] = off + before;
+    if (writes_offsets) {
       a.offsets[tid] = off;
       if (tid == a.E - 1) a.offsets[a.E] = off + all;
     }
   }
-  const int n0 = blockIdx.x * a.tokens * a.k, n1 = min(a.T, (int)(blockIdx.x + 1) * a.tokens) * a.k;
+  const int n0 = t0 * a.k, n1 = t1 * a.k;
   // places past the last pair
   for (int i = n0 + tid; i < n1; i += kThreads)
     if (i >= used) a.rows[i] = -1;
   for (int i0 = n0; i0 < n1; i0 += kThreads) {
-    __syncthreads();
-    for (int i = tid; i < kWaves * a.E; i += kThreads) count[i / a.E][i % a.E] = 0;
+    if (tid < a.E)
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) s.count[w][tid] = 0;
     __syncthreads();
     const int i = i0 + tid;
     int e = i < n1 ? a.experts[i] : -1;
@@ -182,21 +214,82 @@ __global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int stretc
       same &= (e >> bit) & 1 ? m : ~m;
     }
     const int rank = __popcll(same & ((1ull << lane) - 1));
-    if (has && rank == 0) count[wave][e] = __popcll(same);
+    if (has && rank == 0) s.count[wave][e] = __popcll(same);
     __syncthreads();
     int place = -1;
     if (has) {
-      place = base[e] + rank;
-      for (int w = 0; w < wave; ++w) place += count[w][e];
+      place = s.base[e] + rank;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) place += w < wave ? s.count[w][e] : 0;
+      a.rows[place] = i;
     }
     if (i < n1) a.pos[i] = place;
-    if (has) a.rows[place] = i;
+    if (i0 + kThreads >= n1) break;
     __syncthreads();
-    for (int x = tid; x < a.E; x += kThreads) {
+    if (tid < a.E) {
       int c = 0;
-      for (int w = 0; w < kWaves; ++w) c += count[w][x];
-      base[x] += c;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) c += s.count[w][tid];
+      s.base[tid] += c;
     }
+    __syncthreads();
+  }
+}
+
+// One stretch: everything in one workgroup.
+template <int V>
+__global__ __launch_bounds__(kThreads) void route_one_kernel(RouteArgs a) {
+  __shared__ int counts[kMaxE];
+  __shared__ GroupLds s;
+  route_stretch<V>(a, 0, a.T, counts);
+  group_stretch(a, 0, a.T, (int)threadIdx.x < a.E ? counts[threadIdx.x] : 0, 0, true, s);
+}
+
+// Several: count, then place.
+template <int V>
+__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+  __shared__ int counts[kMaxE];
+  const int t0 = blockIdx.x * a.tokens;
+  route_stretch<V>(a, t0, min(a.T, t0 + a.tokens), counts);
+  for (int e = threadIdx.x; e < a.E; e += kThreads) a.hist[(int64_t)blockIdx.x * a.E + e] = counts[e];
+}
+
+__global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int stretches) {
+  __shared__ int part_all[kThreads], part_before[kThreads];
+  __shared__ GroupLds s;
+  // a power of two of experts side by side, the stretches shared out between
+  // the parts of the workgroup that this leaves
+  const int tid = threadIdx.x, wide = 1 << (32 - __builtin_clz(max(a.E, 2) - 1));
+  const int part = tid / wide, parts = kThreads / wide, e = tid - part * wide;
+  int all = 0, before = 0;
+  if (e < a.E) {
+#pragma unroll 8
+    for (int i = part; i < stretches; i += parts) {
+      const int c = a.hist[(int64_t)i * a.E + e];
+      all += c;
+      before += i < (int)blockIdx.x ? c : 0;
+    }
+  }
+  part_all[tid] = all;
+  part_before[tid] = before;
+  __syncthreads();
+  all = before = 0;
+  if (tid < a.E)
+    for (int p = 0; p < parts; ++p) {
+      all += part_all[p * wide + tid];
+      before += part_before[p * wide + tid];
+    }
+  const int t0 = blockIdx.x * a.tokens;
+  group_stretch(a, t0, min(a.T, t0 + a.tokens), all, before, blockIdx.x == 0, s);
+}
+
+template <int V>
+void launch_route(const RouteArgs& a, int stretches, hipStream_t st) {
+  if (stretches <= 1) {
+    hipLaunchKernelGGL(route_one_kernel<V>, dim3(1), dim3(kThreads), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(route_kernel<V>, dim3((unsigned)stretches), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL(group_kernel, dim3((unsigned)stretches), dim3(kThreads), 0, st, a, stretches);
   }
 }
 
@@ -222,16 +315,15 @@ void launch_moe_route(const RouteLaunch& L, hipStream_t st) {
   a.rows = L.rows;
   a.pos = L.pos;
   a.hist = L.hist;
+  a.lines = (reinterpret_cast<uintptr_t>(L.logits) & 15) == 0 && L.ldl % 8 == 0;
   const int stretches = (L.T + a.tokens - 1) / a.tokens;
-  const int v = L.logits ? (L.E + 63) / 64 : 1;
-  const dim3 grid((unsigned)stretches), block(kThreads);
-  if (stretches > 0) {
-    if (v <= 1) hipLaunchKernelGGL(route_kernel<1>, grid, block, 0, st, a);
-    else if (v <= 2) hipLaunchKernelGGL(route_kernel<2>, grid, block, 0, st, a);
-    else if (v <= 4) hipLaunchKernelGGL(route_kernel<4>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(route_kernel<8>, grid, block, 0, st, a);
-  }
-  hipLaunchKernelGGL(group_kernel, dim3((unsigned)(stretches > 0 ? stretches : 1)), block, 0, st, a, stretches);
+  const int v = L.logits ? (L.E + 15) / 16 : 1;  // scores of a lane
+  if (v <= 1) launch_route<1>(a, stretches, st);
+  else if (v <= 2) launch_route<2>(a, stretches, st);
+  else if (v <= 4) launch_route<4>(a, stretches, st);
+  else if (v <= 8) launch_route<8>(a, stretches, st);
+  else if (v <= 16) launch_route<16>(a, stretches, st);
+  else launch_route<32>(a, stretches, st);
 }
 
 }  // namespace ss
