@@ -5,9 +5,9 @@
 // above the complement of the index, so that one unsigned maximum gives the
 // largest score and, among equals, the lowest index.  -inf and NaN are masked:
 // their key is 0 and they have no share of the softmax.
-// The grouping is a counting sort: each workgroup counts its stretch of pairs
-// per expert; a second launch adds the counts of the stretches before it and
-// ranks its own pairs in order (up to 1024 pairs: one workgroup, one launch).  Counts are integers, so the order of the LDS
+// The grouping is a counting sort: each workgroup counts its unit of tokens'
+// pairs per expert; a second launch adds the counts of the units before its own
+// and ranks its pairs in order (up to 1024 pairs: one workgroup, one launch).  Counts are integers, so the order of the LDS
 // atomics that add them does not show.
 #include "ss_device.h"
 #include "ss_internal.h"
@@ -18,13 +18,16 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxE = SWIFTSPEC_MAX_EXPERTS;
-constexpr int kMaxStretches = 128;
+constexpr int kUnitThreads = 512;  // of the workgroup that routes a unit of tokens
+constexpr int kUnits = 2;          // units that a workgroup groups
 
-// tokens of a stretch: whole tokens, at most kMaxStretches stretches
-__host__ __device__ inline int stretch_tokens(int T, int k) {
-  const int least = kThreads / k;  // about one pair a thread
-  const int need = (T + kMaxStretches - 1) / kMaxStretches;
-  return need > least ? need : least;
+// Tokens of a unit: about one pair a thread, so that a prompt fills the chip, but
+// at most 256 units (each grouping workgroup reads all their counts) as long as
+// a unit's counts fit 16 bits.
+inline int unit_tokens(int T, int k) {
+  const int least = kUnitThreads / k, most = 65535 / k;
+  const int need = (T + 255) / 256;
+  return need < least ? least : need > most ? most : need;
 }
 
 // Over the 16 lanes of a row (rotations within it): every lane gets the result.
@@ -63,14 +66,14 @@ struct RouteArgs {
   bool lines;  // rows can be read 16 bytes at a time
   int32_t* experts;
   float* weights;
-  int32_t *offsets, *rows, *pos, *hist;
+  int32_t *offsets, *rows, *pos;
+  uint16_t* hist;  // [units][E rounded up to 4]
 };
 
 // 16 lanes take the top k of a token's row, V scores each (from 8 on in whole
 // 16-byte pieces, 8 (16 q + lane) .. + 7), so that a wave routes four tokens and
 // its reductions stay within the rows of 16 lanes that the ALU shifts in.  Lane
-// j < k keeps the j-th expert; every lane follows the sums.  Where t >= T nothing
-// is written.
+// j < k keeps the j-th expert.  Where t >= T nothing is written.
 template <int V>
 __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* counts) {
   const int l = lane_id() & 15;
@@ -105,35 +108,33 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* coun
     const uint32_t s = score_key(key[i]);
     key[i] = s ? s << 16 | (0xFFFFu - (uint32_t)e) : 0u;
   }
-  uint32_t best = 0;
-  float top = 0.f, mine = 0.f, chosen = 0.f, all = 0.f;
-  for (int j = 0; j < a.k; ++j) {
-    uint32_t m = 0;
+  // the j-th largest key, all keys that are there being different: the largest
+  // difference, modulo 2^32, to the one before it is that of the next below
+  uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) m = max(m, key[i]);
-    m = row_max(m);
-    if (j == 0) {
-      top = m ? key_score(m >> 16) : 0.f;
-      if (!a.renormalize) {
+  for (int i = 0; i < V; ++i) m = max(m, key[i]);
+  m = row_max(m);
+  const float top = m ? key_score(m >> 16) : 0.f;
+  uint32_t best = l == 0 ? m : 0u;
+  for (int j = 1; j < a.k; ++j) {
+    uint32_t d = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (key[i]) all += expf(key_score(key[i] >> 16) - top);
-        all = row_sum(all);
-      }
-    }
-    const float p = m ? expf(key_score(m >> 16) - top) : 0.f;
-    chosen += p;
-    if (l == j) {
-      best = m;
-      mine = p;
-    }
+    for (int i = 0; i < V; ++i) d = max(d, key[i] - m);
+    d = row_max(d);
+    m = m ? m + d : 0u;
+    if (l == j) best = m;
+  }
+  const float mine = best ? expf(key_score(best >> 16) - top) : 0.f;
+  float total = mine;
+  if (!a.renormalize) {
+    total = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (key[i] == m) key[i] = 0;
+      if (key[i]) total += expf(key_score(key[i] >> 16) - top);
   }
+  total = row_sum(total);
   if (l < a.k && there) {
     const int e = best ? (int)(0xFFFFu - (best & 0xFFFFu)) : -1;
-    const float total = a.renormalize ? chosen : all;
     a.experts[(int64_t)t * a.k + l] = e;
     a.weights[(int64_t)t * a.k + l] = best ? mine / total : 0.f;
     if (e >= 0) atomicAdd(counts + e, 1);
@@ -142,16 +143,17 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* coun
 
 // Choose (or read) the experts of tokens t0 .. t1 and count them.
 template <int V>
-__device__ __forceinline__ void route_stretch(const RouteArgs& a, int t0, int t1, int* counts) {
-  for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
+__device__ __forceinline__ void route_tokens(const RouteArgs& a, int t0, int t1, int* counts) {
+  const int threads = blockDim.x;
+  for (int e = threadIdx.x; e < a.E; e += threads) counts[e] = 0;
   __syncthreads();
   if (a.logits) {
-    for (int t = t0 + 4 * (int)(threadIdx.x >> 6); t < t1; t += 4 * kWaves) {
+    for (int t = t0 + 4 * (int)(threadIdx.x >> 6); t < t1; t += threads / 16) {
       const int mine = t + (lane_id() >> 4);
       route_token<V>(a, mine < t1 ? mine : a.T, counts);
     }
   } else {
-    for (int i = t0 * a.k + (int)threadIdx.x; i < t1 * a.k; i += kThreads) {
+    for (int i = t0 * a.k + (int)threadIdx.x; i < t1 * a.k; i += threads) {
       const int e = a.experts[i];
       if (e >= 0 && e < a.E) atomicAdd(counts + e, 1);
     }
@@ -160,14 +162,14 @@ __device__ __forceinline__ void route_stretch(const RouteArgs& a, int t0, int t1
 }
 
 struct GroupLds {
-  int base[kMaxE];           // next place of each expert's pairs in this stretch
+  int base[kMaxE];           // next place of each expert's pairs
   int count[kWaves][kMaxE];  // pairs of each wave
   int wave_total[kWaves];
 };
 
-// The places of the pairs of tokens t0 .. t1.  Thread e brings expert e's pairs
-// in all stretches and in those before this one.
-__device__ __forceinline__ void group_stretch(const RouteArgs& a, int t0, int t1, int all, int before, bool writes_offsets,
+// The places of the pairs of tokens t0 .. t1.  Thread e brings the number of expert
+// e's pairs, of all tokens and of those before t0.
+__device__ __forceinline__ void group_tokens(const RouteArgs& a, int t0, int t1, int all, int before, bool writes_offsets,
                                               GroupLds& s) {
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   int scan = all;
@@ -236,68 +238,82 @@ __device__ __forceinline__ void group_stretch(const RouteArgs& a, int t0, int t1
   }
 }
 
-// One stretch: everything in one workgroup.
+// Up to 1024 pairs: everything in one workgroup.
 template <int V>
 __global__ __launch_bounds__(kThreads) void route_one_kernel(RouteArgs a) {
   __shared__ int counts[kMaxE];
   __shared__ GroupLds s;
-  route_stretch<V>(a, 0, a.T, counts);
-  group_stretch(a, 0, a.T, (int)threadIdx.x < a.E ? counts[threadIdx.x] : 0, 0, true, s);
+  route_tokens<V>(a, 0, a.T, counts);
+  group_tokens(a, 0, a.T, (int)threadIdx.x < a.E ? counts[threadIdx.x] : 0, 0, true, s);
 }
 
-// Several: count, then place.
+// More: count, then place.
 template <int V>
-__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+__global__ __launch_bounds__(kUnitThreads) void route_kernel(RouteArgs a) {
   __shared__ int counts[kMaxE];
   const int t0 = blockIdx.x * a.tokens;
-  route_stretch<V>(a, t0, min(a.T, t0 + a.tokens), counts);
-  for (int e = threadIdx.x; e < a.E; e += kThreads) a.hist[(int64_t)blockIdx.x * a.E + e] = counts[e];
+  route_tokens<V>(a, t0, min(a.T, t0 + a.tokens), counts);
+  const int Ep = (a.E + 3) & ~3;
+  for (int e = threadIdx.x; e < Ep; e += kUnitThreads) a.hist[(int64_t)blockIdx.x * Ep + e] = e < a.E ? (uint16_t)counts[e] : 0;
 }
 
-__global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int stretches) {
-  __shared__ int part_all[kThreads], part_before[kThreads];
+__global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int units) {
+  __shared__ int part_all[kThreads][4], part_before[kThreads][4];
   __shared__ GroupLds s;
-  // a power of two of experts side by side, the stretches shared out between
-  // the parts of the workgroup that this leaves
-  const int tid = threadIdx.x, wide = 1 << (32 - __builtin_clz(max(a.E, 2) - 1));
-  const int part = tid / wide, parts = kThreads / wide, e = tid - part * wide;
-  int all = 0, before = 0;
-  if (e < a.E) {
+  // four experts a thread, a power of two of threads side by side, the units
+  // shared out between the parts of the workgroup that this leaves
+  const int tid = threadIdx.x, E4 = (a.E + 3) >> 2, wide = 1 << (32 - __builtin_clz(max(E4, 2) - 1));
+  const int part = tid / wide, parts = kThreads / wide, e4 = tid - part * wide;
+  const int u0 = kUnits * blockIdx.x;
+  int n[4] = {}, b[4] = {};
+  if (e4 < E4) {
 #pragma unroll 8
-    for (int i = part; i < stretches; i += parts) {
-      const int c = a.hist[(int64_t)i * a.E + e];
-      all += c;
-      before += i < (int)blockIdx.x ? c : 0;
+    for (int i = part; i < units; i += parts) {
+      const u32x2 c = *reinterpret_cast<const u32x2*>(a.hist + ((int64_t)i * E4 + e4) * 4);
+      const int v[4] = {(int)(c[0] & 0xFFFFu), (int)(c[0] >> 16), (int)(c[1] & 0xFFFFu), (int)(c[1] >> 16)};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        n[q] += v[q];
+        b[q] += i < u0 ? v[q] : 0;
+      }
     }
   }
-  part_all[tid] = all;
-  part_before[tid] = before;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    part_all[tid][q] = n[q];
+    part_before[tid][q] = b[q];
+  }
   __syncthreads();
-  all = before = 0;
+  int all = 0, before = 0;
   if (tid < a.E)
     for (int p = 0; p < parts; ++p) {
-      all += part_all[p * wide + tid];
-      before += part_before[p * wide + tid];
+      all += part_all[p * wide + (tid >> 2)][tid & 3];
+      before += part_before[p * wide + (tid >> 2)][tid & 3];
     }
-  const int t0 = blockIdx.x * a.tokens;
-  group_stretch(a, t0, min(a.T, t0 + a.tokens), all, before, blockIdx.x == 0, s);
+  const int64_t t0 = (int64_t)u0 * a.tokens, t1 = t0 + (int64_t)kUnits * a.tokens;
+  group_tokens(a, (int)t0, (int)(t1 < a.T ? t1 : a.T), all, before, blockIdx.x == 0, s);
 }
 
 template <int V>
-void launch_route(const RouteArgs& a, int stretches, hipStream_t st) {
-  if (stretches <= 1) {
+void launch_route(const RouteArgs& a, hipStream_t st) {
+  if ((int64_t)a.T * a.k <= kThreads) {
     hipLaunchKernelGGL(route_one_kernel<V>, dim3(1), dim3(kThreads), 0, st, a);
-  } else {
-    hipLaunchKernelGGL(route_kernel<V>, dim3((unsigned)stretches), dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL(group_kernel, dim3((unsigned)stretches), dim3(kThreads), 0, st, a, stretches);
+    return;
   }
+  const int units = (a.T + a.tokens - 1) / a.tokens;
+  hipLaunchKernelGGL(route_kernel<V>, dim3((unsigned)units), dim3(kUnitThreads), 0, st, a);
+  hipLaunchKernelGGL(group_kernel, dim3((unsigned)((units + kUnits - 1) / kUnits)), dim3(kThreads), 0, st, a, units);
 }
 
 }  // namespace
 
 size_t route_hist_bytes(int T, int E, int k) {
-  const int tokens = stretch_tokens(T, k);
-  return (size_t)((T + tokens - 1) / tokens) * E * sizeof(int32_t);
+  // what any smaller number of tokens may need too: up to 256 units of the least
+  // size, more only of the largest
+  const int64_t least = kUnitThreads / k, most = 65535 / k;
+  const int64_t small = (T + least - 1) / least, large = (T + most - 1) / most;
+  const int64_t units = small < 256 ? small : large > 256 ? large : 256;
+  return (size_t)units * ((E + 3) / 4 * 4) * sizeof(uint16_t);
 }
 
 void launch_moe_route(const RouteLaunch& L, hipStream_t st) {
@@ -308,7 +324,7 @@ void launch_moe_route(const RouteLaunch& L, hipStream_t st) {
   a.E = L.E;
   a.k = L.k;
   a.renormalize = L.renormalize;
-  a.tokens = stretch_tokens(L.T, L.k);
+  a.tokens = unit_tokens(L.T, L.k);
   a.experts = L.experts;
   a.weights = L.weights;
   a.offsets = L.offsets;
@@ -316,14 +332,13 @@ void launch_moe_route(const RouteLaunch& L, hipStream_t st) {
   a.pos = L.pos;
   a.hist = L.hist;
   a.lines = (reinterpret_cast<uintptr_t>(L.logits) & 15) == 0 && L.ldl % 8 == 0;
-  const int stretches = (L.T + a.tokens - 1) / a.tokens;
   const int v = L.logits ? (L.E + 15) / 16 : 1;  // scores of a lane
-  if (v <= 1) launch_route<1>(a, stretches, st);
-  else if (v <= 2) launch_route<2>(a, stretches, st);
-  else if (v <= 4) launch_route<4>(a, stretches, st);
-  else if (v <= 8) launch_route<8>(a, stretches, st);
-  else if (v <= 16) launch_route<16>(a, stretches, st);
-  else launch_route<32>(a, stretches, st);
+  if (v <= 1) launch_route<1>(a, st);
+  else if (v <= 2) launch_route<2>(a, st);
+  else if (v <= 4) launch_route<4>(a, st);
+  else if (v <= 8) launch_route<8>(a, st);
+  else if (v <= 16) launch_route<16>(a, st);
+  else launch_route<32>(a, st);
 }
 
 }  // namespace ss

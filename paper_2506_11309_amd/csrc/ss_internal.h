@@ -205,7 +205,7 @@ struct RouteLaunch {
   int32_t* experts;
   float* weights;
   int32_t *offsets, *rows, *pos;
-  int32_t* hist;  // route_hist_bytes
+  uint16_t* hist;  // route_hist_bytes
 };
 size_t route_hist_bytes(int T, int E, int k);
 void launch_moe_route(const RouteLaunch& L, hipStream_t st);

@@ -377,7 +377,7 @@ int run_route(ss::RouteLaunch& L, const swiftspec_moe_groups* g, void* ws, size_
   L.offsets = g->offsets;
   L.rows = g->rows;
   L.pos = g->pos;
-  L.hist = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + kHeader);
+  L.hist = reinterpret_cast<uint16_t*>(static_cast<char*>(ws) + kHeader);
   ss::launch_moe_route(L, st);
   return check_launch();
 }

@@ -28,7 +28,8 @@ def same_groups(g, want):
 
 
 ROUTES = [(1, 1, 1), (1, 8, 2), (1, 512, 16), (7, 3, 3), (63, 64, 8), (64, 65, 6), (65, 128, 1), (129, 130, 5),
-          (1000, 256, 8), (1025, 2, 1), (3000, 60, 7), (20000, 512, 4)]
+          (1000, 256, 8), (1025, 2, 1), (3000, 60, 7), (20000, 512, 4),
+          (70001, 13, 3)]
 
 
 @pytest.mark.parametrize("T,E,k", ROUTES)
@@ -66,7 +67,7 @@ def test_route_scores_at_their_limits():
         same_groups(g, ref.group(want_e, 70))
 
 
-@pytest.mark.parametrize("T,E,k", [(1, 4, 2), (50, 7, 3), (300, 512, 16), (5000, 9, 2)])
+@pytest.mark.parametrize("T,E,k", [(1, 4, 2), (50, 7, 3), (300, 512, 16), (5000, 9, 2), (17000000, 5, 1)])
 def test_group_of_given_experts(T, E, k):
     rng = np.random.default_rng(T)
     e = rng.integers(-2, E + 2, (T, k)).astype(np.int32)  # some without an expert
