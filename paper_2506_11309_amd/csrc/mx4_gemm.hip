@@ -20,12 +20,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kOutside = 0x80000000u;  // a buffer offset past every operand (they stay below 2 GiB or 4 GiB - 2 GiB)
 
-// c += W (16 columns x 128) . A (16 rows x 128); byte J of each scale word
-template <int J>
+// c += W (16 columns x 128) . A (16 rows x 128); byte J of the weights' scale word, JA of the rows'
+template <int J, int JA = J>
 __device__ __forceinline__ f32x4 mfma_mx4(const u32x4& w, uint32_t ws, const u32x4& a, uint32_t as, const f32x4& c) {
   const i32x8 w8 = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
   const i32x8 a8 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, J, (int)ws, J, (int)as);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, J, (int)ws, JA, (int)as);
 }
 
 // c += W (32 columns x 64) . A (32 rows x 64): lane h*32 + i holds block h of row i
@@ -54,6 +54,12 @@ struct Mx4Args {
   float* part;
   void* ws;
   int col_blocks;
+  // rows quantised by the product itself
+  const uint16_t* x;
+  uint32_t x_row, x_bytes;  // bytes from row to row, of all rows
+  int blocks;               // blocks of 32 columns of a row
+  const int32_t* offsets;
+  int E;
 };
 
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
@@ -67,6 +73,43 @@ __device__ __forceinline__ RowBlock row_block(const Mx4Args& a, int rb, int TM) 
   const int32_t* p = a.map + 4 * ((int64_t)rb + 1);
   return RowBlock{__builtin_amdgcn_readfirstlane(p[0]), __builtin_amdgcn_readfirstlane(p[1]),
                   __builtin_amdgcn_readfirstlane(p[2])};
+}
+
+// The same from the offsets (as Mx4Map describes it), by each wave for itself.
+__device__ __forceinline__ RowBlock find_block(const Mx4Args& a, int rb, int TM, bool first) {
+  if (!a.offsets) return RowBlock{0, rb * TM, min(TM, a.M - rb * TM)};
+  const int lane = lane_id();
+  RowBlock r{0, 0, 0};
+  bool bad = false;
+  int base = 0;
+  for (int e0 = 0; e0 < a.E; e0 += kWave) {
+    const int e = e0 + lane;
+    const int lo = e < a.E ? a.offsets[e] : 0, hi = e < a.E ? a.offsets[e + 1] : 0;
+    bad = bad || __any(lo < 0 || hi < lo || hi > a.M || (e == 0 && lo != 0));
+    const int n = bad ? 0 : (hi - lo + TM - 1) / TM;
+    int s = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(s, d, kWave);
+      if (lane >= d) s += o;
+    }
+    const uint64_t past = __ballot(base + s > rb);
+    if (past && r.n == 0) {
+      const int l = __builtin_ctzll(past);
+      r.e = e0 + l;
+      r.m0 = __shfl(lo + (rb - (base + s - n)) * TM, l, kWave);
+      r.n = min(TM, __shfl(hi, l, kWave) - r.m0);
+    }
+    base += __shfl(s, 63, kWave);
+  }
+  if (first && lane == 0) {  // one wave of the launch
+    if (bad) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+    int32_t* map = const_cast<int32_t*>(a.map);
+    map[0] = !bad;
+    map[1] = bad ? 0 : a.offsets[a.E];
+  }
+  if (bad) r.n = 0;
+  return RowBlock{__builtin_amdgcn_readfirstlane(r.e), __builtin_amdgcn_readfirstlane(r.m0), __builtin_amdgcn_readfirstlane(r.n)};
 }
 
 // Workgroup -> row and column block of a tile.  Tiles are taken in bands of 4 row
@@ -129,7 +172,10 @@ __device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f3
 // added in wave order.  Nothing is staged: a weight block is one coalesced
 // kilobyte, read once from memory by the wave that multiplies it, U groups of
 // each tile at a time and the next U on their way.
-template <int W, int MT, int NT, int U, Mx4Epilogue EPI>
+// RAW: a single launch for very few rows, which each wave quantises itself as it
+// reads them (16 instructions a kilobyte of weights and tile); the block's expert
+// is found from the offsets.
+template <int W, int MT, int NT, int U, bool RAW, Mx4Epilogue EPI>
 __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   constexpr bool SW = EPI == MX4_SWIGLU;
   constexpr int kC = SW ? NT / 2 : NT;
@@ -138,7 +184,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int rb = blockIdx.x / a.col_blocks, cb = blockIdx.x - rb * a.col_blocks;
-  const RowBlock b = row_block(a, rb, 16 * MT);
+  const RowBlock b = RAW ? find_block(a, rb, 16 * MT, blockIdx.x == 0 && wave == 0) : row_block(a, rb, 16 * MT);
   if (b.n <= 0) return;
   const int t0 = cb * kC;
   const int C = (a.G + U - 1) / U;  // chunks of U groups
@@ -147,17 +193,21 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   const auto rw0 = buffer_rsrc(a.w0 + b.e * a.w_stride, wb), rs0 = buffer_rsrc(a.s0 + b.e * a.s_stride, sb);
   const auto rw1 = buffer_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
   const auto rs1 = buffer_rsrc((SW ? a.s1 : a.s0) + b.e * a.s_stride, sb);
-  const auto ra = buffer_rsrc(a.a, a.a_bytes), ras = buffer_rsrc(a.as, a.as_bytes);
+  const auto ra = RAW ? buffer_rsrc(a.x, a.x_bytes) : buffer_rsrc(a.a, a.a_bytes);
+  const auto ras = buffer_rsrc(a.as, RAW ? 0u : a.as_bytes);
   uint32_t va[MT], vs[MT];
   bool live[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int m = 16 * mt + r16;
-    live[mt] = m < b.n;
-    const int src = live[mt] ? source_row(a, b.m0 + m) : -1;
+    const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
     live[mt] = src >= 0;
-    va[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)kq * 16u : kOutside;
-    vs[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
+    if constexpr (RAW) {
+      va[mt] = live[mt] ? (uint32_t)src * a.x_row + (uint32_t)kq * 64u : kOutside;
+    } else {
+      va[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)kq * 16u : kOutside;
+      vs[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
+    }
   }
   f32x4 acc[MT][NT];
 #pragma unroll
@@ -165,7 +215,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
   struct Stage {
-    u32x4 w[U][NT], x[U][MT];
+    u32x4 w[U][NT], x[U][MT][RAW ? 4 : 1];
     uint32_t ws[NT], xs[MT];
   };
   auto load = [&](Stage& s, int c) {
@@ -186,26 +236,51 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t g = (uint32_t)(c * U + u);
-        s.x[u][mt] = buffer_load_x4(ra, g < (uint32_t)a.G ? va[mt] : kOutside, g * 64u);
+        if constexpr (RAW) {
+          const uint32_t v = (int)(4 * g) + kq < a.blocks ? va[mt] : kOutside;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) s.x[u][mt][q] = buffer_load_x4(ra, v, g * 256u + 16u * q);
+        } else {
+          s.x[u][mt][0] = buffer_load_x4(ra, g < (uint32_t)a.G ? va[mt] : kOutside, g * 64u);
+        }
       }
-      s.xs[mt] = buffer_load_x1(ras, vs[mt], (uint32_t)(c * U / 4) * 16u);
+      if constexpr (!RAW) s.xs[mt] = buffer_load_x1(ras, vs[mt], (uint32_t)(c * U / 4) * 16u);
+    }
+  };
+  // the rows' operand of group u and its scale (RAW: in byte 0)
+  auto operand = [&](const Stage& s, int u, int mt, uint32_t& scale) {
+    if constexpr (RAW) {
+      const u32x4* v = s.x[u][mt];
+      const uint32_t m = max(max(mx4_magnitude(v[0]), mx4_magnitude(v[1])), max(mx4_magnitude(v[2]), mx4_magnitude(v[3])));
+      scale = mx4_scale_of(m);
+      return u32x4{mx4_codes(v[0], scale), mx4_codes(v[1], scale), mx4_codes(v[2], scale), mx4_codes(v[3], scale)};
+    } else {
+      scale = s.xs[mt];
+      return s.x[u][mt][0];
     }
   };
   auto multiply = [&](Stage& s, int c) {
     const int sh = U == 4 ? 0 : 8 * ((c * U) & 3);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) s.ws[nt] >>= sh;
+    if constexpr (!RAW) {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) s.xs[mt] >>= sh;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+      for (int mt = 0; mt < MT; ++mt) s.xs[mt] >>= sh;
+    }
+    auto group = [&](auto uc) {
+      constexpr int u = decltype(uc)::value;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        acc[mt][nt] = mfma_mx4<0>(s.w[0][nt], s.ws[nt], s.x[0][mt], s.xs[mt], acc[mt][nt]);
-        if constexpr (U > 1) acc[mt][nt] = mfma_mx4<1>(s.w[1][nt], s.ws[nt], s.x[1][mt], s.xs[mt], acc[mt][nt]);
-        if constexpr (U > 2) acc[mt][nt] = mfma_mx4<2>(s.w[2][nt], s.ws[nt], s.x[2][mt], s.xs[mt], acc[mt][nt]);
-        if constexpr (U > 3) acc[mt][nt] = mfma_mx4<3>(s.w[3][nt], s.ws[nt], s.x[3][mt], s.xs[mt], acc[mt][nt]);
+        uint32_t xs;
+        const u32x4 x = operand(s, u, mt, xs);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          acc[mt][nt] = mfma_mx4<u, RAW ? 0 : u>(s.w[u][nt], s.ws[nt], x, xs, acc[mt][nt]);
       }
+    };
+    group(std::integral_constant<int, 0>{});
+    group(std::integral_constant<int, 1>{});
+    static_assert(U == 2, "groups of a chunk");
   };
   Stage s[2];
   if (c0 < c1) load(s[0], c0);
@@ -307,13 +382,13 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G4 * 16) + (uint32_t)kq * 4u : kOutside;
   }
   for (int m = threadIdx.x; m < TM; m += 256) live[m] = m < b.n && (!a.rows || (uint32_t)a.rows[b.m0 + m] < (uint32_t)a.M);
-  uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, its gate tiles, then its up tiles
+  uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, for SwiGLU a gate tile and its up tile in turn
 #pragma unroll
   for (int i = 0; i < kW; ++i) {
     const int w = wave * kW + i, own = w / NTW, j = w - own * NTW;
-    wt[i] = (uint32_t)min(t0 + own * kCW + (SW ? j % kCW : j), a.Nt - 1);
+    wt[i] = (uint32_t)min(t0 + own * kCW + (SW ? j / 2 : j), a.Nt - 1);
   }
-  auto is_up = [&](int i) { return SW && (wave * kW + i) % NTW >= kCW; };
+  auto is_up = [&](int i) { return SW && ((wave * kW + i) & 1); };
   const uint32_t ax_lds = lds_address(&ax[0][0]), wx_lds = lds_address(&wx[0][0][0]), sc_lds = lds_address(&sc[0][0]);
   // load i of the rows' groups 2 p and 2 p + 1, of the weights' group g, of the
   // scales of groups 4 c .. 4 c + 3; nothing past the last group
@@ -354,7 +429,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     else s.w[i - MTW] = sc[AT + wn * NTW + ((i - MTW) & ~1) + second][(i & 1) * 32 + piece];
   };
   constexpr int kMP = MTW / 2, kNP = NTW / 2;
-  static_assert(MTW % 2 == 0 && kCW % 2 == 0, "blocks go two by two");
+  static_assert(MTW % 2 == 0 && NTW % 2 == 0, "blocks go two by two");
   f32x16 acc[kMP][kNP];
 #pragma unroll
   for (int i = 0; i < kMP; ++i)
@@ -423,9 +498,12 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   }
   vm_lds_barrier<0>();  // loads past the last group still write LDS, other waves read theirs
   // Register 4 q + c of a pair of blocks holds column 8 q + 4 (lane / 32) + c of
-  // row lane % 32.  Through LDS the rows come out as whole 128-byte lines: 64
-  // fp16 columns, or 32 fp32 ones (results that a residual or another sum awaits).
+  // row lane % 32 (SwiGLU: gate columns for q < 2, their up columns after them).
+  // Through LDS the rows come out as whole 128-byte lines: 64 fp16 columns, or 32
+  // fp32 ones (results that a residual or another sum awaits).
   constexpr bool wide = EPI == MX4_ROWS || EPI == MX4_RESIDUAL;
+  constexpr int kPC = SW ? 16 : 32;             // columns of a pair
+  constexpr int kPL = wide ? 1 : 64 / kPC;      // pairs of a line
   uint8_t* my = reinterpret_cast<uint8_t*>(&wx[0][0][0]) + wave * (32 * kTurnRow);
   static_assert(sizeof(wx) >= 4 * 32 * kTurnRow, "the lines' room");
   const int tr = lane >> 3, tc = lane & 7;  // row (of 8) and 16-byte piece of a line
@@ -433,22 +511,21 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   for (int i = 0; i < kMP; ++i) {
     const int ml = 16 * (wm * MTW + 2 * i);
 #pragma unroll
-    for (int j = 0; j < kCW / 2; ++j) {
-      const int n = 16 * (t0 + wn * kCW + 2 * j);
+    for (int j = 0; j < kNP; ++j) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < kPC / 8; ++q) {
         f32x4 v;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           v[c] = acc[i][j][4 * q + c];
-          if constexpr (SW) v[c] = silu(v[c]) * acc[i][j + kNP / 2][4 * q + c];
+          if constexpr (SW) v[c] = silu(v[c]) * acc[i][j][4 * (q + 2) + c];
         }
-        const int col = 8 * q + 4 * (lane >> 5);
+        const int col = kPC * (j % kPL) + 8 * q + 4 * (lane >> 5);
         if constexpr (wide) *reinterpret_cast<f32x4*>(my + r32 * kTurnRow + 4 * col) = v;
-        else *reinterpret_cast<u32x2*>(my + r32 * kTurnRow + 2 * (32 * (j & 1) + col)) = pack4(v);
+        else *reinterpret_cast<u32x2*>(my + r32 * kTurnRow + 2 * col) = pack4(v);
       }
-      if (!wide && (j & 1) == 0 && j + 1 < kCW / 2) continue;  // the line's other half
-      const int first = wide ? n : n - 32 * (j & 1);
+      if ((j + 1) % kPL != 0 && j + 1 < kNP) continue;  // more of the line to come
+      const int n = 16 * (t0 + wn * kCW) + kPC * (j - j % kPL), filled = kPC * (j % kPL + 1);
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -456,8 +533,8 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(my + r * kTurnRow + 16 * tc);
         if (!live[ml + r]) continue;
         const int64_t m = b.m0 + ml + r;
-        const int col = first + (wide ? 4 : 8) * tc;
-        if (col >= a.N || (!wide && (j & 1) == 0 && tc >= 4)) continue;
+        const int in = (wide ? 4 : 8) * tc, col = n + in;
+        if (in >= filled || col >= a.N) continue;
         if constexpr (EPI == MX4_ROWS) {
           *reinterpret_cast<u32x4*>(a.part + m * a.N + col) = v;
         } else if constexpr (EPI == MX4_RESIDUAL) {
@@ -517,11 +594,11 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restric
   *reinterpret_cast<u32x2*>(y + t * ldy + n) = pack4(v);
 }
 
-template <int W, int MT, int NT, Mx4Epilogue EPI>
+template <int W, int MT, int NT, bool RAW, Mx4Epilogue EPI>
 void launch_stream(Mx4Args a, int blocks, hipStream_t st) {
   constexpr int kC = EPI == MX4_SWIGLU ? NT / 2 : NT;
   a.col_blocks = (a.Nt + kC - 1) / kC;
-  hipLaunchKernelGGL((mx4_stream_kernel<W, MT, NT, 2, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(64 * W), 0, st, a);
+  hipLaunchKernelGGL((mx4_stream_kernel<W, MT, NT, 2, RAW, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(64 * W), 0, st, a);
 }
 
 template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
@@ -535,11 +612,14 @@ void launch_tile(Mx4Args a, int blocks, hipStream_t st) {
 struct Plan {
   int form, tm;
 };
-enum { STREAM_1, STREAM_2, STREAM_4, TILE_64, TILE_128, TILE_256 };
-constexpr int kRowsOf[] = {16, 32, 64, 64, 128, 256};
+enum { STREAM_1, STREAM_2, STREAM_4, TILE_64, TILE_128, TILE_256, STREAM_RAW };
+constexpr int kRowsOf[] = {16, 32, 64, 64, 128, 256, 16};
 
 Plan plan_of(const Mx4Launch& L) {
   const int avg = L.offsets ? L.M / L.E : L.M;
+  // very few rows, which fit a 2 GiB buffer and which the output does not touch
+  const uint64_t x_bytes = ((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2;
+  if (L.a_rows <= (L.rows || !L.offsets ? 8 : 64) && L.M <= 64 && x_bytes < kOutside && !L.x_written) return Plan{STREAM_RAW, 16};
   const int form = avg <= 16 ? STREAM_1 : avg <= 32 ? STREAM_2 : avg <= 64 ? STREAM_4 : avg <= 256 ? TILE_128 : TILE_256;
   return Plan{form, kRowsOf[form]};
 }
@@ -547,10 +627,11 @@ Plan plan_of(const Mx4Launch& L) {
 template <Mx4Epilogue EPI>
 void launch_form(int form, const Mx4Args& a, int blocks, hipStream_t st) {
   switch (form) {
-    case STREAM_1: return launch_stream<8, 1, 2, EPI>(a, blocks, st);
-    case STREAM_2: return launch_stream<8, 2, 2, EPI>(a, blocks, st);
-    case STREAM_4: return launch_stream<8, 4, 2, EPI>(a, blocks, st);
-    case TILE_64: return launch_tile<1, 4, 4, 4, EPI>(a, blocks, st);
+    case STREAM_RAW: return launch_stream<8, 1, 2, true, EPI>(a, blocks, st);
+    case STREAM_1: return launch_stream<8, 1, 2, false, EPI>(a, blocks, st);
+    case STREAM_2: return launch_stream<8, 2, 2, false, EPI>(a, blocks, st);
+    case STREAM_4: return launch_stream<8, 4, 2, false, EPI>(a, blocks, st);
+    case TILE_64: return launch_tile<1, 4, 4, 2, EPI>(a, blocks, st);
     case TILE_128: return launch_tile<2, 2, 4, 4, EPI>(a, blocks, st);
     default: return launch_tile<2, 2, 8, 8, EPI>(a, blocks, st);
   }
@@ -568,7 +649,7 @@ void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   map.blocks = L.offsets ? mx4_row_blocks(L.M, L.E, p.tm) : (L.M + p.tm - 1) / p.tm;
   map.map = L.map;
   map.ws = L.ws;
-  launch_mx4_prepare(L.x, L.a_rows, L.K, L.ldx, L.a, L.a_scales, L.rows ? nullptr : L.offsets, map, st);
+  if (p.form != STREAM_RAW) launch_mx4_prepare(L.x, L.a_rows, L.K, L.ldx, L.a, L.a_scales, L.rows ? nullptr : L.offsets, map, st);
   Mx4Args a = {};
   const size_t wq = mx4_code_bytes(L.N, L.K), wsb = mx4_scale_bytes(L.N, L.K);
   a.w0 = static_cast<const uint8_t*>(L.w0);
@@ -595,6 +676,12 @@ void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   a.ldr = L.ldr;
   a.part = L.part;
   a.ws = L.ws;
+  a.x = L.x;
+  a.x_row = (uint32_t)(L.ldx * 2);
+  a.x_bytes = (uint32_t)(((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2);
+  a.blocks = L.K / 32;
+  a.offsets = L.offsets;
+  a.E = L.E;
   if (L.epi == MX4_SWIGLU) launch_form<MX4_SWIGLU>(p.form, a, map.blocks, st);
   else if (L.epi == MX4_ROWS) launch_form<MX4_ROWS>(p.form, a, map.blocks, st);
   else if (L.res) launch_form<MX4_RESIDUAL>(p.form, a, map.blocks, st);

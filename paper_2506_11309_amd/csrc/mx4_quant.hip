@@ -22,25 +22,11 @@ constexpr int kUnits = 4;  // 16-byte pieces of a thread
 // 8 fp16 values of one lane, the block's magnitude maximum over its 4 lanes ->
 // 8 codes and the scale byte
 __device__ __forceinline__ uint32_t quantize8(const u32x4& v, uint32_t& scale) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = v[i] & 0x7FFFu, hi = (v[i] >> 16) & 0x7FFFu;
-    m = max(m, max(lo, hi));
-  }
+  uint32_t m = mx4_magnitude(v);
   m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, true));  // lane ^ 1
   m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, true));  // lane ^ 2
-  const float a = h2f((uint16_t)m);
-  const uint32_t e = bitcast<uint32_t>(a) >> 23;  // every fp16 value is a normal fp32
-  scale = m >= 0x7C00u ? 255u : m == 0 ? 127u : e - 2;
-  if (m >= 0x7C00u) return 0;
-  const float unit = bitcast<float>(scale << 23);
-  uint32_t c = 0;
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, bitcast<half2v>(v[0]), unit, 0);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, bitcast<half2v>(v[1]), unit, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, bitcast<half2v>(v[2]), unit, 2);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, bitcast<half2v>(v[3]), unit, 3);
-  return c;
+  scale = mx4_scale_of(m);
+  return mx4_codes(v, scale);
 }
 
 // One workgroup writes the row blocks of a product (Mx4Map).

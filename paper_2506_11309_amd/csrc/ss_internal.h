@@ -176,6 +176,7 @@ struct Mx4Launch {
   int K, N, E;
   const uint16_t* x;        // activations [a_rows][ldx] fp16
   int64_t ldx, a_rows;
+  bool x_written;           // the output shares memory with x
   uint8_t* a;               // and room for their operand form
   uint8_t* a_scales;
   int M;                    // output rows: of the matrix, or the most that the experts share (T k)

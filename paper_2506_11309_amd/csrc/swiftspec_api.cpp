@@ -640,6 +640,7 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
   L.a = base + w.codes;
   L.a_scales = base + w.scales;
   L.a_rows = L.M = M;
+  L.x_written = M <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, W->K, y, ldy, W->N, M);  // more rows are quantised first anyway
   L.div = 1;
   L.y = y;
   L.ldy = ldy;
@@ -716,6 +717,7 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
   L.a = base + w.codes;
   L.a_scales = base + w.scales;
   L.a_rows = groups->T;
+  L.x_written = false;
   L.M = (int)pairs;
   L.offsets = groups->offsets;
   L.rows = groups->rows;
