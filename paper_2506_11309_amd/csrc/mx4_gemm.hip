@@ -54,6 +54,7 @@ struct Mx4Args {
   float* part;
   void* ws;
   int col_blocks;
+  int split;  // shares of K, each with its own part [M][N]
   // rows quantised by the product itself
   const uint16_t* x;
   uint32_t x_row, x_bytes;  // bytes from row to row, of all rows
@@ -334,6 +335,8 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 // g + 1 from LDS, so neither latency shows; one barrier a step.  Scale words
 // cover four groups: they are loaded in the first of four steps, when every
 // wave has the present ones in registers, and read in the last.
+// Where the tiles are too few for the chip, K is split between workgroups whose
+// parts another kernel adds in order.
 // The waits count this wave's loads in issue order.  Step g loads, in order,
 // the scales of the next four groups (g % 4 == 0), the activations of groups
 // g + 3 and g + 4 (g odd), the weights of group g + 4.
@@ -360,7 +363,9 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   const RowBlock b = row_block(a, rb, TM);
   if (b.n <= 0) return;
   const int t0 = cb * kC;
-  const int G = a.G, G4 = a.G4;
+  // this workgroup's share of K: whole scale words
+  const int first = blockIdx.y * a.G4 / a.split, G4 = (blockIdx.y + 1) * a.G4 / a.split - first;
+  const int G = min(a.G - 4 * first, 4 * G4);
   const uint32_t wb = (uint32_t)a.w_stride, sb = (uint32_t)a.s_stride;
   const i32x4 rw0 = raw_rsrc(a.w0 + b.e * a.w_stride, wb), rs0 = raw_rsrc(a.s0 + b.e * a.s_stride, sb);
   const i32x4 rw1 = raw_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
@@ -373,13 +378,13 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   for (int i = 0; i < kA; ++i) {
     const int m = 8 * (wave * kA + i) + (lane >> 3);
     const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
-    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
+    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
   }
 #pragma unroll
   for (int i = 0; i < AT / 4; ++i) {
     const int m = 16 * (wave * (AT / 4) + i) + r16;
     const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
-    vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(G4 * 16) + (uint32_t)kq * 4u : kOutside;
+    vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
   }
   for (int m = threadIdx.x; m < TM; m += 256) live[m] = m < b.n && (!a.rows || (uint32_t)a.rows[b.m0 + m] < (uint32_t)a.M);
   uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, for SwiGLU a gate tile and its up tile in turn
@@ -393,21 +398,21 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   // load i of the rows' groups 2 p and 2 p + 1, of the weights' group g, of the
   // scales of groups 4 c .. 4 c + 3; nothing past the last group
   auto load_rows = [&](int i, int p) {
-    buffer_load_lds16(ra, 2 * p < G ? va[i] : kOutside, (uint32_t)p * 128u,
+    buffer_load_lds16(ra, 2 * p < G ? va[i] : kOutside, (uint32_t)(p + 2 * first) * 128u,
                       ax_lds + (uint32_t)(p & 1) * (TM * 128u) + (uint32_t)(wave * kA + i) * 1024u);
   };
   auto load_weights = [&](int i, int g) {
     const bool in = g < G;
-    buffer_load_lds16(is_up(i) ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (wt[i] * G + g) * 1024u : 0u,
+    buffer_load_lds16(is_up(i) ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (wt[i] * a.G + g + 4 * first) * 1024u : 0u,
                       wx_lds + (uint32_t)(g & 3) * (WT * 1024u) + (uint32_t)(wave * kW + i) * 1024u);
   };
   auto load_scale = [&](int i, int c) {
     const bool in = c < G4;
     if (i < AT / 4)
-      buffer_load_lds4(ras, in ? vs[i] : kOutside, (uint32_t)c * 16u, sc_lds + (uint32_t)(wave * (AT / 4) + i) * 256u);
+      buffer_load_lds4(ras, in ? vs[i] : kOutside, (uint32_t)(c + first) * 16u, sc_lds + (uint32_t)(wave * (AT / 4) + i) * 256u);
     else
       buffer_load_lds4(is_up(i - AT / 4) ? rs1 : rs0, in ? (uint32_t)lane * 4u : kOutside,
-                       in ? (wt[i - AT / 4] * G4 + c) * 256u : 0u, sc_lds + (uint32_t)(AT + wave * kW + i - AT / 4) * 256u);
+                       in ? (wt[i - AT / 4] * a.G4 + c + first) * 256u : 0u, sc_lds + (uint32_t)(AT + wave * kW + i - AT / 4) * 256u);
   };
   // [2 p + h]: half h of the group (k blocks 2 h, 2 h + 1) of the blocks 2 p, 2 p + 1
   struct Ops {
@@ -536,7 +541,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
         const int in = (wide ? 4 : 8) * tc, col = n + in;
         if (in >= filled || col >= a.N) continue;
         if constexpr (EPI == MX4_ROWS) {
-          *reinterpret_cast<u32x4*>(a.part + m * a.N + col) = v;
+          *reinterpret_cast<u32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + col) = v;
         } else if constexpr (EPI == MX4_RESIDUAL) {
           f32x4 f = bitcast<f32x4>(v);
           add_residual(f, residual(a, m, col));
@@ -594,6 +599,24 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restric
   *reinterpret_cast<u32x2*>(y + t * ldy + n) = pack4(v);
 }
 
+// y = fp16(the sum of `split` parts [M][N] in order + residual); 4 columns a thread.
+__global__ __launch_bounds__(256) void mx4_sum_kernel(const float* __restrict__ part, int split, int M, int N, uint16_t* y, int64_t ldy,
+                                                      const uint16_t* res, int64_t ldr) {
+  const int per = N / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t m = i / per;
+  if (m >= M) return;
+  const int n = (int)(i - m * per) * 4;
+  const float* p = part + m * N + n;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  u32x2 r = {0u, 0u};
+  if (res) r = *reinterpret_cast<const u32x2*>(res + m * ldr + n);
+#pragma unroll 8
+  for (int s = 0; s < split; ++s) v += *reinterpret_cast<const f32x4*>(p + (int64_t)s * M * N);
+  add_residual(v, r);
+  *reinterpret_cast<u32x2*>(y + m * ldy + n) = pack4(v);
+}
+
 template <int W, int MT, int NT, bool RAW, Mx4Epilogue EPI>
 void launch_stream(Mx4Args a, int blocks, hipStream_t st) {
   constexpr int kC = EPI == MX4_SWIGLU ? NT / 2 : NT;
@@ -605,42 +628,88 @@ template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
 void launch_tile(Mx4Args a, int blocks, hipStream_t st) {
   constexpr int kC = EPI == MX4_SWIGLU ? WN * NTW / 2 : WN * NTW;
   a.col_blocks = (a.Nt + kC - 1) / kC;
-  hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)blocks * a.col_blocks, a.split), dim3(256), 0, st, a);
 }
 
-// The form of a product and the rows of its row blocks.
-struct Plan {
-  int form, tm;
-};
-enum { STREAM_1, STREAM_2, STREAM_4, TILE_64, TILE_128, TILE_256, STREAM_RAW };
-constexpr int kRowsOf[] = {16, 32, 64, 64, 128, 256, 16};
+enum Form { STREAM_RAW, STREAM_1, STREAM_2, TILE_64, TILE_128, TILE_256 };
+constexpr int kRowsOf[] = {16, 16, 32, 64, 128, 256};
+constexpr int kColumnsOf[] = {32, 32, 32, 128, 128, 256};
 
-Plan plan_of(const Mx4Launch& L) {
-  const int avg = L.offsets ? L.M / L.E : L.M;
-  // very few rows, which fit a 2 GiB buffer and which the output does not touch
-  const uint64_t x_bytes = ((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2;
-  if (L.a_rows <= (L.rows || !L.offsets ? 8 : 64) && L.M <= 64 && x_bytes < kOutside && !L.x_written) return Plan{STREAM_RAW, 16};
-  const int form = avg <= 16 ? STREAM_1 : avg <= 32 ? STREAM_2 : avg <= 64 ? STREAM_4 : avg <= 256 ? TILE_128 : TILE_256;
-  return Plan{form, kRowsOf[form]};
+// The form of a product, the rows of its row blocks and the shares of K.
+struct Plan {
+  Form form;
+  int tm, split;
+};
+
+// Every line was drawn on products whose weights come from HBM (copies rotated
+// through more than the Infinity Cache), preparation included; the figures are
+// microseconds of the two sides.
+Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
+  const int G4 = (mx4_groups(K) + 3) / 4;
+  const int64_t weights = (int64_t)(E < M ? E : M) * K * N / 2 * (swiglu ? 2 : 1);  // bytes that are read, at most
+  auto plan = [](Form f, int split = 1) { return Plan{f, kRowsOf[f], split}; };
+  // One launch, but more registers and work in it: 8 rows of 8192 x 8192 12.4
+  // against 13.1, 1 row 10.8 against 11.9; of 8192 x 28672 (112 MB) 37.0 against 26.9.
+  if (raw && M <= 8 && weights <= (64 << 20)) return plan(STREAM_RAW);
+  if (grouped) {
+    const int64_t avg = M / E;
+    // Rows per expert: at 2 the stream is faster (8 experts 4096 x 14336: 56.6
+    // against 69.8), at 4 they meet, at 8 the tiles are (98.7 against 89.1); over a
+    // short K, where its workgroups are brief, from 1 (128 experts 1024 x 512: 18.2
+    // against 15.8).
+    if (M < (K <= 1024 ? 1 : 4) * (int64_t)E) return plan(STREAM_1);
+    // 64 rows: 64 against 128 rows a tile 43.9 and 47.3 (64 experts 2048 x 1024);
+    // 128 rows: 60.0 and 57.5.  256 against 128 rows a tile: at 256 rows 91.5 and
+    // 78.8, at 512 127.8 and 142.1; over a long K at 256 rows 118 and 139.
+    return plan(avg < 96 ? TILE_64 : avg < (K >= 8192 ? 192 : 320) ? TILE_128 : TILE_256);
+  }
+  if (M <= 16) return plan(STREAM_1);
+  auto tiles = [&](Form f) { return (int64_t)((M + kRowsOf[f] - 1) / kRowsOf[f]) * ((N + kColumnsOf[f] - 1) / kColumnsOf[f]); };
+  // shares of K that bring a form's tiles to one for each compute unit, each of at
+  // least `least` scale words (four groups each)
+  auto split_of = [&](Form f, int least) {
+    const int64_t want = 256 / tiles(f), most = G4 / least;
+    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+  };
+  // Few rows or little to read: 128 rows of 4096 x 4096 14.3 against 14.8, 32 of
+  // 8192 x 8192 15.3 against 21; but 28672 x 8192 39.2 against 31.6, 8192 x 28672
+  // 38.5 against 35.
+  if (M <= 128 && (int64_t)K * N <= (1 << 24)) return plan(STREAM_2);
+  if (M <= 32 && K < 16384 && N < 24576) return plan(STREAM_2);
+  // 64-row tiles as long as they are at most one for each compute unit (256 rows of
+  // 8192 x 8192 26.5 against 32.1; of 4096 x 4096 16.0 against 17.8), over a long K
+  // only few of them (14336 x 4096: 128 rows 22.3 against 23.3, 256 rows 30.7
+  // against 26.9).
+  if (M <= 64 || (M <= 512 && tiles(TILE_64) <= (K <= 8192 ? 256 : 64))) return plan(TILE_64, split_of(TILE_64, 4));
+  // 256-row tiles where they nearly fill the chip (384 rows of 8192 x 28672, 224
+  // tiles: 66 against 75; 192 rows, 112 tiles: 55 against 51), over a long K with
+  // two shares or more (28672 x 8192: 1024 rows 141 against 158).
+  const int64_t big = tiles(TILE_256);
+  if (M > 192 && (big >= 160 || (K >= 14336 && big >= 96) || (K >= 16384 && big >= 64)))
+    return plan(TILE_256, K >= 14336 ? split_of(TILE_256, 14) : 1);
+  return plan(TILE_128, split_of(TILE_128, 4));
 }
 
 template <Mx4Epilogue EPI>
-void launch_form(int form, const Mx4Args& a, int blocks, hipStream_t st) {
-  switch (form) {
+void launch_form(const Plan& p, const Mx4Args& a, int blocks, hipStream_t st) {
+  switch (p.form) {
     case STREAM_RAW: return launch_stream<8, 1, 2, true, EPI>(a, blocks, st);
     case STREAM_1: return launch_stream<8, 1, 2, false, EPI>(a, blocks, st);
-    case STREAM_2: return launch_stream<8, 2, 2, false, EPI>(a, blocks, st);
-    case STREAM_4: return launch_stream<8, 4, 2, false, EPI>(a, blocks, st);
+    case STREAM_2:
+      if constexpr (EPI == MX4_PLAIN || EPI == MX4_RESIDUAL) launch_stream<8, 2, 2, false, EPI>(a, blocks, st);
+      return;
     case TILE_64: return launch_tile<1, 4, 4, 2, EPI>(a, blocks, st);
     case TILE_128: return launch_tile<2, 2, 4, 4, EPI>(a, blocks, st);
-    default: return launch_tile<2, 2, 8, 8, EPI>(a, blocks, st);
+    case TILE_256: return launch_tile<2, 2, 8, 8, EPI>(a, blocks, st);
   }
 }
 
 }  // namespace
 
 void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
-  const Plan p = plan_of(L);
+  // rows that the product may read itself: within a 2 GiB buffer, not overwritten
+  const uint64_t x_bytes = ((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2;
+  const Plan p = plan_of(L.M, L.E, L.K, L.N, L.epi == MX4_SWIGLU, L.offsets, x_bytes < kOutside && !L.x_written);
   Mx4Map map = {};
   map.offsets = L.offsets;
   map.E = L.E;
@@ -678,14 +747,40 @@ void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   a.ws = L.ws;
   a.x = L.x;
   a.x_row = (uint32_t)(L.ldx * 2);
-  a.x_bytes = (uint32_t)(((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2);
+  a.x_bytes = (uint32_t)x_bytes;
+  a.split = p.split;
   a.blocks = L.K / 32;
   a.offsets = L.offsets;
   a.E = L.E;
-  if (L.epi == MX4_SWIGLU) launch_form<MX4_SWIGLU>(p.form, a, map.blocks, st);
-  else if (L.epi == MX4_ROWS) launch_form<MX4_ROWS>(p.form, a, map.blocks, st);
-  else if (L.res) launch_form<MX4_RESIDUAL>(p.form, a, map.blocks, st);
-  else launch_form<MX4_PLAIN>(p.form, a, map.blocks, st);
+  if (L.epi == MX4_SWIGLU) {
+    launch_form<MX4_SWIGLU>(p, a, map.blocks, st);
+  } else if (L.epi == MX4_ROWS) {
+    launch_form<MX4_ROWS>(p, a, map.blocks, st);
+  } else if (p.split > 1) {
+    launch_form<MX4_ROWS>(p, a, map.blocks, st);
+    hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)L.M * (L.N / 4) + 255) / 256)), dim3(256), 0, st, L.part, p.split,
+                       L.M, L.N, L.y, L.ldy, L.res, L.ldr);
+  } else if (L.res) {
+    launch_form<MX4_RESIDUAL>(p, a, map.blocks, st);
+  } else {
+    launch_form<MX4_PLAIN>(p, a, map.blocks, st);
+  }
+}
+
+size_t mx4_part_bytes(int M, int K, int N) {
+  const Plan p = plan_of(M, 1, K, N, false, false, false);
+  return p.split > 1 ? (size_t)p.split * M * N * sizeof(float) : 0;
+}
+
+size_t mx4_part_bytes_most(int M, int K, int N) {
+  // at most 256 tiles' worth of parts, and no more shares than plan_of allows
+  const int64_t G4 = (mx4_groups(K) + 3) / 4;
+  auto most = [&](Form f, int64_t split) {
+    const int64_t all = 256ll * kRowsOf[f] * kColumnsOf[f], mine = split * M * N;
+    return split > 1 ? (size_t)(all < mine ? all : mine) * sizeof(float) : 0;
+  };
+  const size_t a = most(TILE_128, G4 / 4), b = K >= 14336 ? most(TILE_256, G4 / 14) : 0;
+  return a > b ? a : b;
 }
 
 void launch_moe_combine(const float* part, int T, int k, int N, const int32_t* pos, const int32_t* map,

@@ -189,9 +189,13 @@ struct Mx4Launch {
   int64_t ldy;
   const uint16_t* res;      // residual (PLAIN)
   int64_t ldr;
-  float* part;              // fp32 output [M][N] (ROWS)
+  float* part;              // fp32 output [M][N] (ROWS), or room for the parts of a split K
   void* ws;                 // error word
 };
+// bytes of the parts of one matrix's product whose K is split: of M rows, and the
+// most of up to M rows
+size_t mx4_part_bytes(int M, int K, int N);
+size_t mx4_part_bytes_most(int M, int K, int N);
 // quantises the activations, then multiplies
 void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st);
 // y[t] = fp16(res[t] + sum over j < k with pos[t][j] >= 0 of weights[t][j] part[pos[t][j]]);

@@ -339,11 +339,11 @@ inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3
 bool mx4_rows_fit(int64_t M, int K) { return ss::mx4_code_bytes(M, K) < 0x80000000ull; }
 
 // Workspace of a product: the header, the activations in operand form, the map
-// of row blocks (experts), the experts' rows of the down product.
+// of row blocks (experts; E = 0: none), fp32 results that another kernel adds.
 struct Mx4Ws {
   size_t codes, scales, map, part, total;
 };
-Mx4Ws mx4_ws(int64_t a_rows, int64_t M, int E, int K, int N, bool part) {
+Mx4Ws mx4_ws(int64_t a_rows, int64_t M, int E, int K, size_t part) {
   Mx4Ws w;
   size_t off = kHeader;
   auto take = [&](size_t bytes) {
@@ -354,7 +354,7 @@ Mx4Ws mx4_ws(int64_t a_rows, int64_t M, int E, int K, int N, bool part) {
   w.codes = take(ss::mx4_code_bytes(a_rows, K));
   w.scales = take(ss::mx4_scale_bytes(a_rows, K));
   w.map = take(E ? ss::mx4_map_bytes((int)M, E) : 0);
-  w.part = take(part ? (size_t)M * N * sizeof(float) : 0);
+  w.part = take(part);
   w.total = off;
   return w;
 }
@@ -611,7 +611,7 @@ int swiftspec_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_
 
 size_t swiftspec_mx4_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N) {
   if (M < 1 || K < 1 || N < 1) return kHeader;
-  return mx4_ws(M, M, 0, K, N, false).total;
+  return mx4_ws(M, M, 0, K, ss::mx4_part_bytes_most(M, K, N)).total;
 }
 
 int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int32_t ldx, uint16_t* y, int32_t ldy,
@@ -625,7 +625,7 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
   if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
   if (M == 0) return SWIFTSPEC_OK;
   if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
-  const Mx4Ws w = mx4_ws(M, M, 0, W->K, W->N, false);
+  const Mx4Ws w = mx4_ws(M, M, 0, W->K, ss::mx4_part_bytes(M, W->K, W->N));
   if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   uint8_t* base = static_cast<uint8_t*>(ws);
   hipStream_t st = S(stream);
@@ -646,6 +646,7 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
   L.ldy = ldy;
   L.res = residual;
   L.ldr = ldr;
+  L.part = reinterpret_cast<float*>(base + w.part);
   L.ws = ws;
   ss::launch_mx4_gemm(L, st);
   return check_launch();
@@ -685,7 +686,7 @@ int swiftspec_moe_group(const int32_t* d_experts, const swiftspec_moe_groups* gr
 
 size_t swiftspec_moe_mx4_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
   if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1) return kHeader;
-  return mx4_ws(T, (int64_t)T * k, E, K, N, false).total;
+  return mx4_ws(T, (int64_t)T * k, E, K, 0).total;
 }
 
 int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, const uint16_t* x, int32_t ldx,
@@ -701,7 +702,7 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
   if (!aligned16(x) || ldx % 8 || !aligned8(h) || ldh % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
   if (groups->T == 0) return SWIFTSPEC_OK;
   const int64_t pairs = (int64_t)groups->T * groups->k;
-  const Mx4Ws w = mx4_ws(groups->T, pairs, Wg->E, Wg->K, Wg->N, false);
+  const Mx4Ws w = mx4_ws(groups->T, pairs, Wg->E, Wg->K, 0);
   if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   uint8_t* base = static_cast<uint8_t*>(ws);
   hipStream_t st = S(stream);
@@ -733,7 +734,7 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
 size_t swiftspec_moe_mx4_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
   if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1) return kHeader;
   const int64_t pairs = (int64_t)T * k;
-  return mx4_ws(pairs, pairs, E, K, N, true).total;
+  return mx4_ws(pairs, pairs, E, K, (size_t)pairs * N * sizeof(float)).total;
 }
 
 int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
@@ -751,7 +752,7 @@ int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t l
   if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
   if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
   if (groups->T == 0) return SWIFTSPEC_OK;
-  const Mx4Ws w = mx4_ws(pairs, pairs, Wd->E, Wd->K, Wd->N, true);
+  const Mx4Ws w = mx4_ws(pairs, pairs, Wd->E, Wd->K, (size_t)pairs * Wd->N * sizeof(float));
   if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   uint8_t* base = static_cast<uint8_t*>(ws);
   float* part = reinterpret_cast<float*>(base + w.part);

@@ -98,7 +98,10 @@ def matrix(rng, *shape, **kw):
 SIZES = [(1, 32, 16), (1, 2048, 2048), (2, 96, 48), (3, 128, 32), (5, 160, 80), (8, 1056, 112), (13, 4096, 64),
          (15, 512, 16), (16, 640, 96), (17, 2048, 144), (31, 896, 272), (32, 8192, 64), (33, 384, 48), (48, 1408, 128),
          (63, 2080, 64), (64, 4096, 208), (65, 1024, 512), (100, 352, 336), (128, 256, 256), (129, 288, 528),
-         (200, 4096, 272), (257, 1152, 304), (300, 14336, 32), (511, 64, 16), (513, 544, 1040)]
+         (200, 4096, 272), (257, 1152, 304), (300, 14336, 32), (511, 64, 16), (513, 544, 1040),
+         # few rows over much to read, K split between workgroups, tiles of 128 and 256 rows
+         (33, 8224, 2080), (40, 28672, 656), (96, 16416, 1056), (130, 14368, 1200), (200, 8192, 2128), (700, 1056, 3600),
+         (1030, 14336, 560), (1300, 544, 7056), (2100, 16448, 400)]
 
 
 @pytest.mark.parametrize("M,K,N", SIZES)
@@ -166,7 +169,7 @@ def test_gemm_extreme_scales_and_rows_without_a_value(M, K, N):
     assert n[:, N // 2].all() and n.sum() == n.shape[0]
 
 
-@pytest.mark.parametrize("M,K,N", [(1, 2048, 2048), (32, 2048, 512), (400, 1024, 1024)])
+@pytest.mark.parametrize("M,K,N", [(1, 2048, 2048), (32, 2048, 512), (60, 16384, 1152), (400, 1024, 1024)])
 def test_gemm_replays_and_repeats(M, K, N):
     """Bit-identical from call to call, with a smaller call on the same
     workspace between, and from a graph."""

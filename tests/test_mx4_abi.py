@@ -28,8 +28,9 @@ def test_sizes(ss):  # noqa: F811
                  ("moe_mx4_down", (0, 2, 4, 128, 16))):
         assert getattr(lib, f"swiftspec_{f}_workspace_bytes")(*a) == ss.WS_HEADER_BYTES
     # the query of the most rows serves every smaller number
-    most = lib.swiftspec_mx4_gemm_workspace_bytes(600, 4096, 4096)
-    assert all(lib.swiftspec_mx4_gemm_workspace_bytes(m, 4096, 4096) <= most for m in range(600))
+    for K, N in ((4096, 4096), (28672, 8192), (14336, 512), (16416, 16)):
+        sizes = [lib.swiftspec_mx4_gemm_workspace_bytes(m, K, N) for m in range(3000)]
+        assert sizes == sorted(sizes)
     for f in ("swiglu", "down"):
         q = getattr(lib, f"swiftspec_moe_mx4_{f}_workspace_bytes")
         assert all(q(t, 4, 32, 512, 256) <= q(300, 4, 32, 512, 256) for t in range(300))
