@@ -556,21 +556,25 @@ class DraftTree:
 
 # ------------------------- microscaled 4-bit matrices, mixture of experts
 
-def _rows(t, what, cols=None):
-    """(rows, columns, row stride) of a 16-bit matrix whose rows are contiguous:
-    the library takes a pointer and a leading dimension, so a tensor that it
-    would read differently is refused here."""
-    try:
-        (M, K), (ld, step) = t.shape, t.stride()
-    except ValueError:
-        raise SwiftSpecError(INVALID_ARG, what) from None
-    if t.element_size() != 2 or (step != 1 and K > 1) or (cols is not None and K != cols):
+# a call's own cost on the host counts where the kernels take a few
+# microseconds: the checks below keep to a handful of attribute reads
+_cuda = None  # (handle of a device's current stream, current device)
+
+
+def _rows(t, what, cols):
+    """(rows, row stride) of a 16-bit matrix of `cols` contiguous columns: the
+    library takes a pointer and a leading dimension, so a tensor that it would
+    read differently is refused here."""
+    if t.dim() != 2:
         raise SwiftSpecError(INVALID_ARG, what)
-    return M, K, ld if M > 1 or ld > K else K
+    (M, K), (ld, step) = t.shape, t.stride()
+    if K != cols or t.itemsize != 2 or (step != 1 and K > 1):
+        raise SwiftSpecError(INVALID_ARG, what)
+    return M, ld if M > 1 or ld > K else K
 
 
 def _dense(t, what, shape, dtype_bytes):
-    if t is None or t.shape != shape or t.element_size() != dtype_bytes or not t.is_contiguous():
+    if t is None or t.shape != shape or t.itemsize != dtype_bytes or not t.is_contiguous():
         raise SwiftSpecError(INVALID_ARG, what)
     return t
 
@@ -578,19 +582,25 @@ def _dense(t, what, shape, dtype_bytes):
 def _run(where, fn, stream, tensors, *args):
     """Call fn(*args, stream handle) with the tensors' device current (they must
     all be on it) on `stream`, or on that device's current stream."""
-    import torch
+    global _cuda
+    if _cuda is None:
+        import torch
+        _cuda = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
     dev = tensors[0].get_device()
+    if dev < 0:
+        raise SwiftSpecError(INVALID_ARG, where)
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise SwiftSpecError(INVALID_ARG, where)
-    if dev < 0:
-        raise SwiftSpecError(INVALID_ARG, where)
-    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    if torch._C._cuda_getDevice() == dev:
-        _check(fn(*args, s), where)
+    s = _cuda[0](dev) if stream is None else stream.cuda_stream
+    if _cuda[1]() == dev:
+        st = fn(*args, s)
     else:
+        import torch
         with torch.cuda.device(dev):
-            _check(fn(*args, s), where)
+            st = fn(*args, s)
+    if st:
+        raise SwiftSpecError(st, where)
 
 
 def make_mx4(codes, scales, packed=None) -> MX4:
@@ -622,7 +632,8 @@ def prepack_mx4(W: MX4, device="cuda", stream=None):
 
 def mx4_quantize(x, codes, scales, stream=None):
     """x [M][K] fp16 (rows contiguous) -> codes [M][K/2], scales [M][K/32] u8."""
-    M, K, ld = _rows(x, "mx4_quantize")
+    K = x.shape[-1]
+    M, ld = _rows(x, "mx4_quantize", K)
     _dense(codes, "mx4_quantize", (M, K // 2), 1)
     _dense(scales, "mx4_quantize", (M, K // 32), 1)
     _run("mx4_quantize", _load().swiftspec_mx4_quantize, stream, (x, codes, scales), x.data_ptr(), M, K, ld,
@@ -631,7 +642,8 @@ def mx4_quantize(x, codes, scales, stream=None):
 
 def mx4_dequantize(codes, scales, y, stream=None):
     """codes [M][K/2], scales [M][K/32] u8 -> y [M][K] fp16 (rows contiguous)."""
-    M, K, ld = _rows(y, "mx4_dequantize")
+    K = y.shape[-1]
+    M, ld = _rows(y, "mx4_dequantize", K)
     _dense(codes, "mx4_dequantize", (M, K // 2), 1)
     _dense(scales, "mx4_dequantize", (M, K // 32), 1)
     _run("mx4_dequantize", _load().swiftspec_mx4_dequantize, stream, (codes, scales, y), codes.data_ptr(),
@@ -644,11 +656,11 @@ def mx4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
 
 def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
     """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
-    M, _, ldx = _rows(x, "mx4_gemm", W.K)
-    m, _, ldy = _rows(y, "mx4_gemm", W.N)
+    M, ldx = _rows(x, "mx4_gemm", W.K)
+    m, ldy = _rows(y, "mx4_gemm", W.N)
     r, ldr, res = M, 0, None
     if residual is not None:
-        r, _, ldr = _rows(residual, "mx4_gemm", W.N)
+        r, ldr = _rows(residual, "mx4_gemm", W.N)
         res = residual.data_ptr()
     if m != M or r != M:
         raise SwiftSpecError(INVALID_ARG, "mx4_gemm")
@@ -684,7 +696,7 @@ def moe_route_workspace_bytes(T: int, E: int, k: int) -> int:
 def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True, stream=None):
     """logits [T][E] fp16 -> experts [T][k] int32 and weights [T][k] float32 of
     the k largest scores of each token, and the groups."""
-    T, _, ldl = _rows(logits, "moe_route", groups.E)
+    T, ldl = _rows(logits, "moe_route", groups.E)
     if T != groups.T:
         raise SwiftSpecError(INVALID_ARG, "moe_route")
     _dense(experts, "moe_route", (T, groups.k), 4)
@@ -707,8 +719,8 @@ def moe_mx4_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> in
 
 def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
     """x [T][K] fp16 -> h [T k][N] fp16, a row for each place of the groups."""
-    T, _, ldx = _rows(x, "moe_mx4_swiglu", Wg.K)
-    P, _, ldh = _rows(h, "moe_mx4_swiglu", Wg.N)
+    T, ldx = _rows(x, "moe_mx4_swiglu", Wg.K)
+    P, ldh = _rows(h, "moe_mx4_swiglu", Wg.N)
     if T != groups.T or P != groups.T * groups.k:
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_swiglu")
     _run("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, stream, (x, h, ws, *groups._tensors()), ctypes.byref(Wg),
@@ -723,11 +735,11 @@ def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
 def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, stream=None):
     """h [T k][K] fp16 (as moe_mx4_swiglu wrote it), weights [T][k] float32 ->
     y [T][N] fp16, the weighted sum of each token's experts plus residual."""
-    P, _, ldh = _rows(h, "moe_mx4_down", Wd.K)
-    T, _, ldy = _rows(y, "moe_mx4_down", Wd.N)
+    P, ldh = _rows(h, "moe_mx4_down", Wd.K)
+    T, ldy = _rows(y, "moe_mx4_down", Wd.N)
     r, ldr, res = T, 0, None
     if residual is not None:
-        r, _, ldr = _rows(residual, "moe_mx4_down", Wd.N)
+        r, ldr = _rows(residual, "moe_mx4_down", Wd.N)
         res = residual.data_ptr()
     if T != groups.T or r != T or P != T * groups.k:
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_down")

@@ -131,12 +131,12 @@ __device__ __forceinline__ void place_of(const Mx4Args& a, int& rb, int& cb) {
 // activation row that output row m reads, or -1 where the caller's list is wrong
 __device__ __forceinline__ int source_row(const Mx4Args& a, int m) {
   if (!a.rows) return m;
-  const int r = a.rows[m];
-  if (r < 0 || r >= a.M) {
+  const uint32_t r = (uint32_t)a.rows[m];
+  if (r >= (uint32_t)a.M) {
     report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
     return -1;
   }
-  return r / a.div;
+  return (int)(r / (uint32_t)a.div);
 }
 
 // four columns n .. n + 3 of output row m
@@ -196,6 +196,27 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   const auto rs1 = buffer_rsrc((SW ? a.s1 : a.s0) + b.e * a.s_stride, sb);
   const auto ra = RAW ? buffer_rsrc(a.x, a.x_bytes) : buffer_rsrc(a.a, a.a_bytes);
   const auto ras = buffer_rsrc(a.as, RAW ? 0u : a.as_bytes);
+  struct Stage {
+    u32x4 w[U][NT], x[U][MT][RAW ? 4 : 1];
+    uint32_t ws[NT], xs[MT];
+  };
+  auto load_weights = [&](Stage& s, int c) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      // tiles past the last repeat it (their sums are not written)
+      const uint32_t t = (uint32_t)min(t0 + nt % kC, a.Nt - 1);
+      const bool up = SW && nt >= kC;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t g = (uint32_t)(c * U + u);
+        s.w[u][nt] = buffer_load_x4(up ? rw1 : rw0, g < (uint32_t)a.G ? (uint32_t)lane * 16u : kOutside, (t * a.G + g) * 1024u);
+      }
+      s.ws[nt] = buffer_load_x1(up ? rs1 : rs0, (uint32_t)lane * 4u, (t * a.G4 + (uint32_t)(c * U / 4)) * 256u);
+    }
+  };
+  // the first weights are on their way while the rows are looked up
+  Stage s[2];
+  if (c0 < c1) load_weights(s[0], c0);
   uint32_t va[MT], vs[MT];
   bool live[MT];
 #pragma unroll
@@ -215,23 +236,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  struct Stage {
-    u32x4 w[U][NT], x[U][MT][RAW ? 4 : 1];
-    uint32_t ws[NT], xs[MT];
-  };
-  auto load = [&](Stage& s, int c) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      // tiles past the last repeat it (their sums are not written)
-      const uint32_t t = (uint32_t)min(t0 + nt % kC, a.Nt - 1);
-      const bool up = SW && nt >= kC;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t g = (uint32_t)(c * U + u);
-        s.w[u][nt] = buffer_load_x4(up ? rw1 : rw0, g < (uint32_t)a.G ? (uint32_t)lane * 16u : kOutside, (t * a.G + g) * 1024u);
-      }
-      s.ws[nt] = buffer_load_x1(up ? rs1 : rs0, (uint32_t)lane * 4u, (t * a.G4 + (uint32_t)(c * U / 4)) * 256u);
-    }
+  auto load_rows = [&](Stage& s, int c) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -247,6 +252,10 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
       }
       if constexpr (!RAW) s.xs[mt] = buffer_load_x1(ras, vs[mt], (uint32_t)(c * U / 4) * 16u);
     }
+  };
+  auto load = [&](Stage& s, int c) {
+    load_weights(s, c);
+    load_rows(s, c);
   };
   // the rows' operand of group u and its scale (RAW: in byte 0)
   auto operand = [&](const Stage& s, int u, int mt, uint32_t& scale) {
@@ -283,8 +292,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
     group(std::integral_constant<int, 1>{});
     static_assert(U == 2, "groups of a chunk");
   };
-  Stage s[2];
-  if (c0 < c1) load(s[0], c0);
+  if (c0 < c1) load_rows(s[0], c0);
   for (int c = c0; c < c1; c += 2) {
     if (c + 1 < c1) load(s[1], c + 1);
     multiply(s[0], c);
@@ -350,9 +358,15 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   constexpr int kC = SW ? WT / 2 : WT;   // output column tiles of the workgroup
   constexpr int kCW = SW ? NTW / 2 : NTW;  // and of a wave
   static_assert(WM * WN == 4 && AT % 4 == 0 && WT % 4 == 0, "four waves load alike, rows in whole 16s");
-  __shared__ u32x4 ax[2][TM * 8];          // two groups of the rows
-  __shared__ u32x4 wx[4][WT][kWave];
+  struct Operands {
+    u32x4 ax[2][TM * 8];  // rows: two slots of two groups
+    u32x4 wx[4][WT][kWave];
+  };
+  __shared__ Operands room;
+  auto& ax = room.ax;
+  auto& wx = room.wx;
   __shared__ uint32_t sc[AT + WT][kWave];
+  __shared__ uint32_t row_list[4][kWave];
   __shared__ uint8_t live[TM];  // rows that are written
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -374,19 +388,6 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   // This wave's loads: rows 8 i .. 8 i + 7 of its quarter of the rows, its quarter
   // of the weight tiles, the scales of its quarter of the row blocks.
   uint32_t va[kA], vs[AT / 4];
-#pragma unroll
-  for (int i = 0; i < kA; ++i) {
-    const int m = 8 * (wave * kA + i) + (lane >> 3);
-    const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
-    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
-  }
-#pragma unroll
-  for (int i = 0; i < AT / 4; ++i) {
-    const int m = 16 * (wave * (AT / 4) + i) + r16;
-    const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
-    vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
-  }
-  for (int m = threadIdx.x; m < TM; m += 256) live[m] = m < b.n && (!a.rows || (uint32_t)a.rows[b.m0 + m] < (uint32_t)a.M);
   uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, for SwiGLU a gate tile and its up tile in turn
 #pragma unroll
   for (int i = 0; i < kW; ++i) {
@@ -436,22 +437,54 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   constexpr int kMP = MTW / 2, kNP = NTW / 2;
   static_assert(MTW % 2 == 0 && NTW % 2 == 0, "blocks go two by two");
   f32x16 acc[kMP][kNP];
+  // First what needs no list of rows, behind the list itself (through LDS: the
+  // wait for it then leaves the weights on their way).
+  if (a.rows)
+    buffer_load_lds4(raw_rsrc(a.rows, (uint32_t)a.M * 4u), (uint32_t)lane * 4u, (uint32_t)(b.m0 + wave * (TM / 4)) * 4u,
+                     lds_address(&row_list[wave][0]));
 #pragma unroll
-  for (int i = 0; i < kMP; ++i)
+  for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, i / kW);
+  if (a.rows) {
+    vm_wait<2 * kW>();
+    asm volatile("" ::: "memory");
+  }
+  auto source = [&](int m) {  // row m of this wave's quarter; -1: none, or the caller's list is wrong
+    if (wave * (TM / 4) + m >= b.n) return -1;
+    if (!a.rows) return b.m0 + wave * (TM / 4) + m;
+    const uint32_t r = row_list[wave][m];
+    return r < (uint32_t)a.M ? (int)(r / (uint32_t)a.div) : -1;
+  };
 #pragma unroll
-    for (int j = 0; j < kNP; ++j)
+  for (int i = 0; i < kA; ++i) {
+    const int src = source(8 * i + (lane >> 3));
+    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
+  }
 #pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+  for (int i = 0; i < AT / 4; ++i) {
+    const int src = source(16 * i + r16);
+    vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
+  }
 #pragma unroll
   for (int i = 0; i < kS; ++i) load_scale(i, 0);
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
+  for (int i = 0; i < 2 * kA; ++i) load_rows(i % kA, i / kA);
 #pragma unroll
-    for (int i = 0; i < kA; ++i) load_rows(i, p);
-#pragma unroll
-    for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, 2 * p + i / kW);
+  for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, 2 + i / kW);
+  if (lane < TM / 4) {
+    const bool ok = source(lane) >= 0;
+    live[wave * (TM / 4) + lane] = ok;
+    if (!ok && wave * (TM / 4) + lane < b.n) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
   }
-  vm_lds_barrier<kA + 3 * kW>();
+  // the sums are cleared while the loads run
+#pragma unroll
+  for (int i = 0; i < kMP; ++i)
+#pragma unroll
+    for (int j = 0; j < kNP; ++j) {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+      asm volatile("" : "+a"(acc[i][j]));
+    }
+  vm_lds_barrier<kA + 2 * kW>();  // the weights of group 0, the scales, the rows of groups 0 and 1
   Ops ops[2];
   Scales s[2];
 #pragma unroll
@@ -509,14 +542,16 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   constexpr bool wide = EPI == MX4_ROWS || EPI == MX4_RESIDUAL;
   constexpr int kPC = SW ? 16 : 32;             // columns of a pair
   constexpr int kPL = wide ? 1 : 64 / kPC;      // pairs of a line
-  uint8_t* my = reinterpret_cast<uint8_t*>(&wx[0][0][0]) + wave * (32 * kTurnRow);
-  static_assert(sizeof(wx) >= 4 * 32 * kTurnRow, "the lines' room");
+  constexpr int kLines = (kNP + kPL - 1) / kPL;  // of 32 rows, all in LDS at one time
+  constexpr int kLine = 32 * kTurnRow;
+  uint8_t* my = reinterpret_cast<uint8_t*>(&room) + wave * (kLines * kLine);
+  static_assert(sizeof(Operands) >= 4 * kLines * kLine, "the lines' room");
   const int tr = lane >> 3, tc = lane & 7;  // row (of 8) and 16-byte piece of a line
 #pragma unroll
   for (int i = 0; i < kMP; ++i) {
     const int ml = 16 * (wm * MTW + 2 * i);
 #pragma unroll
-    for (int j = 0; j < kNP; ++j) {
+    for (int j = 0; j < kNP; ++j)
 #pragma unroll
       for (int q = 0; q < kPC / 8; ++q) {
         f32x4 v;
@@ -525,33 +560,44 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
           v[c] = acc[i][j][4 * q + c];
           if constexpr (SW) v[c] = silu(v[c]) * acc[i][j][4 * (q + 2) + c];
         }
+        uint8_t* line = my + (j / kPL) * kLine + r32 * kTurnRow;
         const int col = kPC * (j % kPL) + 8 * q + 4 * (lane >> 5);
-        if constexpr (wide) *reinterpret_cast<f32x4*>(my + r32 * kTurnRow + 4 * col) = v;
-        else *reinterpret_cast<u32x2*>(my + r32 * kTurnRow + 2 * col) = pack4(v);
+        if constexpr (wide) *reinterpret_cast<f32x4*>(line + 4 * col) = v;
+        else *reinterpret_cast<u32x2*>(line + 2 * col) = pack4(v);
       }
-      if ((j + 1) % kPL != 0 && j + 1 < kNP) continue;  // more of the line to come
-      const int n = 16 * (t0 + wn * kCW) + kPC * (j - j % kPL), filled = kPC * (j % kPL + 1);
-      __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int r = 8 * u + tr;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(my + r * kTurnRow + 16 * tc);
-        if (!live[ml + r]) continue;
-        const int64_t m = b.m0 + ml + r;
-        const int in = (wide ? 4 : 8) * tc, col = n + in;
-        if (in >= filled || col >= a.N) continue;
-        if constexpr (EPI == MX4_ROWS) {
-          *reinterpret_cast<u32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + col) = v;
-        } else if constexpr (EPI == MX4_RESIDUAL) {
-          f32x4 f = bitcast<f32x4>(v);
-          add_residual(f, residual(a, m, col));
-          *reinterpret_cast<u32x2*>(a.y + m * a.ldy + col) = pack4(f);
-        } else {
-          store_rows16(a.y + m * a.ldy + col, v);
+    for (int u = 0; u < 4; ++u) {
+      const int r = 8 * u + tr;
+      const bool write = live[ml + r];
+      const int64_t m = b.m0 + ml + r;
+      u32x4 v[kLines];
+      u32x2 add[kLines];
+#pragma unroll
+      for (int l = 0; l < kLines; ++l) {
+        v[l] = *reinterpret_cast<const u32x4*>(my + l * kLine + r * kTurnRow + 16 * tc);
+        if constexpr (EPI == MX4_RESIDUAL) {
+          const int col = 16 * (t0 + wn * kCW) + kPC * kPL * l + 4 * tc;
+          if (write && col < a.N) add[l] = residual(a, m, col);
         }
       }
-      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int l = 0; l < kLines; ++l) {
+        constexpr int kAll = kPC * kNP;  // columns of the wave
+        const int in = kPC * kPL * l + (wide ? 4 : 8) * tc, col = 16 * (t0 + wn * kCW) + in;
+        if (!write || in >= kAll || col >= a.N) continue;
+        if constexpr (EPI == MX4_ROWS) {
+          *reinterpret_cast<u32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + col) = v[l];
+        } else if constexpr (EPI == MX4_RESIDUAL) {
+          f32x4 f = bitcast<f32x4>(v[l]);
+          add_residual(f, add[l]);
+          *reinterpret_cast<u32x2*>(a.y + m * a.ldy + col) = pack4(f);
+        } else {
+          store_rows16(a.y + m * a.ldy + col, v[l]);
+        }
+      }
     }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
