@@ -53,7 +53,7 @@ struct Mx4Args {
   int64_t ldr;
   float* part;
   void* ws;
-  int col_blocks, tiles;
+  int col_blocks;
   int split;  // shares of K, each with its own part [M][N]
   // rows quantised by the product itself
   const uint16_t* x;
@@ -71,9 +71,9 @@ struct RowBlock {
 };
 __device__ __forceinline__ RowBlock row_block(const Mx4Args& a, int rb, int TM) {
   if (!a.map) return RowBlock{0, rb * TM, min(TM, a.M - rb * TM)};
-  // written by an earlier launch: read through the scalar cache
-  const auto* p = (const __attribute__((address_space(4))) int32_t*)(a.map + 4 * ((int64_t)rb + 1));
-  return RowBlock{p[0], p[1], p[2]};
+  const int32_t* p = a.map + 4 * ((int64_t)rb + 1);
+  return RowBlock{__builtin_amdgcn_readfirstlane(p[0]), __builtin_amdgcn_readfirstlane(p[1]),
+                  __builtin_amdgcn_readfirstlane(p[2])};
 }
 
 // The same from the offsets (as Mx4Map describes it), by each wave for itself.
@@ -113,19 +113,19 @@ __device__ __forceinline__ RowBlock find_block(const Mx4Args& a, int rb, int TM,
   return RowBlock{__builtin_amdgcn_readfirstlane(r.e), __builtin_amdgcn_readfirstlane(r.m0), __builtin_amdgcn_readfirstlane(r.n)};
 }
 
-// Tile number -> its row and column block.  Tiles are taken in bands of 4 row
+// Workgroup -> row and column block of a tile.  Tiles are taken in bands of 4 row
 // blocks, column by column, and stretches of 32 of them (what a chiplet's
 // compute units run at one time) go to the 8 chiplets in turn, as workgroups do:
 // what a chiplet reads is then a few row blocks and 8 column blocks, out of its
 // own L2, and the empty row blocks at the end of a list of experts (they come
 // last) are no chiplet's alone.
-__device__ __forceinline__ void place_of(const Mx4Args& a, int tile, int& rb, int& cb) {
-  const int all = a.tiles, x = tile & 7, s = tile >> 3;
-  const int id = tile < (all & ~255) ? (((s >> 5) << 3) + x) * 32 + (s & 31) : tile;
+__device__ __forceinline__ void place_of(const Mx4Args& a, int& rb, int& cb) {
+  const int all = gridDim.x, x = blockIdx.x & 7, s = blockIdx.x >> 3;
+  const int id = (int)blockIdx.x < (all & ~255) ? (((s >> 5) << 3) + x) * 32 + (s & 31) : (int)blockIdx.x;
   const int band = id / (4 * a.col_blocks), in = id - band * 4 * a.col_blocks;
   const int high = min(4, all / a.col_blocks - 4 * band);
-  rb = __builtin_amdgcn_readfirstlane(4 * band + in % high);
-  cb = __builtin_amdgcn_readfirstlane(in / high);
+  rb = 4 * band + in % high;
+  cb = in / high;
 }
 
 // activation row that output row m reads, or -1 where the caller's list is wrong
@@ -354,71 +354,46 @@ template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
 __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   constexpr bool SW = EPI == MX4_SWIGLU;
   constexpr int AT = WM * MTW, WT = WN * NTW, TM = 16 * AT;
-  constexpr bool kStay = TM == 256;  // one workgroup a compute unit, which stays and takes tile after tile
   constexpr int kA = 2 * AT / 4, kW = WT / 4, kS = (AT + WT) / 4;  // loads of a wave: two groups of rows, a group of weights, scales
   constexpr int kC = SW ? WT / 2 : WT;   // output column tiles of the workgroup
   constexpr int kCW = SW ? NTW / 2 : NTW;  // and of a wave
   static_assert(WM * WN == 4 && AT % 4 == 0 && WT % 4 == 0, "four waves load alike, rows in whole 16s");
-  constexpr bool wide = EPI == MX4_ROWS || EPI == MX4_RESIDUAL;
-  constexpr int kMP = MTW / 2, kNP = NTW / 2;
-  static_assert(MTW % 2 == 0 && NTW % 2 == 0, "blocks go two by two");
-  constexpr int kPC = SW ? 16 : 32;              // output columns of a pair of blocks
-  constexpr int kPL = wide ? 1 : 64 / kPC;       // pairs of a line
-  constexpr int kLines = (kNP + kPL - 1) / kPL;  // lines of a row that a wave writes
-  constexpr int kAtOnce = kStay ? 1 : kLines;    // of 32 rows, in LDS at one time
-  constexpr int kLine = 32 * kTurnRow;
   struct Operands {
     u32x4 ax[2][TM * 8];  // rows: two slots of two groups
     u32x4 wx[4][WT][kWave];
   };
-  struct Lines {
-    u32x4 at[4 * kAtOnce * kLine / 16];
-  };
   __shared__ Operands room;
-  __shared__ uint32_t sc[AT + WT][kWave];
-  __shared__ uint32_t row_list[kStay ? 2 : 1][4][kWave];
-  __shared__ uint8_t live[kStay ? 2 : 1][TM];  // rows that are written
   auto& ax = room.ax;
   auto& wx = room.wx;
-  uint8_t* my;  // this wave's lines
-  if constexpr (kStay) {
-    // the next tile's operands arrive while the lines are written
-    __shared__ Lines lines;
-    my = reinterpret_cast<uint8_t*>(&lines);
-  } else {
-    static_assert(sizeof(Operands) >= sizeof(Lines), "the lines' room");
-    my = reinterpret_cast<uint8_t*>(&room);
-  }
+  __shared__ uint32_t sc[AT + WT][kWave];
+  __shared__ uint32_t row_list[4][kWave];
+  __shared__ uint8_t live[TM];  // rows that are written
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  my += wave * (kAtOnce * kLine);
   const int wm = wave / WN, wn = wave - wm * WN;
   const int r16 = lane & 15, kq = lane >> 4;
+  int rb, cb;
+  place_of(a, rb, cb);
+  const RowBlock b = row_block(a, rb, TM);
+  if (b.n <= 0) return;
+  const int t0 = cb * kC;
   // this workgroup's share of K: whole scale words
   const int first = blockIdx.y * a.G4 / a.split, G4 = (blockIdx.y + 1) * a.G4 / a.split - first;
   const int G = min(a.G - 4 * first, 4 * G4);
   const uint32_t wb = (uint32_t)a.w_stride, sb = (uint32_t)a.s_stride;
-  struct Tile {
-    RowBlock b;
-    int t0;
-  };
-  // the first tile that has rows from `tile` on, in steps of the grid
-  auto find = [&](int tile, Tile& t) {
-    for (; tile < a.tiles; tile += gridDim.x) {
-      int rb, cb;
-      place_of(a, tile, rb, cb);
-      t.b = row_block(a, rb, TM);
-      t.t0 = cb * kC;
-      if (t.b.n > 0) break;
-    }
-    return tile;
-  };
-  i32x4 rw0, rs0, rw1, rs1;
+  const i32x4 rw0 = raw_rsrc(a.w0 + b.e * a.w_stride, wb), rs0 = raw_rsrc(a.s0 + b.e * a.s_stride, sb);
+  const i32x4 rw1 = raw_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
+  const i32x4 rs1 = raw_rsrc((SW ? a.s1 : a.s0) + b.e * a.s_stride, sb);
   const i32x4 ra = raw_rsrc(a.a, a.a_bytes), ras = raw_rsrc(a.as, a.as_bytes);
   // This wave's loads: rows 8 i .. 8 i + 7 of its quarter of the rows, its quarter
   // of the weight tiles, the scales of its quarter of the row blocks.
   uint32_t va[kA], vs[AT / 4];
   uint32_t wt[kW];  // tile of the matrix; tile w of the workgroup: wave w / NTW, for SwiGLU a gate tile and its up tile in turn
+#pragma unroll
+  for (int i = 0; i < kW; ++i) {
+    const int w = wave * kW + i, own = w / NTW, j = w - own * NTW;
+    wt[i] = (uint32_t)min(t0 + own * kCW + (SW ? j / 2 : j), a.Nt - 1);
+  }
   auto is_up = [&](int i) { return SW && ((wave * kW + i) & 1); };
   const uint32_t ax_lds = lds_address(&ax[0][0]), wx_lds = lds_address(&wx[0][0][0]), sc_lds = lds_address(&sc[0][0]);
   // load i of the rows' groups 2 p and 2 p + 1, of the weights' group g, of the
@@ -459,161 +434,57 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     if (i < MTW) s.x[i] = sc[wm * MTW + (i & ~1) + second][(i & 1) * 32 + piece];
     else s.w[i - MTW] = sc[AT + wn * NTW + ((i - MTW) & ~1) + second][(i & 1) * 32 + piece];
   };
+  constexpr int kMP = MTW / 2, kNP = NTW / 2;
+  static_assert(MTW % 2 == 0 && NTW % 2 == 0, "blocks go two by two");
   f32x16 acc[kMP][kNP];
-  // the list of a tile's rows (this wave's quarter), through LDS so that nothing
-  // else has to be waited for
-  auto load_list = [&](const Tile& t, int set) {
-    buffer_load_lds4(raw_rsrc(a.rows, (uint32_t)a.M * 4u), (uint32_t)lane * 4u, (uint32_t)(t.b.m0 + wave * (TM / 4)) * 4u,
-                     lds_address(&row_list[set][wave][0]));
-  };
-  // First loads of a tile; `listed`: its list of rows is there already.
-  auto begin = [&](const Tile& t, int set, bool listed) {
-    if (a.rows && !listed) load_list(t, set);
+  // First what needs no list of rows, behind the list itself (through LDS: the
+  // wait for it then leaves the weights on their way).
+  if (a.rows)
+    buffer_load_lds4(raw_rsrc(a.rows, (uint32_t)a.M * 4u), (uint32_t)lane * 4u, (uint32_t)(b.m0 + wave * (TM / 4)) * 4u,
+                     lds_address(&row_list[wave][0]));
 #pragma unroll
-    for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, i / kW);
-    if (a.rows && !listed) vm_wait<2 * kW>();
+  for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, i / kW);
+  if (a.rows) {
+    vm_wait<2 * kW>();
     asm volatile("" ::: "memory");
-    // lane m: the activation row of row m of this wave's quarter; -1: none, or the
-    // caller's list is wrong
-    const int m = wave * (TM / 4) + lane;
-    int src = lane < TM / 4 && m < t.b.n ? t.b.m0 + m : -1;
-    if (a.rows && src >= 0) {
-      const uint32_t r = row_list[set][wave][lane];
-      src = r < (uint32_t)a.M ? (int)(r / (uint32_t)a.div) : -1;
-      if (src < 0) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-    }
-    if (lane < TM / 4) live[set][m] = src >= 0;
-#pragma unroll
-    for (int i = 0; i < kA; ++i) {
-      const int from = __shfl(src, 8 * i + (lane >> 3), kWave);
-      va[i] = from >= 0 ? (uint32_t)from * (uint32_t)(a.G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
-    }
-#pragma unroll
-    for (int i = 0; i < AT / 4; ++i) {
-      const int from = __shfl(src, 16 * i + r16, kWave);
-      vs[i] = from >= 0 ? (uint32_t)from * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
-    }
-#pragma unroll
-    for (int i = 0; i < kS; ++i) load_scale(i, 0);
-#pragma unroll
-    for (int i = 0; i < 2 * kA; ++i) load_rows(i % kA, i / kA);
-#pragma unroll
-    for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, 2 + i / kW);
+  }
+  auto source = [&](int m) {  // row m of this wave's quarter; -1: none, or the caller's list is wrong
+    if (wave * (TM / 4) + m >= b.n) return -1;
+    if (!a.rows) return b.m0 + wave * (TM / 4) + m;
+    const uint32_t r = row_list[wave][m];
+    return r < (uint32_t)a.M ? (int)(r / (uint32_t)a.div) : -1;
   };
-  auto clear = [&]() {
 #pragma unroll
-    for (int i = 0; i < kMP; ++i)
+  for (int i = 0; i < kA; ++i) {
+    const int src = source(8 * i + (lane >> 3));
+    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
+  }
 #pragma unroll
-      for (int j = 0; j < kNP; ++j) {
+  for (int i = 0; i < AT / 4; ++i) {
+    const int src = source(16 * i + r16);
+    vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
+  }
 #pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-        asm volatile("" : "+a"(acc[i][j]));
-      }
-  };
-  // A tile's first loads are under way while the lines of the one before it are
-  // written.  `set`: of the lists of the tile that begins.
-  Tile tile, done;
-  int at = find(blockIdx.x, tile), set = 0;
-  if (at >= a.tiles) return;
-  for (bool begun = false;; begun = true) {
-  const bool more = at < a.tiles;
-  {
-    const int e = __builtin_amdgcn_readfirstlane(more ? tile.b.e : 0);
-    rw0 = raw_rsrc(a.w0 + e * a.w_stride, wb);
-    rs0 = raw_rsrc(a.s0 + e * a.s_stride, sb);
-    rw1 = raw_rsrc((SW ? a.w1 : a.w0) + e * a.w_stride, wb);
-    rs1 = raw_rsrc((SW ? a.s1 : a.s0) + e * a.s_stride, sb);
-    const int t0 = __builtin_amdgcn_readfirstlane(tile.t0);
+  for (int i = 0; i < kS; ++i) load_scale(i, 0);
 #pragma unroll
-    for (int i = 0; i < kW; ++i) {
-      const int w = wave * kW + i, own = w / NTW, j = w - own * NTW;
-      wt[i] = (uint32_t)min(t0 + own * kCW + (SW ? j / 2 : j), a.Nt - 1);
+  for (int i = 0; i < 2 * kA; ++i) load_rows(i % kA, i / kA);
+#pragma unroll
+  for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, 2 + i / kW);
+  if (lane < TM / 4) {
+    const bool ok = source(lane) >= 0;
+    live[wave * (TM / 4) + lane] = ok;
+    if (!ok && wave * (TM / 4) + lane < b.n) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+  }
+  // the sums are cleared while the loads run
+#pragma unroll
+  for (int i = 0; i < kMP; ++i)
+#pragma unroll
+    for (int j = 0; j < kNP; ++j) {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+      asm volatile("" : "+a"(acc[i][j]));
     }
-  }
-  if (more) begin(tile, set, begun);
-  bool stored = false;  // this wave wrote every line, so many stores follow those loads
-  if (begun) {
-  // Register 4 q + c of a pair of blocks holds column 8 q + 4 (lane / 32) + c of
-  // row lane % 32 (SwiGLU: gate columns for q < 2, their up columns after them).
-  // Through LDS the rows come out as whole 128-byte lines: 64 fp16 columns, or 32
-  // fp32 ones (results that a residual or another sum awaits).
-  int el = lane;
-  asm volatile("" : "+v"(el));  // addresses made of it are not kept in registers across the tiles
-  const int tr = el >> 3, tc = el & 7;  // row (of 8) and 16-byte piece of a line
-#pragma unroll
-  for (int i = 0; i < kMP; ++i) {
-    const int ml = 16 * (wm * MTW + 2 * i);
-#pragma unroll
-    for (int j = 0; j < kNP; ++j) asm volatile("" : "+a"(acc[i][j]));  // in the accumulation registers up to here
-#pragma unroll
-    for (int l0 = 0; l0 < kLines; l0 += kAtOnce) {
-#pragma unroll
-      for (int j = l0 * kPL; j < kNP && j < (l0 + kAtOnce) * kPL; ++j)
-#pragma unroll
-        for (int q = 0; q < kPC / 8; ++q) {
-          f32x4 v;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            v[c] = acc[i][j][4 * q + c];
-            if constexpr (SW) v[c] = silu(v[c]) * acc[i][j][4 * (q + 2) + c];
-          }
-          uint8_t* line = my + (j / kPL - l0) * kLine + (el & 31) * kTurnRow;
-          const int col = kPC * (j % kPL) + 8 * q + 4 * (el >> 5);
-          if constexpr (wide) *reinterpret_cast<f32x4*>(line + 4 * col) = v;
-          else *reinterpret_cast<u32x2*>(line + 2 * col) = pack4(v);
-        }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int r = 8 * u + tr;
-        const bool write = live[set ^ (kStay ? 1 : 0)][ml + r];
-        const int64_t m = done.b.m0 + ml + r;
-        u32x4 v[kAtOnce];
-        u32x2 add[kAtOnce];
-#pragma unroll
-        for (int l = 0; l < kAtOnce; ++l) {
-          v[l] = *reinterpret_cast<const u32x4*>(my + l * kLine + r * kTurnRow + 16 * tc);
-          if constexpr (EPI == MX4_RESIDUAL) {
-            const int col = 16 * (done.t0 + wn * kCW) + kPC * kPL * (l0 + l) + 4 * tc;
-            if (write && col < a.N) add[l] = residual(a, m, col);
-          }
-        }
-#pragma unroll
-        for (int l = 0; l < kAtOnce; ++l) {
-          constexpr int kAll = kPC * kNP;  // columns of the wave
-          const int in = kPC * kPL * (l0 + l) + (wide ? 4 : 8) * tc, col = 16 * (done.t0 + wn * kCW) + in;
-          if (!write || in >= kAll || col >= a.N) continue;
-          if constexpr (EPI == MX4_ROWS) {
-            *reinterpret_cast<u32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + col) = v[l];
-          } else if constexpr (EPI == MX4_RESIDUAL) {
-            f32x4 f = bitcast<f32x4>(v[l]);
-            add_residual(f, add[l]);
-            *reinterpret_cast<u32x2*>(a.y + m * a.ldy + col) = pack4(f);
-          } else {
-            store_rows16(a.y + m * a.ldy + col, v[l]);
-          }
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_sched_barrier(0);  // no later line's sums in registers yet
-    }
-  }
-    // every store was issued if all of the wave's rows and columns are there
-    bool all = 16 * (done.t0 + (wn + 1) * kCW) <= a.N;
-#pragma unroll
-    for (int r = 0; r < 16 * MTW; r += kWave) all = all && (r + lane >= 16 * MTW || live[set ^ (kStay ? 1 : 0)][16 * wm * MTW + r + lane]);
-    stored = __all(all);
-  }
-  if (!more) break;
-  clear();
-  done = tile;
-  at = kStay ? find(at + gridDim.x, tile) : a.tiles;
-  if (kStay && at < a.tiles && a.rows) load_list(tile, set ^ 1);
-  // the weights of group 0, the scales, the rows of groups 0 and 1; of the later
-  // loads and stores as many may be under way as there are for certain
-  constexpr int kStores = EPI == MX4_RESIDUAL ? 0 : kMP * kLines * 4, kAhead = kA + 2 * kW;
-  if (stored) vm_lds_barrier<(kAhead + kStores < 63 ? kAhead + kStores : 63)>();
-  else vm_lds_barrier<kAhead>();
+  vm_lds_barrier<kA + 2 * kW>();  // the weights of group 0, the scales, the rows of groups 0 and 1
   Ops ops[2];
   Scales s[2];
 #pragma unroll
@@ -628,11 +499,8 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     constexpr int kScale = J == 0 ? kS : 0, kRows = J & 1 ? kA : 0, kLoads = kScale + kRows + kW;
     constexpr int kReads = kR + (J == 3 ? kR : 0), kMfma = 2 * kMP * kNP;
     const int g = 4 * c + J;
-    // what was loaded after the weights of g + 1 (J even) or the rows of g + 1 (J odd);
-    // in a tile's first steps the stores of the one before it stand between them
-    constexpr int kAfter = (J & 1 ? 2 * kW : 2 * kW + kA) + (J == 1 || J == 2 ? kS : 0);
-    if (kStay && J < 3 && c == 0 && stored) vm_lds_barrier<(kAfter + kStores < 63 ? kAfter + kStores : 63)>();
-    else vm_lds_barrier<kAfter>();
+    // what was loaded after the weights of g + 1 (J even) or the rows of g + 1 (J odd)
+    vm_lds_barrier<(J & 1 ? 2 * kW : 2 * kW + kA) + (J == 1 || J == 2 ? kS : 0)>();
     const Ops& o = ops[J & 1];
     Ops& n = ops[(J & 1) ^ 1];
     auto load = [&](int q) {
@@ -667,7 +535,69 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     }
   }
   vm_lds_barrier<0>();  // loads past the last group still write LDS, other waves read theirs
-  if (kStay) set ^= 1;
+  // Register 4 q + c of a pair of blocks holds column 8 q + 4 (lane / 32) + c of
+  // row lane % 32 (SwiGLU: gate columns for q < 2, their up columns after them).
+  // Through LDS the rows come out as whole 128-byte lines: 64 fp16 columns, or 32
+  // fp32 ones (results that a residual or another sum awaits).
+  constexpr bool wide = EPI == MX4_ROWS || EPI == MX4_RESIDUAL;
+  constexpr int kPC = SW ? 16 : 32;             // columns of a pair
+  constexpr int kPL = wide ? 1 : 64 / kPC;      // pairs of a line
+  constexpr int kLines = (kNP + kPL - 1) / kPL;  // of 32 rows, all in LDS at one time
+  constexpr int kLine = 32 * kTurnRow;
+  uint8_t* my = reinterpret_cast<uint8_t*>(&room) + wave * (kLines * kLine);
+  static_assert(sizeof(Operands) >= 4 * kLines * kLine, "the lines' room");
+  const int tr = lane >> 3, tc = lane & 7;  // row (of 8) and 16-byte piece of a line
+#pragma unroll
+  for (int i = 0; i < kMP; ++i) {
+    const int ml = 16 * (wm * MTW + 2 * i);
+#pragma unroll
+    for (int j = 0; j < kNP; ++j)
+#pragma unroll
+      for (int q = 0; q < kPC / 8; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          v[c] = acc[i][j][4 * q + c];
+          if constexpr (SW) v[c] = silu(v[c]) * acc[i][j][4 * (q + 2) + c];
+        }
+        uint8_t* line = my + (j / kPL) * kLine + r32 * kTurnRow;
+        const int col = kPC * (j % kPL) + 8 * q + 4 * (lane >> 5);
+        if constexpr (wide) *reinterpret_cast<f32x4*>(line + 4 * col) = v;
+        else *reinterpret_cast<u32x2*>(line + 2 * col) = pack4(v);
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = 8 * u + tr;
+      const bool write = live[ml + r];
+      const int64_t m = b.m0 + ml + r;
+      u32x4 v[kLines];
+      u32x2 add[kLines];
+#pragma unroll
+      for (int l = 0; l < kLines; ++l) {
+        v[l] = *reinterpret_cast<const u32x4*>(my + l * kLine + r * kTurnRow + 16 * tc);
+        if constexpr (EPI == MX4_RESIDUAL) {
+          const int col = 16 * (t0 + wn * kCW) + kPC * kPL * l + 4 * tc;
+          if (write && col < a.N) add[l] = residual(a, m, col);
+        }
+      }
+#pragma unroll
+      for (int l = 0; l < kLines; ++l) {
+        constexpr int kAll = kPC * kNP;  // columns of the wave
+        const int in = kPC * kPL * l + (wide ? 4 : 8) * tc, col = 16 * (t0 + wn * kCW) + in;
+        if (!write || in >= kAll || col >= a.N) continue;
+        if constexpr (EPI == MX4_ROWS) {
+          *reinterpret_cast<u32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + col) = v[l];
+        } else if constexpr (EPI == MX4_RESIDUAL) {
+          f32x4 f = bitcast<f32x4>(v[l]);
+          add_residual(f, add[l]);
+          *reinterpret_cast<u32x2*>(a.y + m * a.ldy + col) = pack4(f);
+        } else {
+          store_rows16(a.y + m * a.ldy + col, v[l]);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -744,10 +674,7 @@ template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
 void launch_tile(Mx4Args a, int blocks, hipStream_t st) {
   constexpr int kC = EPI == MX4_SWIGLU ? WN * NTW / 2 : WN * NTW;
   a.col_blocks = (a.Nt + kC - 1) / kC;
-  a.tiles = blocks * a.col_blocks;
-  // tiles of 256 rows: no more workgroups than there are compute units
-  const int grid = WM * MTW == 16 && a.tiles > 256 ? 256 : a.tiles;
-  hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)grid, a.split), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)blocks * a.col_blocks, a.split), dim3(256), 0, st, a);
 }
 
 enum Form { STREAM_RAW, STREAM_1, STREAM_2, TILE_64, TILE_128, TILE_256 };
