@@ -71,9 +71,9 @@ struct RowBlock {
 };
 __device__ __forceinline__ RowBlock row_block(const Mx4Args& a, int rb, int TM) {
   if (!a.map) return RowBlock{0, rb * TM, min(TM, a.M - rb * TM)};
-  const int32_t* p = a.map + 4 * ((int64_t)rb + 1);
-  return RowBlock{__builtin_amdgcn_readfirstlane(p[0]), __builtin_amdgcn_readfirstlane(p[1]),
-                  __builtin_amdgcn_readfirstlane(p[2])};
+  // written by an earlier launch: read through the scalar cache
+  const auto* p = (const __attribute__((address_space(4))) int32_t*)(a.map + 4 * ((int64_t)rb + 1));
+  return RowBlock{p[0], p[1], p[2]};
 }
 
 // The same from the offsets (as Mx4Map describes it), by each wave for itself.
@@ -448,21 +448,25 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
     vm_wait<2 * kW>();
     asm volatile("" ::: "memory");
   }
-  auto source = [&](int m) {  // row m of this wave's quarter; -1: none, or the caller's list is wrong
-    if (wave * (TM / 4) + m >= b.n) return -1;
-    if (!a.rows) return b.m0 + wave * (TM / 4) + m;
-    const uint32_t r = row_list[wave][m];
-    return r < (uint32_t)a.M ? (int)(r / (uint32_t)a.div) : -1;
-  };
+  // lane m: the activation row of row m of this wave's quarter; -1: none, or the
+  // caller's list is wrong
+  const int mine = wave * (TM / 4) + lane;
+  int src = lane < TM / 4 && mine < b.n ? b.m0 + mine : -1;
+  if (a.rows && src >= 0) {
+    const uint32_t r = row_list[wave][lane];
+    src = r < (uint32_t)a.M ? (int)(r / (uint32_t)a.div) : -1;
+    if (src < 0) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+  }
+  if (lane < TM / 4) live[mine] = src >= 0;
 #pragma unroll
   for (int i = 0; i < kA; ++i) {
-    const int src = source(8 * i + (lane >> 3));
-    va[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
+    const int from = __shfl(src, 8 * i + (lane >> 3), kWave);
+    va[i] = from >= 0 ? (uint32_t)from * (uint32_t)(a.G * 64) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
   }
 #pragma unroll
   for (int i = 0; i < AT / 4; ++i) {
-    const int src = source(16 * i + r16);
-    vs[i] = src >= 0 ? (uint32_t)src * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
+    const int from = __shfl(src, 16 * i + r16, kWave);
+    vs[i] = from >= 0 ? (uint32_t)from * (uint32_t)(a.G4 * 16) + (uint32_t)kq * 4u : kOutside;
   }
 #pragma unroll
   for (int i = 0; i < kS; ++i) load_scale(i, 0);
@@ -470,11 +474,6 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   for (int i = 0; i < 2 * kA; ++i) load_rows(i % kA, i / kA);
 #pragma unroll
   for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, 2 + i / kW);
-  if (lane < TM / 4) {
-    const bool ok = source(lane) >= 0;
-    live[wave * (TM / 4) + lane] = ok;
-    if (!ok && wave * (TM / 4) + lane < b.n) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-  }
   // the sums are cleared while the loads run
 #pragma unroll
   for (int i = 0; i < kMP; ++i)
