@@ -579,19 +579,13 @@ def _dense(t, what, shape, dtype_bytes):
     return t
 
 
-def _run(where, fn, stream, tensors, *args):
-    """Call fn(*args, stream handle) with the tensors' device current (they must
-    all be on it) on `stream`, or on that device's current stream."""
+def _run(where, fn, stream, dev, *args):
+    """Call fn(*args, stream handle) with device `dev` current, on `stream` or on
+    the device's current stream."""
     global _cuda
     if _cuda is None:
         import torch
         _cuda = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-    dev = tensors[0].get_device()
-    if dev < 0:
-        raise SwiftSpecError(INVALID_ARG, where)
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise SwiftSpecError(INVALID_ARG, where)
     s = _cuda[0](dev) if stream is None else stream.cuda_stream
     if _cuda[1]() == dev:
         st = fn(*args, s)
@@ -601,6 +595,17 @@ def _run(where, fn, stream, tensors, *args):
             st = fn(*args, s)
     if st:
         raise SwiftSpecError(st, where)
+
+
+def _same_device(where, t, *others):
+    """The GPU that all of a call's tensors (None: not given) are on."""
+    dev = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            raise SwiftSpecError(INVALID_ARG, where)
+    if dev < 0:
+        raise SwiftSpecError(INVALID_ARG, where)
+    return dev
 
 
 def make_mx4(codes, scales, packed=None) -> MX4:
@@ -625,7 +630,7 @@ def prepack_mx4(W: MX4, device="cuda", stream=None):
     (keep the tensor alive)."""
     import torch
     t = torch.empty(mx4_packed_bytes(W.K, W.N, W.E), dtype=torch.uint8, device=device)
-    _run("mx4_prepack", _load().swiftspec_mx4_prepack, stream, (t,), ctypes.byref(W), t.data_ptr(), t.numel())
+    _run("mx4_prepack", _load().swiftspec_mx4_prepack, stream, _same_device("mx4_prepack", t), ctypes.byref(W), t.data_ptr(), t.numel())
     W.packed = t.data_ptr()
     return t
 
@@ -636,7 +641,7 @@ def mx4_quantize(x, codes, scales, stream=None):
     M, ld = _rows(x, "mx4_quantize", K)
     _dense(codes, "mx4_quantize", (M, K // 2), 1)
     _dense(scales, "mx4_quantize", (M, K // 32), 1)
-    _run("mx4_quantize", _load().swiftspec_mx4_quantize, stream, (x, codes, scales), x.data_ptr(), M, K, ld,
+    _run("mx4_quantize", _load().swiftspec_mx4_quantize, stream, _same_device("mx4_quantize", x, codes, scales), x.data_ptr(), M, K, ld,
          codes.data_ptr(), scales.data_ptr())
 
 
@@ -646,7 +651,7 @@ def mx4_dequantize(codes, scales, y, stream=None):
     M, ld = _rows(y, "mx4_dequantize", K)
     _dense(codes, "mx4_dequantize", (M, K // 2), 1)
     _dense(scales, "mx4_dequantize", (M, K // 32), 1)
-    _run("mx4_dequantize", _load().swiftspec_mx4_dequantize, stream, (codes, scales, y), codes.data_ptr(),
+    _run("mx4_dequantize", _load().swiftspec_mx4_dequantize, stream, _same_device("mx4_dequantize", codes, scales, y), codes.data_ptr(),
          scales.data_ptr(), M, K, y.data_ptr(), ld)
 
 
@@ -664,7 +669,7 @@ def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
         res = residual.data_ptr()
     if m != M or r != M:
         raise SwiftSpecError(INVALID_ARG, "mx4_gemm")
-    _run("mx4_gemm", _load().swiftspec_mx4_gemm, stream, (x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M, ldx,
+    _run("mx4_gemm", _load().swiftspec_mx4_gemm, stream, _same_device("mx4_gemm", x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M, ldx,
          y.data_ptr(), ldy, res, ldr, ws.data_ptr(), ws.numel() * ws.element_size())
 
 
@@ -680,6 +685,7 @@ class MoeGroups:
         self.offsets = _dense(new(E + 1) if offsets is None else offsets, "MoeGroups", (E + 1,), 4)
         self.rows = _dense(new(T * k) if rows is None else rows, "MoeGroups", (T * k,), 4)
         self.pos = _dense(new(T * k) if pos is None else pos, "MoeGroups", (T * k,), 4)
+        _same_device("MoeGroups", self.offsets, self.rows, self.pos)
         self._c = _Groups(T, k, E, self.offsets.data_ptr(), self.rows.data_ptr() or None, self.pos.data_ptr() or None)
 
     def _ref(self):
@@ -701,7 +707,7 @@ def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True,
         raise SwiftSpecError(INVALID_ARG, "moe_route")
     _dense(experts, "moe_route", (T, groups.k), 4)
     _dense(weights, "moe_route", (T, groups.k), 4)
-    _run("moe_route", _load().swiftspec_moe_route, stream, (logits, experts, weights, ws, *groups._tensors()),
+    _run("moe_route", _load().swiftspec_moe_route, stream, _same_device("moe_route", groups.offsets, logits, experts, weights, ws),
          logits.data_ptr(), ldl, int(bool(renormalize)), experts.data_ptr(), weights.data_ptr(), groups._ref(),
          ws.data_ptr(), ws.numel() * ws.element_size())
 
@@ -709,7 +715,7 @@ def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True,
 def moe_group(experts, groups: MoeGroups, ws, stream=None):
     """The groups of given experts [T][k] int32 (outside [0, E): none)."""
     _dense(experts, "moe_group", (groups.T, groups.k), 4)
-    _run("moe_group", _load().swiftspec_moe_group, stream, (experts, ws, *groups._tensors()), experts.data_ptr(),
+    _run("moe_group", _load().swiftspec_moe_group, stream, _same_device("moe_group", groups.offsets, experts, ws), experts.data_ptr(),
          groups._ref(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
@@ -723,7 +729,7 @@ def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
     P, ldh = _rows(h, "moe_mx4_swiglu", Wg.N)
     if T != groups.T or P != groups.T * groups.k:
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_swiglu")
-    _run("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, stream, (x, h, ws, *groups._tensors()), ctypes.byref(Wg),
+    _run("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, stream, _same_device("moe_mx4_swiglu", groups.offsets, x, h, ws), ctypes.byref(Wg),
          ctypes.byref(Wu), x.data_ptr(), ldx, groups._ref(), h.data_ptr(), ldh, ws.data_ptr(),
          ws.numel() * ws.element_size())
 
@@ -744,7 +750,7 @@ def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, s
     if T != groups.T or r != T or P != T * groups.k:
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_down")
     _dense(weights, "moe_mx4_down", (T, groups.k), 4)
-    _run("moe_mx4_down", _load().swiftspec_moe_mx4_down, stream, (h, weights, y, ws, residual, *groups._tensors()),
+    _run("moe_mx4_down", _load().swiftspec_moe_mx4_down, stream, _same_device("moe_mx4_down", groups.offsets, h, weights, y, ws, residual),
          ctypes.byref(Wd), h.data_ptr(), ldh, groups._ref(), weights.data_ptr(), y.data_ptr(), ldy, res, ldr,
          ws.data_ptr(), ws.numel() * ws.element_size())
 

@@ -18,14 +18,13 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxE = SWIFTSPEC_MAX_EXPERTS;
-constexpr int kUnitThreads = 512;  // of the workgroup that routes a unit of tokens
 constexpr int kUnits = 2;          // units that a workgroup groups
 
-// Tokens of a unit: about one pair a thread, so that a prompt fills the chip, but
+// Tokens of a unit: about 512 pairs, so that a prompt fills the chip, but
 // at most 256 units (each grouping workgroup reads all their counts) as long as
 // a unit's counts fit 16 bits.
 inline int unit_tokens(int T, int k) {
-  const int least = kUnitThreads / k, most = 65535 / k;
+  const int least = 512 / k, most = 65535 / k;
   const int need = (T + 255) / 256;
   return need < least ? least : need > most ? most : need;
 }
@@ -75,7 +74,7 @@ struct RouteArgs {
 // its reductions stay within the rows of 16 lanes that the ALU shifts in.  Lane
 // j < k keeps the j-th expert.  Where t >= T nothing is written.
 template <int V>
-__device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* counts) {
+__device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* counts, int16_t* chosen) {
   const int l = lane_id() & 15;
   const bool there = t < a.T;
   const uint16_t* row = a.logits + (int64_t)(there ? t : 0) * a.ldl;
@@ -137,25 +136,29 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* coun
     const int e = best ? (int)(0xFFFFu - (best & 0xFFFFu)) : -1;
     a.experts[(int64_t)t * a.k + l] = e;
     a.weights[(int64_t)t * a.k + l] = best ? mine / total : 0.f;
+    if (chosen) chosen[t * a.k + l] = (int16_t)e;
     if (e >= 0) atomicAdd(counts + e, 1);
   }
 }
 
-// Choose (or read) the experts of tokens t0 .. t1 and count them.
+// Choose (or read) the experts of tokens t0 .. t1 and count them; `chosen` (LDS,
+// nullable) receives them too, -1 for none.
 template <int V>
-__device__ __forceinline__ void route_tokens(const RouteArgs& a, int t0, int t1, int* counts) {
+__device__ __forceinline__ void route_tokens(const RouteArgs& a, int t0, int t1, int* counts, int16_t* chosen) {
   const int threads = blockDim.x;
   for (int e = threadIdx.x; e < a.E; e += threads) counts[e] = 0;
   __syncthreads();
   if (a.logits) {
     for (int t = t0 + 4 * (int)(threadIdx.x >> 6); t < t1; t += threads / 16) {
       const int mine = t + (lane_id() >> 4);
-      route_token<V>(a, mine < t1 ? mine : a.T, counts);
+      route_token<V>(a, mine < t1 ? mine : a.T, counts, chosen);
     }
   } else {
     for (int i = t0 * a.k + (int)threadIdx.x; i < t1 * a.k; i += threads) {
       const int e = a.experts[i];
-      if (e >= 0 && e < a.E) atomicAdd(counts + e, 1);
+      const bool has = e >= 0 && e < a.E;
+      if (chosen) chosen[i] = (int16_t)(has ? e : -1);
+      if (has) atomicAdd(counts + e, 1);
     }
   }
   __syncthreads();
@@ -170,14 +173,9 @@ struct GroupLds {
 // The places of the pairs of tokens t0 .. t1.  Thread e brings the number of expert
 // e's pairs, of all tokens and of those before t0.
 __device__ __forceinline__ void group_tokens(const RouteArgs& a, int t0, int t1, int all, int before, bool writes_offsets,
-                                              GroupLds& s) {
+                                             const int16_t* chosen, int e_first, GroupLds& s) {
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
-  int scan = all;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(scan, d, kWave);
-    if (lane >= d) scan += o;
-  }
+  const int scan = wave_scan_add(all);
   if (lane == 63) s.wave_total[wave] = scan;
   __syncthreads();
   int lead = 0, used = 0;
@@ -205,7 +203,7 @@ __device__ __forceinline__ void group_tokens(const RouteArgs& a, int t0, int t1,
       for (int w = 0; w < kWaves; ++w) s.count[w][tid] = 0;
     __syncthreads();
     const int i = i0 + tid;
-    int e = i < n1 ? a.experts[i] : -1;
+    int e = i >= n1 ? -1 : chosen ? chosen[i] : i0 == n0 ? e_first : a.experts[i];
     if (e >= a.E) e = -1;
     const bool has = e >= 0;
     // lanes of this wave with the same expert
@@ -242,19 +240,20 @@ __device__ __forceinline__ void group_tokens(const RouteArgs& a, int t0, int t1,
 template <int V>
 __global__ __launch_bounds__(kThreads) void route_one_kernel(RouteArgs a) {
   __shared__ int counts[kMaxE];
+  __shared__ int16_t chosen[kThreads];
   __shared__ GroupLds s;
-  route_tokens<V>(a, 0, a.T, counts);
-  group_tokens(a, 0, a.T, (int)threadIdx.x < a.E ? counts[threadIdx.x] : 0, 0, true, s);
+  route_tokens<V>(a, 0, a.T, counts, chosen);
+  group_tokens(a, 0, a.T, (int)threadIdx.x < a.E ? counts[threadIdx.x] : 0, 0, true, chosen, -1, s);
 }
 
 // More: count, then place.
 template <int V>
-__global__ __launch_bounds__(kUnitThreads) void route_kernel(RouteArgs a) {
+__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
   __shared__ int counts[kMaxE];
   const int t0 = blockIdx.x * a.tokens;
-  route_tokens<V>(a, t0, min(a.T, t0 + a.tokens), counts);
+  route_tokens<V>(a, t0, min(a.T, t0 + a.tokens), counts, nullptr);
   const int Ep = (a.E + 3) & ~3;
-  for (int e = threadIdx.x; e < Ep; e += kUnitThreads) a.hist[(int64_t)blockIdx.x * Ep + e] = e < a.E ? (uint16_t)counts[e] : 0;
+  for (int e = threadIdx.x; e < Ep; e += kThreads) a.hist[(int64_t)blockIdx.x * Ep + e] = e < a.E ? (uint16_t)counts[e] : 0;
 }
 
 __global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int units) {
@@ -265,6 +264,9 @@ __global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int units)
   const int tid = threadIdx.x, E4 = (a.E + 3) >> 2, wide = 1 << (32 - __builtin_clz(max(E4, 2) - 1));
   const int part = tid / wide, parts = kThreads / wide, e4 = tid - part * wide;
   const int u0 = kUnits * blockIdx.x;
+  const int64_t t0 = (int64_t)u0 * a.tokens, t1 = t0 + (int64_t)kUnits * a.tokens;
+  const int64_t mine = t0 * a.k + tid;  // this thread's first pair: read beside the counts
+  const int e_first = mine < (int64_t)a.T * a.k ? a.experts[mine] : -1;
   int n[4] = {}, b[4] = {};
   if (e4 < E4) {
 #pragma unroll 8
@@ -290,8 +292,7 @@ __global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int units)
       all += part_all[p * wide + (tid >> 2)][tid & 3];
       before += part_before[p * wide + (tid >> 2)][tid & 3];
     }
-  const int64_t t0 = (int64_t)u0 * a.tokens, t1 = t0 + (int64_t)kUnits * a.tokens;
-  group_tokens(a, (int)t0, (int)(t1 < a.T ? t1 : a.T), all, before, blockIdx.x == 0, s);
+  group_tokens(a, (int)t0, (int)(t1 < a.T ? t1 : a.T), all, before, blockIdx.x == 0, nullptr, e_first, s);
 }
 
 template <int V>
@@ -301,7 +302,7 @@ void launch_route(const RouteArgs& a, hipStream_t st) {
     return;
   }
   const int units = (a.T + a.tokens - 1) / a.tokens;
-  hipLaunchKernelGGL(route_kernel<V>, dim3((unsigned)units), dim3(kUnitThreads), 0, st, a);
+  hipLaunchKernelGGL(route_kernel<V>, dim3((unsigned)units), dim3(kThreads), 0, st, a);
   hipLaunchKernelGGL(group_kernel, dim3((unsigned)((units + kUnits - 1) / kUnits)), dim3(kThreads), 0, st, a, units);
 }
 
@@ -310,7 +311,7 @@ void launch_route(const RouteArgs& a, hipStream_t st) {
 size_t route_hist_bytes(int T, int E, int k) {
   // what any smaller number of tokens may need too: up to 256 units of the least
   // size, more only of the largest
-  const int64_t least = kUnitThreads / k, most = 65535 / k;
+  const int64_t least = 512 / k, most = 65535 / k;
   const int64_t small = (T + least - 1) / least, large = (T + most - 1) / most;
   const int64_t units = small < 256 ? small : large > 256 ? large : 256;
   return (size_t)units * ((E + 3) / 4 * 4) * sizeof(uint16_t);

@@ -89,20 +89,15 @@ __device__ __forceinline__ RowBlock find_block(const Mx4Args& a, int rb, int TM,
     const int lo = e < a.E ? a.offsets[e] : 0, hi = e < a.E ? a.offsets[e + 1] : 0;
     bad = bad || __any(lo < 0 || hi < lo || hi > a.M || (e == 0 && lo != 0));
     const int n = bad ? 0 : (hi - lo + TM - 1) / TM;
-    int s = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(s, d, kWave);
-      if (lane >= d) s += o;
-    }
+    const int s = wave_scan_add(n);
     const uint64_t past = __ballot(base + s > rb);
     if (past && r.n == 0) {
       const int l = __builtin_ctzll(past);
       r.e = e0 + l;
-      r.m0 = __shfl(lo + (rb - (base + s - n)) * TM, l, kWave);
-      r.n = min(TM, __shfl(hi, l, kWave) - r.m0);
+      r.m0 = __builtin_amdgcn_readlane(lo + (rb - (base + s - n)) * TM, l);
+      r.n = min(TM, __builtin_amdgcn_readlane(hi, l) - r.m0);
     }
-    base += __shfl(s, 63, kWave);
+    base += __builtin_amdgcn_readlane(s, 63);
   }
   if (first && lane == 0) {  // one wave of the launch
     if (bad) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
@@ -130,15 +125,15 @@ __device__ __forceinline__ void place_of(const Mx4Args& a, int& rb, int& cb) {
 }
 
 // activation row that output row m reads, or -1 where the caller's list is wrong
-__device__ __forceinline__ int source_row(const Mx4Args& a, int m) {
-  if (!a.rows) return m;
-  const uint32_t r = (uint32_t)a.rows[m];
+__device__ __forceinline__ int source_of(const Mx4Args& a, int listed) {
+  const uint32_t r = (uint32_t)listed;
   if (r >= (uint32_t)a.M) {
     report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
     return -1;
   }
   return (int)(r / (uint32_t)a.div);
 }
+__device__ __forceinline__ int source_row(const Mx4Args& a, int m) { return a.rows ? source_of(a, a.rows[m]) : m; }
 
 // four columns n .. n + 3 of output row m
 __device__ __forceinline__ u32x2 residual(const Mx4Args& a, int64_t m, int n) {
@@ -185,6 +180,8 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int rb = blockIdx.x / a.col_blocks, cb = blockIdx.x - rb * a.col_blocks;
+  // RAW: at most 64 rows, whose list is read beside the offsets
+  const int listed = RAW && a.rows && lane < a.M ? a.rows[lane] : 0;
   const RowBlock b = RAW ? find_block(a, rb, 16 * MT, blockIdx.x == 0 && wave == 0) : row_block(a, rb, 16 * MT);
   if (b.n <= 0) return;
   const int t0 = cb * kC;
@@ -222,7 +219,8 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int m = 16 * mt + r16;
-    const int src = m < b.n ? source_row(a, b.m0 + m) : -1;
+    const int row = RAW && a.rows ? __shfl(listed, (b.m0 + m) & 63, kWave) : 0;
+    const int src = m >= b.n ? -1 : RAW && a.rows ? source_of(a, row) : source_row(a, b.m0 + m);
     live[mt] = src >= 0;
     if constexpr (RAW) {
       va[mt] = live[mt] ? (uint32_t)src * a.x_row + (uint32_t)kq * 64u : kOutside;

@@ -33,6 +33,7 @@ __device__ __forceinline__ uint32_t quantize8(const u32x4& v, uint32_t& scale) {
 __device__ void write_map(const Mx4Map& m) {
   constexpr int kPer = SWIFTSPEC_MAX_EXPERTS / 256;
   __shared__ int first[SWIFTSPEC_MAX_EXPERTS + 1];  // blocks before expert e
+  __shared__ int begin[SWIFTSPEC_MAX_EXPERTS], end[SWIFTSPEC_MAX_EXPERTS];
   __shared__ int wave_sum[4];
   __shared__ int bad;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
@@ -45,17 +46,14 @@ __device__ void write_map(const Mx4Map& m) {
     n[i] = 0;
     if (e < m.E) {
       const int lo = m.offsets[e], hi = m.offsets[e + 1];
+      begin[e] = lo;
+      end[e] = hi;
       if (lo < 0 || hi < lo || hi > m.M || (e == 0 && lo != 0)) bad = 1;
       else n[i] = (hi - lo + m.tm - 1) / m.tm;
     }
     sum += n[i];
   }
-  int s = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(s, d, kWave);
-    if (lane >= d) s += o;
-  }
+  const int s = wave_scan_add(sum);
   if (lane == 63) wave_sum[wave] = s;
   __syncthreads();
   int at = s - sum;
@@ -71,7 +69,7 @@ __device__ void write_map(const Mx4Map& m) {
   if (tid == 0) {
     if (bad) report_error(m.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
     m.map[0] = !bad;
-    m.map[1] = bad ? 0 : m.offsets[m.E];
+    m.map[1] = bad ? 0 : end[m.E - 1];
   }
   const int used = bad ? 0 : first[m.E];
   for (int i = tid; i < m.blocks; i += 256) {
@@ -83,8 +81,8 @@ __device__ void write_map(const Mx4Map& m) {
         if (first[mid] <= i) lo = mid;
         else hi = mid - 1;
       }
-      const int m0 = m.offsets[lo] + (i - first[lo]) * m.tm;
-      v = u32x4{(uint32_t)lo, (uint32_t)m0, (uint32_t)min(m.tm, m.offsets[lo + 1] - m0), 0u};
+      const int m0 = begin[lo] + (i - first[lo]) * m.tm;
+      v = u32x4{(uint32_t)lo, (uint32_t)m0, (uint32_t)min(m.tm, end[lo] - m0), 0u};
     }
     *reinterpret_cast<u32x4*>(m.map + 4 * ((int64_t)i + 1)) = v;
   }

@@ -74,6 +74,21 @@ __device__ __forceinline__ bool tree_masks_wave(const int32_t* __restrict__ pare
   return tree_masks_from<kForest>(lane < T ? parent[lane] : -1, T, anc, depth);
 }
 
+// Sum over the lanes up to this one, on the ALU's own lane shifts.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_or_zero(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan_add(int v) {
+  v += dpp_or_zero<0x111, 0xF>(v);  // from 1, 2, 4, 8 lanes before, within rows of 16
+  v += dpp_or_zero<0x112, 0xF>(v);
+  v += dpp_or_zero<0x114, 0xF>(v);
+  v += dpp_or_zero<0x118, 0xF>(v);
+  v += dpp_or_zero<0x142, 0xA>(v);  // the last lane of a row to rows 1 and 3
+  v += dpp_or_zero<0x143, 0xC>(v);  // lane 31 to rows 2 and 3
+  return v;
+}
+
 // fp16 bit helpers
 __device__ __forceinline__ float h2f(uint16_t h) {
   _Float16 v;
