@@ -20,13 +20,13 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kMaxE = SWIFTSPEC_MAX_EXPERTS;
 constexpr int kUnits = 2;          // units that a workgroup groups
 
-// Tokens of a unit: about 512 pairs, so that a prompt fills the chip, but
-// at most 256 units (each grouping workgroup reads all their counts) as long as
-// a unit's counts fit 16 bits.
+// Tokens of a unit: as many as its waves take at one time, so that a prompt fills
+// the chip, but at most 256 units (each grouping workgroup reads all their
+// counts) as long as a unit's counts fit 16 bits.
+constexpr int kLeast = 4 * kWaves;
 inline int unit_tokens(int T, int k) {
-  const int least = 512 / k, most = 65535 / k;
-  const int need = (T + 255) / 256;
-  return need < least ? least : need > most ? most : need;
+  const int most = 65535 / k, need = (T + 255) / 256;
+  return need < kLeast ? kLeast : need > most ? most : need;
 }
 
 // Over the 16 lanes of a row (rotations within it): every lane gets the result.
@@ -69,8 +69,8 @@ struct RouteArgs {
   uint16_t* hist;  // [units][E rounded up to 4]
 };
 
-// 16 lanes take the top k of a token's row, V scores each (from 8 on in whole
-// 16-byte pieces, 8 (16 q + lane) .. + 7), so that a wave routes four tokens and
+// 16 lanes take the top k of a token's row, V scores each (in whole 16-byte pieces,
+// 8 (16 q + lane) .. + 7, where rows are aligned and wide enough), so that a wave routes four tokens and
 // its reductions stay within the rows of 16 lanes that the ALU shifts in.  Lane
 // j < k keeps the j-th expert.  Where t >= T nothing is written.
 template <int V>
@@ -79,7 +79,8 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* coun
   const bool there = t < a.T;
   const uint16_t* row = a.logits + (int64_t)(there ? t : 0) * a.ldl;
   uint32_t key[V];
-  if constexpr (V < 8) {
+  const bool lines = V >= 8 && a.lines;
+  if (!lines) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int e = l + 16 * i;
@@ -90,7 +91,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* coun
     for (int q = 0; q < V / 8; ++q) {
       const int e = 8 * (16 * q + l);
       u32x4 v = {0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
-      if (a.lines && e + 8 <= a.E) {
+      if (e + 8 <= a.E) {
         v = *reinterpret_cast<const u32x4*>(row + e);
       } else {
 #pragma unroll
@@ -103,7 +104,7 @@ __device__ __forceinline__ void route_token(const RouteArgs& a, int t, int* coun
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int e = V < 8 ? l + 16 * i : 8 * (16 * (i >> 3) + l) + (i & 7);
+    const int e = lines ? 8 * (16 * (i >> 3) + l) + (i & 7) : l + 16 * i;
     const uint32_t s = score_key(key[i]);
     key[i] = s ? s << 16 | (0xFFFFu - (uint32_t)e) : 0u;
   }
@@ -311,8 +312,8 @@ void launch_route(const RouteArgs& a, hipStream_t st) {
 size_t route_hist_bytes(int T, int E, int k) {
   // what any smaller number of tokens may need too: up to 256 units of the least
   // size, more only of the largest
-  const int64_t least = 512 / k, most = 65535 / k;
-  const int64_t small = (T + least - 1) / least, large = (T + most - 1) / most;
+  const int64_t most = 65535 / k;
+  const int64_t small = (T + kLeast - 1) / kLeast, large = (T + most - 1) / most;
   const int64_t units = small < 256 ? small : large > 256 ? large : 256;
   return (size_t)units * ((E + 3) / 4 * 4) * sizeof(uint16_t);
 }

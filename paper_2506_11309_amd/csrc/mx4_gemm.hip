@@ -613,9 +613,10 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restric
   const int per = N / 4;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t t = i / per;
-  if (t >= T || !map[0]) return;
+  if (t >= T) return;
   const int n = (int)(i - t * per) * 4;
-  const int used = map[1];
+  // the lists and the residual are read side by side
+  const int valid = map[0], used = map[1];
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (res) add_residual(v, *reinterpret_cast<const u32x2*>(res + t * ldr + n));
   for (int j0 = 0; j0 < k; j0 += KU) {
@@ -624,12 +625,18 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restric
     f32x4 o[KU];
 #pragma unroll
     for (int j = 0; j < KU; ++j) {
-      p[j] = j0 + j < k ? pos[t * k + j0 + j] : -1;
+      const int64_t at = t * k + min(j0 + j, k - 1);
+      p[j] = pos[at];
+      w[j] = weights[at];
+    }
+    if (!valid) return;
+#pragma unroll
+    for (int j = 0; j < KU; ++j) {
+      if (j0 + j >= k) p[j] = -1;
       if (p[j] >= used) {
         report_error(ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
         p[j] = -1;
       }
-      w[j] = p[j] >= 0 ? weights[t * k + j0 + j] : 0.f;
     }
 #pragma unroll
     for (int j = 0; j < KU; ++j)
@@ -703,10 +710,16 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
     // short K, where its workgroups are brief, from 1 (128 experts 1024 x 512: 18.2
     // against 15.8).
     if (M < (K <= 1024 ? 1 : 4) * (int64_t)E) return plan(STREAM_1);
+    // Larger tiles as long as there are enough of them for the chip (blocks of
+    // rows: an expert's last is half full).
+    auto enough = [&](Form f) {
+      return (M / kRowsOf[f] + (E < M ? E : M) / 2) * (int64_t)((N * (swiglu ? 2 : 1) + kColumnsOf[f] - 1) / kColumnsOf[f]) >= 200;
+    };
     // 64 rows: 64 against 128 rows a tile 43.9 and 47.3 (64 experts 2048 x 1024);
     // 128 rows: 60.0 and 57.5.  256 against 128 rows a tile: at 256 rows 91.5 and
     // 78.8, at 512 127.8 and 142.1; over a long K at 256 rows 118 and 139.
-    return plan(avg < 96 ? TILE_64 : avg < (K >= 8192 ? 192 : 320) ? TILE_128 : TILE_256);
+    if (avg >= (K >= 8192 ? 192 : 320) && enough(TILE_256)) return plan(TILE_256);
+    return plan(avg >= 96 && enough(TILE_128) ? TILE_128 : TILE_64);
   }
   if (M <= 16) return plan(STREAM_1);
   auto tiles = [&](Form f) { return (int64_t)((M + kRowsOf[f] - 1) / kRowsOf[f]) * ((N + kColumnsOf[f] - 1) / kColumnsOf[f]); };
@@ -725,14 +738,14 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
   // 8192 x 8192 26.5 against 32.1; of 4096 x 4096 16.0 against 17.8), over a long K
   // only few of them (14336 x 4096: 128 rows 22.3 against 23.3, 256 rows 30.7
   // against 26.9).
-  if (M <= 64 || (M <= 512 && tiles(TILE_64) <= (K <= 8192 ? 256 : 64))) return plan(TILE_64, split_of(TILE_64, 4));
+  if (M <= 64 || (M <= 512 && tiles(TILE_64) <= (K <= 8192 ? 256 : 64))) return plan(TILE_64, split_of(TILE_64, 2));
   // 256-row tiles where they nearly fill the chip (384 rows of 8192 x 28672, 224
   // tiles: 66 against 75; 192 rows, 112 tiles: 55 against 51), over a long K with
   // two shares or more (28672 x 8192: 1024 rows 141 against 158).
   const int64_t big = tiles(TILE_256);
   if (M > 192 && (big >= 160 || (K >= 14336 && big >= 96) || (K >= 16384 && big >= 64)))
     return plan(TILE_256, K >= 14336 ? split_of(TILE_256, 14) : 1);
-  return plan(TILE_128, split_of(TILE_128, 4));
+  return plan(TILE_128, split_of(TILE_128, 2));
 }
 
 template <Mx4Epilogue EPI>
@@ -828,7 +841,7 @@ size_t mx4_part_bytes_most(int M, int K, int N) {
     const int64_t all = 256ll * kRowsOf[f] * kColumnsOf[f], mine = split * M * N;
     return split > 1 ? (size_t)(all < mine ? all : mine) * sizeof(float) : 0;
   };
-  const size_t a = most(TILE_128, G4 / 4), b = K >= 14336 ? most(TILE_256, G4 / 14) : 0;
+  const size_t a = most(TILE_128, G4 / 2), b = K >= 14336 ? most(TILE_256, G4 / 14) : 0;
   return a > b ? a : b;
 }
 
