@@ -702,7 +702,10 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
   auto plan = [](Form f, int split = 1) { return Plan{f, kRowsOf[f], split}; };
   // One launch, but more registers and work in it: 8 rows of 8192 x 8192 12.4
   // against 13.1, 1 row 10.8 against 11.9; of 8192 x 28672 (112 MB) 37.0 against 26.9.
-  if (raw && M <= 8 && weights <= (64 << 20)) return plan(STREAM_RAW);
+  // Up to a whole block of rows where there is little to read (16 of 4096 x 4096 8.3
+  // against 9.6; 16 pairs of experts 1024 x 1024, 8 MB, with their combination 11.2
+  // against 13.9; but SwiGLU of them, 16 MB, 13.2 against 10.1).
+  if (raw && M <= (weights <= (12 << 20) ? 16 : 8) && weights <= (64 << 20)) return plan(STREAM_RAW);
   if (grouped) {
     const int64_t avg = M / E;
     // Rows per expert: at 2 the stream is faster (8 experts 4096 x 14336: 56.6
