@@ -29,7 +29,7 @@ def same_groups(g, want):
 
 ROUTES = [(1, 1, 1), (1, 8, 2), (1, 512, 16), (7, 3, 3), (63, 64, 8), (64, 65, 6), (65, 128, 1), (129, 130, 5),
           (1000, 256, 8), (1025, 2, 1), (3000, 60, 7), (20000, 512, 4),
-          (70001, 13, 3)]
+          (70001, 13, 3), (96, 146, 10), (97, 146, 2), (256, 64, 4), (257, 64, 2), (1024, 4, 1), (640, 3, 2), (16385, 4, 4)]
 
 
 @pytest.mark.parametrize("T,E,k", ROUTES)
