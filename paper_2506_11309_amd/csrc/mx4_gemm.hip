@@ -731,9 +731,11 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
       return (M / kRowsOf[f] + (E < M ? E : M) / 2) * (int64_t)((N * (swiglu ? 2 : 1) + kColumnsOf[f] - 1) / kColumnsOf[f]) >= 200;
     };
     // 64 rows: 64 against 128 rows a tile 43.9 and 47.3 (64 experts 2048 x 1024);
-    // 128 rows: 60.0 and 57.5.  256 against 128 rows a tile: at 256 rows 91.5 and
-    // 78.8, at 512 127.8 and 142.1; over a long K at 256 rows 118 and 139.
-    if (avg >= (K >= 8192 ? 192 : 320) && enough(TILE_256)) return plan(TILE_256);
+    // 128 rows: 60.0 and 57.5.  256 against 128 rows a tile (64 experts): SwiGLU
+    // 2048 x 1024 of 384 rows 115 and 102, 768 rows 177 and 174, 1536 rows 306 and
+    // 316; down 1024 x 2048 of 384 rows 132 and 128, 768 rows 234 and 241; over a
+    // long K (8 experts, down 14336 x 4096) of 192 rows 111 and 133.
+    if (avg >= (K >= 8192 ? 192 : 512) && enough(TILE_256)) return plan(TILE_256);
     return plan(avg >= 96 && enough(TILE_128) ? TILE_128 : TILE_64);
   }
   if (M <= 16) return plan(STREAM_1);
