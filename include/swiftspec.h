@@ -461,7 +461,8 @@ int swiftspec_greedy_accept(const uint16_t* logits, int32_t ldl, int32_t T, int3
  *           by the caller), the only one that the products read.
  * K % 32 == 0 (K is padded to whole groups of 128 in the packed copy),
  * N % 16 == 0, 1 <= E <= SWIFTSPEC_MAX_EXPERTS, one matrix's packed copy below
- * 4 GiB (UNSUPPORTED otherwise).
+ * 4 GiB and all of them below 64 GiB; a product whose launch would need 2^32
+ * threads or more is refused (UNSUPPORTED in each case).
  * Products take fp16 activations and quantise them by the same blocks first:
  * both operands are in 4 bits, the sums in fp32. */
 typedef struct {
@@ -479,7 +480,7 @@ int swiftspec_mx4_prepack(const swiftspec_mx4* W, void* packed, size_t packed_by
  * largest magnitude a: s - 127 = floor(log2 a) - 2, every value goes to the
  * nearest code of v / 2^(s - 127), ties to the even code, saturating at 6;
  * a = 0: s = 127.  A block that holds an infinity or a NaN gets s = 255 and
- * codes 0: it stands for NaN. */
+ * codes 0: it stands for NaN.  M K < 2^35 (also of dequantize). */
 int swiftspec_mx4_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx, uint8_t* codes, uint8_t* scales,
                            void* stream);
 /* y [M][ldy] fp16 (16-byte aligned, ldy % 8 == 0): the values that codes and
@@ -551,9 +552,9 @@ size_t swiftspec_moe_mx4_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E,
  * order, each product rounded to fp32 only; every row of y is written (a token
  * without experts gets its residual, or 0).  h [T k][ldh] as swiglu wrote it
  * (all T k rows must be readable; those past offsets[E] do not enter), y and
- * residual [T][ld*] as in swiftspec_mx4_gemm.  Invalid offsets set
- * SWIFTSPEC_DEVERR_BAD_GROUPS and nothing is written; a place outside
- * [0, offsets[E]) sets it and does not enter. */
+ * residual [T][ld*] as in swiftspec_mx4_gemm; T N < 2^33.  Invalid offsets set
+ * SWIFTSPEC_DEVERR_BAD_GROUPS and nothing is written; a place from offsets[E] on
+ * sets it and does not enter (a negative one: no expert). */
 int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
                            const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr,
                            void* ws, size_t ws_bytes, void* stream);

@@ -48,6 +48,7 @@ class W4(ctypes.Structure):
 
 class MX4(ctypes.Structure):
     _fields_ = [("codes", vp), ("scales", vp), ("K", i32), ("N", i32), ("E", i32), ("packed", vp)]
+    device = None  # index of the GPU that make_mx4 found the codes on
 
 
 class _Groups(ctypes.Structure):
@@ -559,22 +560,36 @@ class DraftTree:
 # a call's own cost on the host counts where the kernels take a few
 # microseconds: the checks below keep to a handful of attribute reads
 _cuda = None  # (handle of a device's current stream, current device)
+_half = None  # torch.float16
 
 
-def _rows(t, what, cols):
-    """(rows, row stride) of a 16-bit matrix of `cols` contiguous columns: the
-    library takes a pointer and a leading dimension, so a tensor that it would
-    read differently is refused here."""
+def _rows(t, what, cols, most=2**31 - 1):
+    """(rows, row stride) of an fp16 matrix of `cols` contiguous columns: the
+    library takes a pointer and a leading dimension (both of them 32-bit numbers
+    but in the quantisation), so a tensor that it would read differently is
+    refused here."""
+    global _half
+    if _half is None:
+        import torch
+        _half = torch.float16
     if t.dim() != 2:
         raise SwiftSpecError(INVALID_ARG, what)
     (M, K), (ld, step) = t.shape, t.stride()
-    if K != cols or t.itemsize != 2 or (step != 1 and K > 1):
+    if K != cols or t.dtype is not _half or (step != 1 and K > 1):
         raise SwiftSpecError(INVALID_ARG, what)
-    return M, ld if M > 1 or ld > K else K
+    if M <= 1 and ld <= K:
+        ld = K
+    if M > most or ld > most:
+        raise SwiftSpecError(UNSUPPORTED, what)
+    return M, ld
 
 
-def _dense(t, what, shape, dtype_bytes):
+def _dense(t, what, shape, dtype_bytes, real=None):
+    """t, if it is a contiguous tensor of these sizes: floats (`real`), integers
+    (real=False) or any bytes."""
     if t is None or t.shape != shape or t.itemsize != dtype_bytes or not t.is_contiguous():
+        raise SwiftSpecError(INVALID_ARG, what)
+    if real is not None and t.dtype.is_floating_point != real:
         raise SwiftSpecError(INVALID_ARG, what)
     return t
 
@@ -597,13 +612,14 @@ def _run(where, fn, stream, dev, *args):
         raise SwiftSpecError(st, where)
 
 
-def _same_device(where, t, *others):
-    """The GPU that all of a call's tensors (None: not given) are on."""
+def _same_device(where, W, t, *others):
+    """The GPU that all of a call's tensors (None: not given) and its matrix W
+    (None: no matrix) are on."""
     dev = t.get_device()
     for o in others:
         if o is not None and o.get_device() != dev:
             raise SwiftSpecError(INVALID_ARG, where)
-    if dev < 0:
+    if dev < 0 or (W is not None and W.device not in (None, dev)):
         raise SwiftSpecError(INVALID_ARG, where)
     return dev
 
@@ -616,8 +632,10 @@ def make_mx4(codes, scales, packed=None) -> MX4:
         raise SwiftSpecError(INVALID_ARG, "make_mx4")
     _dense(scales, "make_mx4", (*codes.shape[:-1], codes.shape[-1] // 16), 1)
     E = codes.shape[0] if codes.dim() == 3 else 1
-    return MX4(codes.data_ptr(), scales.data_ptr(), 2 * codes.shape[-1], codes.shape[-2], E,
-               packed.data_ptr() if packed is not None else None)
+    W = MX4(codes.data_ptr(), scales.data_ptr(), 2 * codes.shape[-1], codes.shape[-2], E,
+            packed.data_ptr() if packed is not None else None)
+    W.device = _same_device("make_mx4", None, codes, scales, packed)
+    return W
 
 
 def mx4_packed_bytes(K: int, N: int, E: int = 1) -> int:
@@ -625,12 +643,12 @@ def mx4_packed_bytes(K: int, N: int, E: int = 1) -> int:
 
 
 def prepack_mx4(W: MX4, device="cuda", stream=None):
-    """Allocate and fill the kernel-native copy of W on `device` (the one that
-    holds its codes); returns the uint8 device tensor and sets W.packed to it
-    (keep the tensor alive)."""
+    """Allocate and fill the kernel-native copy of W on `device` (the GPU that
+    holds its codes; another one is refused); returns the uint8 device tensor and
+    sets W.packed to it (keep the tensor alive)."""
     import torch
     t = torch.empty(mx4_packed_bytes(W.K, W.N, W.E), dtype=torch.uint8, device=device)
-    _run("mx4_prepack", _load().swiftspec_mx4_prepack, stream, _same_device("mx4_prepack", t), ctypes.byref(W), t.data_ptr(), t.numel())
+    _run("mx4_prepack", _load().swiftspec_mx4_prepack, stream, _same_device("mx4_prepack", W, t), ctypes.byref(W), t.data_ptr(), t.numel())
     W.packed = t.data_ptr()
     return t
 
@@ -638,20 +656,20 @@ def prepack_mx4(W: MX4, device="cuda", stream=None):
 def mx4_quantize(x, codes, scales, stream=None):
     """x [M][K] fp16 (rows contiguous) -> codes [M][K/2], scales [M][K/32] u8."""
     K = x.shape[-1]
-    M, ld = _rows(x, "mx4_quantize", K)
+    M, ld = _rows(x, "mx4_quantize", K, 2**63 - 1)
     _dense(codes, "mx4_quantize", (M, K // 2), 1)
     _dense(scales, "mx4_quantize", (M, K // 32), 1)
-    _run("mx4_quantize", _load().swiftspec_mx4_quantize, stream, _same_device("mx4_quantize", x, codes, scales), x.data_ptr(), M, K, ld,
+    _run("mx4_quantize", _load().swiftspec_mx4_quantize, stream, _same_device("mx4_quantize", None, x, codes, scales), x.data_ptr(), M, K, ld,
          codes.data_ptr(), scales.data_ptr())
 
 
 def mx4_dequantize(codes, scales, y, stream=None):
     """codes [M][K/2], scales [M][K/32] u8 -> y [M][K] fp16 (rows contiguous)."""
     K = y.shape[-1]
-    M, ld = _rows(y, "mx4_dequantize", K)
+    M, ld = _rows(y, "mx4_dequantize", K, 2**63 - 1)
     _dense(codes, "mx4_dequantize", (M, K // 2), 1)
     _dense(scales, "mx4_dequantize", (M, K // 32), 1)
-    _run("mx4_dequantize", _load().swiftspec_mx4_dequantize, stream, _same_device("mx4_dequantize", codes, scales, y), codes.data_ptr(),
+    _run("mx4_dequantize", _load().swiftspec_mx4_dequantize, stream, _same_device("mx4_dequantize", None, codes, scales, y), codes.data_ptr(),
          scales.data_ptr(), M, K, y.data_ptr(), ld)
 
 
@@ -669,7 +687,7 @@ def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
         res = residual.data_ptr()
     if m != M or r != M:
         raise SwiftSpecError(INVALID_ARG, "mx4_gemm")
-    _run("mx4_gemm", _load().swiftspec_mx4_gemm, stream, _same_device("mx4_gemm", x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M, ldx,
+    _run("mx4_gemm", _load().swiftspec_mx4_gemm, stream, _same_device("mx4_gemm", W, x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M, ldx,
          y.data_ptr(), ldy, res, ldr, ws.data_ptr(), ws.numel() * ws.element_size())
 
 
@@ -682,10 +700,10 @@ class MoeGroups:
         import torch
         new = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
         self.T, self.k, self.E = T, k, E
-        self.offsets = _dense(new(E + 1) if offsets is None else offsets, "MoeGroups", (E + 1,), 4)
-        self.rows = _dense(new(T * k) if rows is None else rows, "MoeGroups", (T * k,), 4)
-        self.pos = _dense(new(T * k) if pos is None else pos, "MoeGroups", (T * k,), 4)
-        _same_device("MoeGroups", self.offsets, self.rows, self.pos)
+        self.offsets = _dense(new(E + 1) if offsets is None else offsets, "MoeGroups", (E + 1,), 4, real=False)
+        self.rows = _dense(new(T * k) if rows is None else rows, "MoeGroups", (T * k,), 4, real=False)
+        self.pos = _dense(new(T * k) if pos is None else pos, "MoeGroups", (T * k,), 4, real=False)
+        _same_device("MoeGroups", None, self.offsets, self.rows, self.pos)
         self._c = _Groups(T, k, E, self.offsets.data_ptr(), self.rows.data_ptr() or None, self.pos.data_ptr() or None)
 
     def _ref(self):
@@ -705,17 +723,17 @@ def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True,
     T, ldl = _rows(logits, "moe_route", groups.E)
     if T != groups.T:
         raise SwiftSpecError(INVALID_ARG, "moe_route")
-    _dense(experts, "moe_route", (T, groups.k), 4)
-    _dense(weights, "moe_route", (T, groups.k), 4)
-    _run("moe_route", _load().swiftspec_moe_route, stream, _same_device("moe_route", groups.offsets, logits, experts, weights, ws),
+    _dense(experts, "moe_route", (T, groups.k), 4, real=False)
+    _dense(weights, "moe_route", (T, groups.k), 4, real=True)
+    _run("moe_route", _load().swiftspec_moe_route, stream, _same_device("moe_route", None, groups.offsets, logits, experts, weights, ws),
          logits.data_ptr(), ldl, int(bool(renormalize)), experts.data_ptr(), weights.data_ptr(), groups._ref(),
          ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def moe_group(experts, groups: MoeGroups, ws, stream=None):
     """The groups of given experts [T][k] int32 (outside [0, E): none)."""
-    _dense(experts, "moe_group", (groups.T, groups.k), 4)
-    _run("moe_group", _load().swiftspec_moe_group, stream, _same_device("moe_group", groups.offsets, experts, ws), experts.data_ptr(),
+    _dense(experts, "moe_group", (groups.T, groups.k), 4, real=False)
+    _run("moe_group", _load().swiftspec_moe_group, stream, _same_device("moe_group", None, groups.offsets, experts, ws), experts.data_ptr(),
          groups._ref(), ws.data_ptr(), ws.numel() * ws.element_size())
 
 
@@ -727,9 +745,9 @@ def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
     """x [T][K] fp16 -> h [T k][N] fp16, a row for each place of the groups."""
     T, ldx = _rows(x, "moe_mx4_swiglu", Wg.K)
     P, ldh = _rows(h, "moe_mx4_swiglu", Wg.N)
-    if T != groups.T or P != groups.T * groups.k:
+    if T != groups.T or P != groups.T * groups.k or Wu.device not in (None, Wg.device):
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_swiglu")
-    _run("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, stream, _same_device("moe_mx4_swiglu", groups.offsets, x, h, ws), ctypes.byref(Wg),
+    _run("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, stream, _same_device("moe_mx4_swiglu", Wg, groups.offsets, x, h, ws), ctypes.byref(Wg),
          ctypes.byref(Wu), x.data_ptr(), ldx, groups._ref(), h.data_ptr(), ldh, ws.data_ptr(),
          ws.numel() * ws.element_size())
 
@@ -749,8 +767,8 @@ def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, s
         res = residual.data_ptr()
     if T != groups.T or r != T or P != T * groups.k:
         raise SwiftSpecError(INVALID_ARG, "moe_mx4_down")
-    _dense(weights, "moe_mx4_down", (T, groups.k), 4)
-    _run("moe_mx4_down", _load().swiftspec_moe_mx4_down, stream, _same_device("moe_mx4_down", groups.offsets, h, weights, y, ws, residual),
+    _dense(weights, "moe_mx4_down", (T, groups.k), 4, real=True)
+    _run("moe_mx4_down", _load().swiftspec_moe_mx4_down, stream, _same_device("moe_mx4_down", Wd, groups.offsets, h, weights, y, ws, residual),
          ctypes.byref(Wd), h.data_ptr(), ldh, groups._ref(), weights.data_ptr(), y.data_ptr(), ldy, res, ldr,
          ws.data_ptr(), ws.numel() * ws.element_size())
 

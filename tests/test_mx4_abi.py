@@ -178,3 +178,59 @@ def test_reference_block_of_one_expert_is_a_dense_one():
     h16 = h.astype(np.float16)
     y, _ = ref.down(h16, wd, offsets, pos, np.ones((T, 1), np.float32))
     assert np.allclose(y, ref.gemm(h16, wd[0])[0])
+
+
+def test_launches_of_too_many_threads(ss):  # noqa: F811
+    """Sizes whose launch would reach 2^32 threads are refused, whatever memory the
+    caller names for them."""
+    lib = ss.lib()
+    W = lambda K, N, E: ss.MX4(FAKE, FAKE, K, N, E, FAKE)  # noqa: E731
+    G = lambda T, k, E: ss._Groups(T, k, E, FAKE, FAKE, FAKE)  # noqa: E731
+    r = ctypes.byref
+    # 512 matrices of 65536 x 4096: 72 GB packed
+    assert status(lib, "mx4_prepack", r(W(65536, 4096, 512)), FAKE, BIG) == ss.UNSUPPORTED
+    rows = (1 << 35) // 64
+    assert status(lib, "mx4_quantize", FAKE, rows, 64, 64, FAKE, FAKE) == ss.UNSUPPORTED
+    assert status(lib, "mx4_dequantize", FAKE, FAKE, rows, 64, FAKE, 64) == ss.UNSUPPORTED
+    # at most 504 rows of 512 experts over 2^19 columns: up to 535 blocks of 16 rows
+    assert status(lib, "moe_mx4_swiglu", r(W(128, 1 << 19, 512)), r(W(128, 1 << 19, 512)), FAKE, 128, r(G(63, 8, 512)), FAKE, 1 << 19,
+                  FAKE, BIG) == ss.UNSUPPORTED
+    # four results a thread of the combination
+    assert status(lib, "moe_mx4_down", r(W(128, 8192, 8)), FAKE, 128, r(G(1 << 20, 1, 8)), FAKE, FAKE, 8192, None, 0, FAKE,
+                  BIG) == ss.UNSUPPORTED
+
+
+def test_tensors_that_the_library_would_read_differently(ss):  # noqa: F811
+    """The binding refuses another type of the same width, sizes and strides that a
+    32-bit number does not hold, and a matrix on another GPU."""
+    torch = pytest.importorskip("torch")
+
+    def refused(status, f, *args, **named):
+        with pytest.raises(ss.SwiftSpecError) as e:
+            f(*args, **named)
+        assert e.value.status == status
+
+    bad, big = ss.INVALID_ARG, ss.UNSUPPORTED
+    t = lambda shape, stride, dtype: torch.empty_strided(shape, stride, dtype=dtype, device="meta")  # noqa: E731
+    half, wide = torch.float16, (1 << 32) + 64
+    assert ss._rows(t((3, 64), (72, 1), half), "", 64) == (3, 72)
+    assert ss._rows(t((1, 64), (wide, 1), half), "", 64, 2**63 - 1) == (1, wide)
+    for dtype in (torch.bfloat16, torch.int16, torch.float32):
+        refused(bad, ss._rows, t((3, 64), (64, 1), dtype), "", 64)
+    refused(big, ss._rows, t((2, 64), (wide, 1), half), "", 64)
+    refused(big, ss._rows, t((1 << 31, 64), (64, 1), half), "", 64)
+    refused(bad, ss._dense, t((3, 2), (2, 1), torch.float32), "", (3, 2), 4, real=False)
+    refused(bad, ss._dense, t((3, 2), (2, 1), torch.int32), "", (3, 2), 4, real=True)
+    codes, scales = torch.zeros(16, 64, dtype=torch.uint8), torch.zeros(16, 4, dtype=torch.uint8)
+    refused(bad, ss.make_mx4, codes, scales)  # not on a GPU
+
+    class OnGpu:
+        def get_device(self):
+            return 1
+
+    W = ss.MX4(FAKE, FAKE, 128, 16, 1, FAKE)
+    assert ss._same_device("", W, OnGpu()) == 1  # made without tensors: not known
+    W.device = 0
+    refused(bad, ss._same_device, "", W, OnGpu())
+    W.device = 1
+    assert ss._same_device("", W, OnGpu(), None, OnGpu()) == 1
