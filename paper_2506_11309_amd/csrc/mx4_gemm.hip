@@ -761,8 +761,11 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
   // Few rows or little to read: 128 rows of 4096 x 4096 14.3 against 14.8, 32 of
   // 8192 x 8192 15.3 against 21; but 28672 x 8192 39.2 against 31.6, 8192 x 28672
   // 38.5 against 35.
-  if (M <= 128 && (int64_t)K * N <= (1 << 24)) return plan(STREAM_2);
-  if (M <= 32 && K < 16384 && N < 24576) return plan(STREAM_2);
+  // 16 rows a workgroup, not 32, where those would leave compute units idle (32
+  // rows of 11008 x 4096 13.7 against 16.9, of 4096 x 4096 10.0 against 11.8; but of
+  // 8192 x 8192 16.3 against 15.1).
+  if ((M <= 128 && (int64_t)K * N <= (1 << 24)) || (M <= 32 && K < 16384 && N < 24576))
+    return plan(tiles(STREAM_2) < 256 ? STREAM_1 : STREAM_2);
   // 64-row tiles as long as they are at most one for each compute unit (256 rows of
   // 8192 x 8192 26.5 against 32.1; of 4096 x 4096 16.0 against 17.8), over a long K
   // only few of them (14336 x 4096: 128 rows 22.3 against 23.3, 256 rows 30.7

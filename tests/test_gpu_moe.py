@@ -107,7 +107,10 @@ def experts_of(rng, T, E, k, kind):
 CASES = [(1, 1, 1, 32, 16, "random"), (1, 8, 2, 256, 48, "random"), (1, 64, 8, 2048, 64, "random"), (5, 4, 2, 160, 80, "padded"),
          (16, 8, 2, 1024, 32, "random"), (33, 5, 3, 96, 112, "twice"), (64, 2, 1, 512, 64, "one"), (64, 16, 4, 1408, 96, "padded"),
          (40, 300, 16, 128, 32, "random"), (7, 4, 2, 128, 32, "none"), (300, 3, 2, 352, 144, "random"), (600, 8, 2, 256, 272, "padded"),
-         (700, 2, 2, 544, 80, "twice"), (513, 4, 1, 4096, 64, "one")]
+         (700, 2, 2, 544, 80, "twice"), (513, 4, 1, 4096, 64, "one"),
+         # fewer rows than experts, then enough tiles for the chip of 128 and of 256 rows
+         (20, 64, 2, 256, 64, "random"), (30, 40, 4, 1056, 48, "twice"), (600, 8, 2, 96, 2064, "padded"),
+         (1500, 3, 2, 160, 4112, "random")]
 
 
 def groups_of(e, E):

@@ -101,7 +101,9 @@ SIZES = [(1, 32, 16), (1, 2048, 2048), (2, 96, 48), (3, 128, 32), (5, 160, 80), 
          (200, 4096, 272), (257, 1152, 304), (300, 14336, 32), (511, 64, 16), (513, 544, 1040),
          # few rows over much to read, K split between workgroups, tiles of 128 and 256 rows
          (33, 8224, 2080), (40, 28672, 656), (96, 16416, 1056), (130, 14368, 1200), (200, 8192, 2128), (700, 1056, 3600),
-         (1030, 14336, 560), (1300, 544, 7056), (2100, 16448, 400)]
+         (1030, 14336, 560), (1300, 544, 7056), (2100, 16448, 400), (1800, 16448, 2064),
+         # 16 and 32 rows a workgroup
+         (3, 8192, 16400), (11, 4096, 6400), (40, 256, 4112), (100, 160, 2064), (27, 1056, 8208)]
 
 
 @pytest.mark.parametrize("M,K,N", SIZES)
