@@ -18,7 +18,12 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr uint32_t kOutside = 0x80000000u;  // a buffer offset past every operand (they stay below 2 GiB or 4 GiB - 2 GiB)
+// A lane offset past the end of every buffer of activations (they stay below 2 GiB):
+// such a load gives zeros.  The uniform offset beside it may not count in the range
+// check: it stays inside the buffer, and is 0 where all lanes are outside.  (Of a
+// matrix of more than 2 GiB the load reads other codes of it, which then meet rows
+// of zeros or none.)
+constexpr uint32_t kOutside = 0x80000000u;
 
 // c += W (16 columns x 128) . A (16 rows x 128); byte J of the weights' scale word, JA of the rows'
 template <int J, int JA = J>
@@ -209,7 +214,8 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t g = (uint32_t)(c * U + u);
-        s.w[u][nt] = buffer_load_x4(up ? rw1 : rw0, g < (uint32_t)a.G ? (uint32_t)lane * 16u : kOutside, (t * a.G + g) * 1024u);
+        const bool in = g < (uint32_t)a.G;
+        s.w[u][nt] = buffer_load_x4(up ? rw1 : rw0, in ? (uint32_t)lane * 16u : kOutside, in ? (t * a.G + g) * 1024u : 0u);
       }
       s.ws[nt] = buffer_load_x1(up ? rs1 : rs0, (uint32_t)lane * 4u, (t * a.G4 + (uint32_t)(c * U / 4)) * 256u);
     }
@@ -242,13 +248,13 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t g = (uint32_t)(c * U + u);
+        const uint32_t g = (uint32_t)(c * U + u), at = g < (uint32_t)a.G ? g : 0u;
         if constexpr (RAW) {
           const uint32_t v = (int)(4 * g) + kq < a.blocks ? va[mt] : kOutside;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) s.x[u][mt][q] = buffer_load_x4(ra, v, g * 256u + 16u * q);
+          for (int q = 0; q < 4; ++q) s.x[u][mt][q] = buffer_load_x4(ra, v, at * 256u + 16u * q);
         } else {
-          s.x[u][mt][0] = buffer_load_x4(ra, g < (uint32_t)a.G ? va[mt] : kOutside, g * 64u);
+          s.x[u][mt][0] = buffer_load_x4(ra, g < (uint32_t)a.G ? va[mt] : kOutside, at * 64u);
         }
       }
       if constexpr (!RAW) s.xs[mt] = buffer_load_x1(ras, vs[mt], (uint32_t)(c * U / 4) * 16u);
@@ -410,7 +416,8 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   // load i of the rows' groups 2 p and 2 p + 1, of the weights' group g, of the
   // scales of groups 4 c .. 4 c + 3; nothing past the last group
   auto load_rows = [&](int i, int p) {
-    buffer_load_lds16(ra, 2 * p < G ? va[i] : kOutside, (uint32_t)(p + 2 * first) * 128u,
+    const bool in = 2 * p < G;
+    buffer_load_lds16(ra, in ? va[i] : kOutside, in ? (uint32_t)(p + 2 * first) * 128u : 0u,
                       ax_lds + (uint32_t)(p & 1) * (TM * 128u) + (uint32_t)(wave * kA + i) * 1024u);
   };
   auto load_weights = [&](int i, int g) {
@@ -421,7 +428,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   auto load_scale = [&](int i, int c) {
     const bool in = c < G4;
     if (i < AT / 4)
-      buffer_load_lds4(ras, in ? vs[i] : kOutside, (uint32_t)(c + first) * 16u, sc_lds + (uint32_t)(wave * (AT / 4) + i) * 256u);
+      buffer_load_lds4(ras, in ? vs[i] : kOutside, in ? (uint32_t)(c + first) * 16u : 0u, sc_lds + (uint32_t)(wave * (AT / 4) + i) * 256u);
     else
       buffer_load_lds4(is_up(i - AT / 4) ? rs1 : rs0, in ? (uint32_t)lane * 4u : kOutside,
                        in ? (wt[i - AT / 4] * a.G4 + c + first) * 256u : 0u, sc_lds + (uint32_t)(AT + wave * kW + i - AT / 4) * 256u);
@@ -450,8 +457,9 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   f32x16 acc[kMP][kNP];
   // First what needs no list of rows, behind the list itself (through LDS: the
   // wait for it then leaves the weights on their way).
+  const int mine = wave * (TM / 4) + lane;
   if (a.rows)
-    buffer_load_lds4(raw_rsrc(a.rows, (uint32_t)a.M * 4u), (uint32_t)lane * 4u, (uint32_t)(b.m0 + wave * (TM / 4)) * 4u,
+    buffer_load_lds4(raw_rsrc(a.rows, (uint32_t)a.M * 4u), mine < b.n ? (uint32_t)(b.m0 + mine) * 4u : kOutside, 0u,
                      lds_address(&row_list[wave][0]));
 #pragma unroll
   for (int i = 0; i < 2 * kW; ++i) load_weights(i % kW, i / kW);
@@ -461,7 +469,6 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   }
   // lane m: the activation row of row m of this wave's quarter; -1: none, or the
   // caller's list is wrong
-  const int mine = wave * (TM / 4) + lane;
   int src = lane < TM / 4 && mine < b.n ? b.m0 + mine : -1;
   if (a.rows && src >= 0) {
     const uint32_t r = row_list[wave][lane];
