@@ -9,6 +9,7 @@
 #include "ss_device.h"
 #include "ss_internal.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace ss {
@@ -631,11 +632,11 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
 
 // ---------------------------------------------------------------- combine
 // One thread per 4 columns of a token; the addends in slot order, KU of them
-// loaded at a time.  Nothing is written where the offsets were invalid (map[0]).
+// loaded at a time, each the sum of `split` parts in order.  Nothing is written where the offsets were invalid (map[0]).
 // Bound by the fp32 rows that it reads: 5000 tokens of 8 slots (10 % of them masked)
 // x 2048 columns, 295 MB, 50 us (5.9 TB/s).
 template <int KU>
-__global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restrict__ part, int T, int k, int N,
+__global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restrict__ part, int split, int T, int k, int N,
                                                           const int32_t* __restrict__ pos,
                                                           const int32_t* __restrict__ map,
                                                           const float* __restrict__ weights, uint16_t* y, int64_t ldy,
@@ -674,6 +675,7 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restric
 #pragma unroll
     for (int j = 0; j < KU; ++j)
       if (p[j] >= 0) {
+        for (int s = 1; s < split; ++s) o[j] += *reinterpret_cast<const f32x4*>(part + ((int64_t)s * T * k + p[j]) * N + n);
 #pragma unroll
         for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(w[j], o[j][c], v[c]);
       }
@@ -731,6 +733,12 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
   const int G4 = (mx4_groups(K) + 3) / 4;
   const int64_t weights = (int64_t)(E < M ? E : M) * K * N / 2 * (swiglu ? 2 : 1);  // bytes that are read, at most
   auto plan = [](Form f, int split = 1) { return Plan{f, kRowsOf[f], split}; };
+  // shares of K that bring the tiles to one for each compute unit, each of at least
+  // `least` scale words (four groups each)
+  auto split_of = [&](int64_t tiles, int least) {
+    const int64_t want = 256 / tiles, most = G4 / least;
+    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+  };
   // One launch, but more registers and work in it: 8 rows of 8192 x 8192 12.4
   // against 13.1, 1 row 10.8 against 11.9; of 8192 x 28672 (112 MB) 37.0 against 26.9.
   // Up to a whole block of rows where there is little to read (16 of 4096 x 4096 8.3
@@ -745,9 +753,11 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
     // against 15.8).
     if (M < (K <= 1024 ? 1 : 4) * (int64_t)E) return plan(STREAM_1);
     // Larger tiles as long as there are enough of them for the chip (blocks of
-    // rows: an expert's last is half full).
+    // rows: an expert's last is half full): down 5536 x 864, 10 experts of 899 rows,
+    // 160 tiles of 256 rows 72.5 against 78.3; 8192 x 2048, 8 experts of 200 rows, 80
+    // of them 62.7 against 54.5, and 160 tiles of 128 rows 54.5 against 49.5 with 64.
     auto enough = [&](Form f) {
-      return (M / kRowsOf[f] + (E < M ? E : M) / 2) * (int64_t)((N * (swiglu ? 2 : 1) + kColumnsOf[f] - 1) / kColumnsOf[f]) >= 200;
+      return (M / kRowsOf[f] + (E < M ? E : M) / 2) * (int64_t)((N * (swiglu ? 2 : 1) + kColumnsOf[f] - 1) / kColumnsOf[f]) >= (f == TILE_256 ? 160 : 200);
     };
     // 64 rows: 64 against 128 rows a tile 43.9 and 47.3 (64 experts 2048 x 1024);
     // 128 rows: 60.0 and 57.5.  256 against 128 rows a tile (64 experts): SwiGLU
@@ -755,16 +765,14 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
     // 316; down 1024 x 2048 of 384 rows 132 and 128, 768 rows 234 and 241; over a
     // long K (8 experts, down 14336 x 4096) of 192 rows 111 and 133.
     if (avg >= (K >= 8192 ? 192 : 512) && enough(TILE_256)) return plan(TILE_256);
-    return plan(avg >= 96 && enough(TILE_128) ? TILE_128 : TILE_64);
+    const Form f = avg >= 96 && enough(TILE_128) ? TILE_128 : TILE_64;
+    // K in shares where tiles are few, and the combination adds their sums: 28 rows
+    // of 6 experts 4544 x 1120 16.6 against 14.3, 400 of 8 experts 14336 x 1024 41.8
+    // against 36.0.
+    return plan(f, swiglu ? 1 : split_of((int64_t)std::max(std::min(E, M), M / kRowsOf[f] + std::min(E, M) / 2) * ((N + 127) / 128), 2));
   }
   if (M <= 16) return plan(STREAM_1);
   auto tiles = [&](Form f) { return (int64_t)((M + kRowsOf[f] - 1) / kRowsOf[f]) * ((N + kColumnsOf[f] - 1) / kColumnsOf[f]); };
-  // shares of K that bring a form's tiles to one for each compute unit, each of at
-  // least `least` scale words (four groups each)
-  auto split_of = [&](Form f, int least) {
-    const int64_t want = 256 / tiles(f), most = G4 / least;
-    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
-  };
   // Few rows or little to read: 128 rows of 4096 x 4096 14.3 against 14.8, 32 of
   // 8192 x 8192 15.3 against 21; but 28672 x 8192 39.2 against 31.6, 8192 x 28672
   // 38.5 against 35.
@@ -777,14 +785,14 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
   // 8192 x 8192 26.5 against 32.1; of 4096 x 4096 16.0 against 17.8), over a long K
   // only few of them (14336 x 4096: 128 rows 22.3 against 23.3, 256 rows 30.7
   // against 26.9).
-  if (M <= 64 || (M <= 512 && tiles(TILE_64) <= (K <= 8192 ? 256 : 64))) return plan(TILE_64, split_of(TILE_64, 2));
+  if (M <= 64 || (M <= 512 && tiles(TILE_64) <= (K <= 8192 ? 256 : 64))) return plan(TILE_64, split_of(tiles(TILE_64), 2));
   // 256-row tiles where they nearly fill the chip (384 rows of 8192 x 28672, 224
   // tiles: 66 against 75; 192 rows, 112 tiles: 55 against 51), over a long K with
   // two shares or more (28672 x 8192: 1024 rows 141 against 158).
   const int64_t big = tiles(TILE_256);
   if (M > 192 && (big >= 160 || (K >= 14336 && big >= 96) || (K >= 16384 && big >= 64)))
-    return plan(TILE_256, K >= 14336 ? split_of(TILE_256, 14) : 1);
-  return plan(TILE_128, split_of(TILE_128, 2));
+    return plan(TILE_256, K >= 14336 ? split_of(tiles(TILE_256), 14) : 1);
+  return plan(TILE_128, split_of(tiles(TILE_128), 2));
 }
 
 template <Mx4Epilogue EPI>
@@ -803,7 +811,7 @@ void launch_form(const Plan& p, const Mx4Args& a, int blocks, hipStream_t st) {
 
 }  // namespace
 
-void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
+int launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   // rows that the product may read itself: within a 2 GiB buffer, not overwritten
   const uint64_t x_bytes = ((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2;
   const Plan p = plan_of(L.M, L.E, L.K, L.N, L.epi == MX4_SWIGLU, L.offsets, x_bytes < kOutside && !L.x_written);
@@ -866,6 +874,7 @@ void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   } else {
     launch_form<MX4_PLAIN>(p, a, map.blocks, st);
   }
+  return p.split;
 }
 
 bool mx4_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped) {
@@ -895,13 +904,23 @@ size_t mx4_part_bytes_most(int M, int K, int N) {
   return a > b ? a : b;
 }
 
-void launch_moe_combine(const float* part, int T, int k, int N, const int32_t* pos, const int32_t* map,
+size_t mx4_rows_bytes(int M, int E, int K, int N) {
+  return (size_t)plan_of(M, E, K, N, false, true, false).split * M * N * sizeof(float);
+}
+
+size_t mx4_rows_bytes_most(int64_t M, int K, int N) {
+  // one part, or as many as plan_of allows of at most 256 tiles
+  const size_t one = (size_t)M * N * sizeof(float), all = std::max<int64_t>((mx4_groups(K) + 3) / 4 / 2, 1) * one;
+  return std::max(one, std::min(all, (size_t)256 * 128 * 128 * sizeof(float)));
+}
+
+void launch_moe_combine(const float* part, int split, int T, int k, int N, const int32_t* pos, const int32_t* map,
                         const float* weights, uint16_t* y, int64_t ldy, const uint16_t* res, int64_t ldr, void* ws,
                         hipStream_t st) {
   const dim3 grid((unsigned)(((int64_t)T * (N / 4) + 255) / 256));
-  if (k <= 2) hipLaunchKernelGGL(moe_combine_kernel<2>, grid, dim3(256), 0, st, part, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
-  else if (k <= 4) hipLaunchKernelGGL(moe_combine_kernel<4>, grid, dim3(256), 0, st, part, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
-  else hipLaunchKernelGGL(moe_combine_kernel<8>, grid, dim3(256), 0, st, part, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
+  if (k <= 2) hipLaunchKernelGGL(moe_combine_kernel<2>, grid, dim3(256), 0, st, part, split, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
+  else if (k <= 4) hipLaunchKernelGGL(moe_combine_kernel<4>, grid, dim3(256), 0, st, part, split, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
+  else hipLaunchKernelGGL(moe_combine_kernel<8>, grid, dim3(256), 0, st, part, split, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
 }
 
 }  // namespace ss

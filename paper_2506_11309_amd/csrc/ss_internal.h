@@ -198,11 +198,14 @@ size_t mx4_part_bytes(int M, int K, int N);
 size_t mx4_part_bytes_most(int M, int K, int N);
 // whether a product's launch has fewer than 2^32 threads
 bool mx4_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped);
-// quantises the activations, then multiplies
-void launch_mx4_gemm(const Mx4Launch& L, hipStream_t st);
-// y[t] = fp16(res[t] + sum over j < k with pos[t][j] >= 0 of weights[t][j] part[pos[t][j]]);
-// map as the product's launch left it
-void launch_moe_combine(const float* part, int T, int k, int N, const int32_t* pos, const int32_t* map,
+// of the fp32 rows of an experts' product (ROWS), exactly, and the most of up to M rows
+size_t mx4_rows_bytes(int M, int E, int K, int N);
+size_t mx4_rows_bytes_most(int64_t M, int K, int N);
+// quantises the activations, then multiplies; the parts [M][N] that ROWS left
+int launch_mx4_gemm(const Mx4Launch& L, hipStream_t st);
+// y[t] = fp16(res[t] + sum over j < k with pos[t][j] >= 0 of weights[t][j] part[pos[t][j]]),
+// part the sum of `split` parts [T k][N] in order; map as the product's launch left it
+void launch_moe_combine(const float* part, int split, int T, int k, int N, const int32_t* pos, const int32_t* map,
                         const float* weights, uint16_t* y, int64_t ldy, const uint16_t* res, int64_t ldr, void* ws,
                         hipStream_t st);
 

@@ -737,7 +737,7 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
 size_t swiftspec_moe_mx4_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
   if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1) return kHeader;
   const int64_t pairs = (int64_t)T * k;
-  return mx4_ws(pairs, pairs, E, K, (size_t)pairs * N * sizeof(float)).total;
+  return mx4_ws(pairs, pairs, E, K, ss::mx4_rows_bytes_most(pairs, K, N)).total;
 }
 
 int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
@@ -756,7 +756,7 @@ int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t l
   if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
   if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
   if (groups->T == 0) return SWIFTSPEC_OK;
-  const Mx4Ws w = mx4_ws(pairs, pairs, Wd->E, Wd->K, (size_t)pairs * Wd->N * sizeof(float));
+  const Mx4Ws w = mx4_ws(pairs, pairs, Wd->E, Wd->K, ss::mx4_rows_bytes((int)pairs, Wd->E, Wd->K, Wd->N));
   if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   uint8_t* base = static_cast<uint8_t*>(ws);
   float* part = reinterpret_cast<float*>(base + w.part);
@@ -778,8 +778,8 @@ int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t l
   L.map = reinterpret_cast<int32_t*>(base + w.map);
   L.part = part;
   L.ws = ws;
-  ss::launch_mx4_gemm(L, st);
-  ss::launch_moe_combine(part, groups->T, groups->k, Wd->N, groups->pos, L.map, d_weights, y, ldy,
+  const int split = ss::launch_mx4_gemm(L, st);
+  ss::launch_moe_combine(part, split, groups->T, groups->k, Wd->N, groups->pos, L.map, d_weights, y, ldy,
                          residual, ldr, ws, st);
   return check_launch();
 }
