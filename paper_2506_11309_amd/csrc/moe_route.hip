@@ -12,8 +12,8 @@
 // Bound by latency: launches, dependent reads, k rounds of row maxima.  64 tokens,
 // 8 of 64 experts: 4.6 us in one launch; 16000 tokens, 8 of 256 (8 MB of scores):
 // 7.7 us to choose and count, 7.3 us to place.
-#include "ss_device.h"
-#include "ss_internal.h"
+#include "mx4_device.h"
+#include "mx4_internal.h"
 
 namespace ss {
 

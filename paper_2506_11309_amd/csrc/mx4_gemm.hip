@@ -6,8 +6,8 @@
 // kq*16 + i takes the 32 codes of row i in k block kq and that block's scale
 // byte.  The weights are its first operand, so that a lane ends up with four
 // consecutive columns of one output row.
-#include "ss_device.h"
-#include "ss_internal.h"
+#include "mx4_device.h"
+#include "mx4_internal.h"
 
 #include <algorithm>
 #include <type_traits>

@@ -10,8 +10,8 @@
 // a is found on the fp16 bits (an unsigned maximum of magnitudes), its
 // exponent is exact in fp32, and the conversion instruction rounds as above
 // for every fp16 value, subnormals included.
-#include "ss_device.h"
-#include "ss_internal.h"
+#include "mx4_device.h"
+#include "mx4_internal.h"
 
 namespace ss {
 

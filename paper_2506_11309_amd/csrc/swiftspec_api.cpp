@@ -9,6 +9,7 @@
 #include <new>
 
 #include "../../include/swiftspec.h"
+#include "mx4_internal.h"
 #include "ss_internal.h"
 
 namespace {
