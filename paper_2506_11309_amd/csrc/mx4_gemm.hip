@@ -49,7 +49,7 @@ struct Mx4Args {
   int G, G4, Nt, N;
   const uint8_t *a, *as;
   uint32_t a_bytes, as_bytes;
-  int M, a_rows;
+  int M;
   const int32_t* map;   // {expert, first row, rows, 0} per row block, or null
   const int32_t* rows;
   int div;
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int rb = blockIdx.x / a.col_blocks, cb = blockIdx.x - rb * a.col_blocks;
-  // RAW: at most 64 rows, whose list is read beside the offsets
+  // RAW: at most 16 rows, whose list is read beside the offsets
   const int listed = RAW && a.rows && lane < a.M ? a.rows[lane] : 0;
   const RowBlock b = RAW ? find_block(a, rb, 16 * MT, blockIdx.x == 0 && wave == 0) : row_block(a, rb, 16 * MT);
   if (b.n <= 0) return;
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
     }
   };
   auto multiply = [&](Stage& s, int c) {
-    const int sh = U == 4 ? 0 : 8 * ((c * U) & 3);
+    const int sh = 8 * ((c * U) & 3);  // this chunk's bytes of its scale words
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) s.ws[nt] >>= sh;
     if constexpr (!RAW) {
