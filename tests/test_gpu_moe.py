@@ -110,7 +110,9 @@ CASES = [(1, 1, 1, 32, 16, "random"), (1, 8, 2, 256, 48, "random"), (1, 64, 8, 2
          (700, 2, 2, 544, 80, "twice"), (513, 4, 1, 4096, 64, "one"),
          # fewer rows than experts, then enough tiles for the chip of 128 and of 256 rows
          (20, 64, 2, 256, 64, "random"), (30, 40, 4, 1056, 48, "twice"), (600, 8, 2, 96, 2064, "padded"),
-         (1500, 3, 2, 160, 4112, "random")]
+         (1500, 3, 2, 160, 4112, "random"),
+         # one slot a token: 64, 128 and 256 rows a tile
+         (200, 5, 1, 256, 80, "padded"), (700, 6, 1, 96, 4112, "padded"), (2000, 3, 1, 64, 5136, "padded")]
 
 
 def groups_of(e, E):
