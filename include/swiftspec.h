@@ -524,12 +524,13 @@ typedef struct {
  * the k.  A score of -inf or NaN is masked: it has no probability and is never
  * chosen; slots left without an expert (a token of padding) get expert -1,
  * weight 0 and no place in a group.  +inf counts as 65504.  Then the groups, as
- * swiftspec_moe_group makes them.  logits 2-byte aligned, ldl >= E. */
+ * swiftspec_moe_group makes them.  logits 2-byte, ws 8-byte aligned, ldl >= E. */
 int swiftspec_moe_route(const uint16_t* logits, int32_t ldl, int32_t renormalize, int32_t* d_experts,
                         float* d_weights, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
                         void* stream);
 /* The groups of experts that were chosen otherwise: d_experts [T][k]; an index
- * outside [0, E) means no expert, one that a token names twice counts twice. */
+ * outside [0, E) means no expert, one that a token names twice counts twice.
+ * ws 8-byte aligned. */
 int swiftspec_moe_group(const int32_t* d_experts, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
                         void* stream);
 size_t swiftspec_moe_route_workspace_bytes(int32_t T, int32_t E, int32_t k);

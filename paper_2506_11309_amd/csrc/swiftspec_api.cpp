@@ -372,7 +372,7 @@ int check_groups(const swiftspec_moe_groups* g) {
 
 int run_route(ss::RouteLaunch& L, const swiftspec_moe_groups* g, void* ws, size_t ws_bytes, hipStream_t st) {
   if (!ws) return SWIFTSPEC_INVALID_ARG;
-  if (!aligned4(ws)) return SWIFTSPEC_MISALIGNED;
+  if (!aligned8(ws)) return SWIFTSPEC_MISALIGNED;  // the counts are read eight bytes at a time
   if (ws_bytes < kHeader + align_up(ss::route_hist_bytes(g->T, g->E, g->k))) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   L.T = g->T;
   L.E = g->E;
