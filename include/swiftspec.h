@@ -462,7 +462,9 @@ int swiftspec_greedy_accept(const uint16_t* logits, int32_t ldl, int32_t T, int3
  * K % 32 == 0 (K is padded to whole groups of 128 in the packed copy),
  * N % 16 == 0, 1 <= E <= SWIFTSPEC_MAX_EXPERTS, one matrix's packed copy below
  * 4 GiB and all of them below 64 GiB; a product whose launch would need 2^32
- * threads or more is refused (UNSUPPORTED in each case).
+ * threads or more is refused (UNSUPPORTED in each case).  For sizes that the
+ * calls refuse for these limits, packed_bytes is 0 and a workspace query answers
+ * the header alone.
  * Products take fp16 activations and quantise them by the same blocks first:
  * both operands are in 4 bits, the sums in fp32. */
 typedef struct {

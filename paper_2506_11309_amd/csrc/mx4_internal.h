@@ -12,7 +12,7 @@ namespace ss {
 //            scales [E][N/16][ceil(G/4)][64 lanes] u32, byte j = group 4 g4 + j;
 //   activations: codes [M][G] x 64 bytes (row-major, so that an expert's rows
 //            can be gathered), scales [M][ceil(G/4)][4 kq] u32, bytes as above.
-inline int mx4_groups(int K) { return (K + 127) / 128; }
+inline int mx4_groups(int K) { return (int)(((int64_t)K + 127) / 128); }
 inline size_t mx4_code_bytes(int64_t M, int K) { return (size_t)M * mx4_groups(K) * 64; }
 inline size_t mx4_scale_bytes(int64_t M, int K) { return (size_t)M * ((mx4_groups(K) + 3) / 4) * 16; }
 inline size_t mx4_packed_bytes(int K, int N, int E) {
@@ -38,7 +38,7 @@ struct Mx4Map {
   void* ws;
 };
 // the most blocks of tm rows that M rows of E experts can make
-inline int mx4_row_blocks(int M, int E, int tm) { return M / tm + (E < M ? E : M); }
+inline int mx4_row_blocks(int M, int E, int tm) { return M / tm + (E < M ? E : M); }  // M < 2^28
 inline size_t mx4_map_bytes(int M, int E) { return ((size_t)mx4_row_blocks(M, E, 16) + 1) * 16; }
 // x [M][ldx] fp16 -> the activations' operand form; with experts whose rows are
 // in order (last not null) only the first last[E] rows
@@ -94,7 +94,7 @@ struct RouteLaunch {
   int32_t *offsets, *rows, *pos;
   uint16_t* hist;  // route_hist_bytes
 };
-size_t route_hist_bytes(int T, int E, int k);
+size_t route_hist_bytes(int T, int E, int k);  // T k < 2^28
 void launch_moe_route(const RouteLaunch& L, hipStream_t st);
 
 }  // namespace ss

@@ -317,13 +317,23 @@ size_t layer_ws_query(const swiftspec_dims* d, int T) {
 }
 
 // ---- microscaled 4-bit matrices
+// Positive sizes that the calls take, before their divisibility; outside them
+// the size queries answer as if there were nothing to do, and their arithmetic
+// would not fit its types.
+bool mx4_matrices_fit(int K, int N, int E) {
+  if (E > SWIFTSPEC_MAX_EXPERTS) return false;
+  // the kernels address one matrix through a 32-bit buffer range
+  if (ss::mx4_packed_bytes(K, N, 1) > 0xFFFFFFFFull) return false;
+  // a launch has fewer than 2^32 threads
+  return ss::mx4_packed_bytes(K, N, E) < 1ull << 36;
+}
+bool groups_fit(int T, int k, int E) {
+  return E <= SWIFTSPEC_MAX_EXPERTS && k <= SWIFTSPEC_MAX_TOPK && (int64_t)T * k < (1 << 28);
+}
+
 int check_mx4_shape(const swiftspec_mx4* W) {
   if (!W || W->K <= 0 || W->N <= 0 || W->E <= 0) return SWIFTSPEC_INVALID_ARG;
-  if (W->K % 32 || W->N % 16 || W->E > SWIFTSPEC_MAX_EXPERTS) return SWIFTSPEC_UNSUPPORTED;
-  // the kernels address one matrix through a 32-bit buffer range
-  if (ss::mx4_packed_bytes(W->K, W->N, 1) > 0xFFFFFFFFull) return SWIFTSPEC_UNSUPPORTED;
-  // a launch has fewer than 2^32 threads
-  if (ss::mx4_packed_bytes(W->K, W->N, W->E) >= 1ull << 36) return SWIFTSPEC_UNSUPPORTED;
+  if (W->K % 32 || W->N % 16 || !mx4_matrices_fit(W->K, W->N, W->E)) return SWIFTSPEC_UNSUPPORTED;
   return SWIFTSPEC_OK;
 }
 
@@ -364,7 +374,7 @@ Mx4Ws mx4_ws(int64_t a_rows, int64_t M, int E, int K, size_t part) {
 
 int check_groups(const swiftspec_moe_groups* g) {
   if (!g || g->T < 0 || g->E < 1 || g->k < 1 || g->k > g->E) return SWIFTSPEC_INVALID_ARG;
-  if (g->E > SWIFTSPEC_MAX_EXPERTS || g->k > SWIFTSPEC_MAX_TOPK || (int64_t)g->T * g->k >= (1 << 28)) return SWIFTSPEC_UNSUPPORTED;
+  if (!groups_fit(g->T, g->k, g->E)) return SWIFTSPEC_UNSUPPORTED;
   if (!g->offsets || (g->T > 0 && (!g->rows || !g->pos))) return SWIFTSPEC_INVALID_ARG;
   if (!aligned4(g->offsets) || !aligned4(g->rows) || !aligned4(g->pos)) return SWIFTSPEC_MISALIGNED;
   return SWIFTSPEC_OK;
@@ -569,7 +579,7 @@ int swiftspec_rmsnorm_w4a16_swiglu(const swiftspec_w4* Wg, const swiftspec_w4* W
 // ---- microscaled 4-bit matrices and mixtures of experts
 
 size_t swiftspec_mx4_packed_bytes(int32_t K, int32_t N, int32_t E) {
-  if (K <= 0 || N <= 0 || E <= 0) return 0;
+  if (K <= 0 || N <= 0 || E <= 0 || !mx4_matrices_fit(K, N, E)) return 0;
   return ss::mx4_packed_bytes(K, N, E);
 }
 
@@ -614,7 +624,7 @@ int swiftspec_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_
 }
 
 size_t swiftspec_mx4_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N) {
-  if (M < 1 || K < 1 || N < 1) return kHeader;
+  if (M < 1 || K < 1 || N < 1 || !mx4_matrices_fit(K, N, 1) || !mx4_rows_fit(M, K)) return kHeader;
   return mx4_ws(M, M, 0, K, ss::mx4_part_bytes_most(M, K, N)).total;
 }
 
@@ -657,7 +667,7 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
 }
 
 size_t swiftspec_moe_route_workspace_bytes(int32_t T, int32_t E, int32_t k) {
-  if (T < 1 || E < 1 || k < 1 || k > SWIFTSPEC_MAX_TOPK) return kHeader;
+  if (T < 1 || E < 1 || k < 1 || !groups_fit(T, k, E)) return kHeader;
   return kHeader + align_up(ss::route_hist_bytes(T, E, k));
 }
 
@@ -689,7 +699,8 @@ int swiftspec_moe_group(const int32_t* d_experts, const swiftspec_moe_groups* gr
 }
 
 size_t swiftspec_moe_mx4_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
-  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1) return kHeader;
+  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1 || !groups_fit(T, k, E) || !mx4_matrices_fit(K, N, E)) return kHeader;
+  if (!mx4_rows_fit(T, K)) return kHeader;
   return mx4_ws(T, (int64_t)T * k, E, K, 0).total;
 }
 
@@ -736,8 +747,9 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
 }
 
 size_t swiftspec_moe_mx4_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
-  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1) return kHeader;
+  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1 || !groups_fit(T, k, E) || !mx4_matrices_fit(K, N, E)) return kHeader;
   const int64_t pairs = (int64_t)T * k;
+  if (!mx4_rows_fit(pairs, K)) return kHeader;
   return mx4_ws(pairs, pairs, E, K, ss::mx4_rows_bytes_most(pairs, K, N)).total;
 }
 

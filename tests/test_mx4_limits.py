@@ -23,3 +23,35 @@ def test_router_workspace_alignment(ss):  # noqa: F811
     for off in (0, 8):  # aligned enough: the next check answers
         assert status(lib, "moe_route", FAKE, 8, 1, FAKE, FAKE, groups(ss), FAKE + off, small) == ss.WORKSPACE_TOO_SMALL
         assert status(lib, "moe_group", FAKE, groups(ss), FAKE + off, small) == ss.WORKSPACE_TOO_SMALL
+
+
+def test_size_queries_outside_what_the_calls_take(ss):  # noqa: F811
+    """Sizes that no call takes, up to the largest 32-bit numbers, get no packed
+    bytes and a workspace of the header alone; the largest that they do take get
+    their size, whose parts pass 32 bits."""
+    lib, top, head = ss.lib(), 2**31 - 1, ss.WS_HEADER_BYTES
+    packed = lambda K, N, E: E * N * (-(-K // 128) * 64 + -(-K // 512) * 16)  # noqa: E731
+    for K, N, E in ((65536, 65536, 1), (2**22 - 32, 1600, 8), (128, 32 * 2**20, 17), (top // 32 * 32, 16 * 2, 0), (4096, 14336, 512)):
+        want = packed(K, N, E) if E else 0
+        assert lib.swiftspec_mx4_packed_bytes(K, N, E) == want < 2**36
+    for K, N, E in ((top, 16, 1), (top // 32 * 32, 16, 1), (128, top, 1), (128, top // 16 * 16, 512), (top, top, 1), (top, top, top),
+                    (131072, 131072, 1), (128, 16, 513), (128, 16, top), (65536, 4096, 512), (0, 16, 1), (128, -16, 1)):
+        assert lib.swiftspec_mx4_packed_bytes(K, N, E) == 0, (K, N, E)
+    up = lambda n: -(-n // 256) * 256  # noqa: E731
+    rows = 2**25 - 1  # of 128 columns: just below 2 GiB
+    assert lib.swiftspec_mx4_gemm_workspace_bytes(rows, 128, 16) == head + up(rows * 64) + up(rows * 16)
+    for M, K, N in ((rows + 1, 128, 16), (top, 128, 16), (1, top, 16), (top, top, top), (16, top // 32 * 32, 16), (1, 128, top), (-1, 128, 16)):
+        assert lib.swiftspec_mx4_gemm_workspace_bytes(M, K, N) == head, (M, K, N)
+    # 256 units and more, of 65535 / k tokens; E rounded up to 4
+    assert lib.swiftspec_moe_route_workspace_bytes(2**28 - 1, 5, 1) == head + up(-(-(2**28 - 1) // 65535) * 8 * 2)
+    assert lib.swiftspec_moe_route_workspace_bytes(2**24 - 1, 512, 16) == head + up(-(-(2**24 - 1) // 4095) * 512 * 2)
+    for T, E, k in ((2**28, 5, 1), (top, 5, 1), (top, 512, 16), (2**24, 512, 16), (4, 513, 1), (4, top, 2), (4, 64, 17), (4, 64, top)):
+        assert lib.swiftspec_moe_route_workspace_bytes(T, E, k) == head, (T, E, k)
+    swiglu, down = lib.swiftspec_moe_mx4_swiglu_workspace_bytes, lib.swiftspec_moe_mx4_down_workspace_bytes
+    T = 2**24 - 1
+    assert swiglu(T, 16, 512, 128, 16) == head + up(T * 64) + up(T * 16) + up((T + 512 + 1) * 16)
+    assert down(T, 2, 512, 128, 16) == head + up(2 * T * 64) + up(2 * T * 16) + up((2 * T // 16 + 512 + 1) * 16) + up(2 * T * 64)
+    for T, k, E, K, N in ((2**28, 1, 8, 128, 16), (top, 16, 512, 128, 16), (top, top, top, top, top), (1, 1, 1, top, 16), (4, 2, 513, 128, 16),
+                          (4, 17, 64, 128, 16), (4, 2, 8, 128, top), (2**25, 1, 8, 128, 16), (4, 2, 512, 65536, 4096)):
+        assert swiglu(T, k, E, K, N) == down(T, k, E, K, N) == head, (T, k, E, K, N)
+    assert down(2**24, 2, 8, 128, 16) == head < swiglu(2**24, 2, 8, 128, 16)  # its rows are the pairs
