@@ -542,7 +542,7 @@ size_t swiftspec_moe_route_workspace_bytes(int32_t T, int32_t E, int32_t k);
  *   h[i][n] = fp16( silu(Q(x[t]) . Wg'[e][n]) * (Q(x[t]) . Wu'[e][n]) )
  * (Q, sums and alignment as swiftspec_mx4_gemm; x [T][ldx], h [T k][ldh]; Wg and
  * Wu share K, N and E = groups->E).  Rows of h past offsets[E] are left as they
- * were.  h must not overlap x.  Offsets that do not ascend from 0 to at most T k
+ * were.  h may overlap x.  Offsets that do not ascend from 0 to at most T k
  * set SWIFTSPEC_DEVERR_BAD_GROUPS and nothing is written; a row outside
  * [0, T k) sets it and its row of h is not written. */
 int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, const uint16_t* x, int32_t ldx,

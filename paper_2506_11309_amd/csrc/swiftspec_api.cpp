@@ -96,14 +96,14 @@ struct NormIn {
   float eps;
 };
 
-// whether a row of a [M][lda] (na elements) and one of b [M][ldb] (nb) share memory
-bool rows_overlap(const uint16_t* a, int lda, int na, const uint16_t* b, int ldb, int nb, int M) {
+// whether a row of a [Ma][lda] (na elements) and one of b [Mb][ldb] (nb) share memory
+bool rows_overlap(const uint16_t* a, int lda, int na, int Ma, const uint16_t* b, int ldb, int nb, int Mb) {
   const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
   const auto row = [](uintptr_t p, int ld, int m) { return p + (uintptr_t)m * ld * sizeof(uint16_t); };
   const uintptr_t ab = (uintptr_t)na * sizeof(uint16_t), bb = (uintptr_t)nb * sizeof(uint16_t);
-  if (row(a0, lda, M - 1) + ab <= b0 || row(b0, ldb, M - 1) + bb <= a0) return false;
-  for (int i = 0; i < M; ++i)
-    for (int j = 0; j < M; ++j)
+  if (row(a0, lda, Ma - 1) + ab <= b0 || row(b0, ldb, Mb - 1) + bb <= a0) return false;
+  for (int i = 0; i < Ma; ++i)
+    for (int j = 0; j < Mb; ++j)
       if (row(a0, lda, i) < row(b0, ldb, j) + bb && row(b0, ldb, j) < row(a0, lda, i) + ab) return true;
   return false;
 }
@@ -115,7 +115,7 @@ bool rows_overlap(const uint16_t* a, int lda, int na, const uint16_t* b, int ldb
 bool norm_in_gemm(const swiftspec_w4* W0, bool swiglu, const NormIn& n, int M, const uint16_t* y, int ldy) {
   ss::GemmPlan p = ss::plan_w4a16_gemm(M, W0->K, W0->N, swiglu);
   return ss::norm_in_ksplit(p, M, W0->K, W0->N, swiglu) && (uint64_t)n.ldx * 32 <= 0xFFFFFFFFull &&
-         !rows_overlap(n.x, n.ldx, W0->K, y, ldy, W0->N, M);
+         !rows_overlap(n.x, n.ldx, W0->K, M, y, ldy, W0->N, M);
 }
 
 void run_gemm(const swiftspec_w4* W0, const swiftspec_w4* W1, const uint16_t* aprep, int M,
@@ -654,7 +654,7 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
   L.a = base + w.codes;
   L.a_scales = base + w.scales;
   L.a_rows = L.M = M;
-  L.x_written = M <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, W->K, y, ldy, W->N, M);  // more rows are quantised first anyway
+  L.x_written = M <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, W->K, M, y, ldy, W->N, M);  // more rows are quantised first anyway
   L.div = 1;
   L.y = y;
   L.ldy = ldy;
@@ -733,7 +733,7 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
   L.a = base + w.codes;
   L.a_scales = base + w.scales;
   L.a_rows = groups->T;
-  L.x_written = false;
+  L.x_written = pairs <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, Wg->K, groups->T, h, ldh, Wg->N, (int)pairs);
   L.M = (int)pairs;
   L.offsets = groups->offsets;
   L.rows = groups->rows;
