@@ -716,23 +716,19 @@ void launch_tile(Mx4Args a, int blocks, hipStream_t st) {
   hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)blocks * a.col_blocks, a.split), dim3(256), 0, st, a);
 }
 
-enum Form { STREAM_RAW, STREAM_1, STREAM_2, TILE_64, TILE_128, TILE_256 };
+// of each Mx4Form
 constexpr int kRowsOf[] = {16, 16, 32, 64, 128, 256};
 constexpr int kColumnsOf[] = {32, 32, 32, 128, 128, 256};
 
-// The form of a product, the rows of its row blocks and the shares of K.
-struct Plan {
-  Form form;
-  int tm, split;
-};
+}  // namespace
 
 // Every line was drawn on products whose weights come from HBM (copies rotated
 // through more than the Infinity Cache), preparation included; the figures are
 // microseconds of the two sides.
-Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
+Mx4Plan plan_mx4_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
   const int G4 = (mx4_groups(K) + 3) / 4;
   const int64_t weights = (int64_t)(E < M ? E : M) * K * N / 2 * (swiglu ? 2 : 1);  // bytes that are read, at most
-  auto plan = [](Form f, int split = 1) { return Plan{f, kRowsOf[f], split}; };
+  auto plan = [](Mx4Form f, int split = 1) { return Mx4Plan{f, kRowsOf[f], split}; };
   // shares of K that bring the tiles to one for each compute unit, each of at least
   // `least` scale words (four groups each)
   auto split_of = [&](int64_t tiles, int least) {
@@ -756,7 +752,7 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
     // rows: an expert's last is half full): down 5536 x 864, 10 experts of 899 rows,
     // 160 tiles of 256 rows 72.5 against 78.3; 8192 x 2048, 8 experts of 200 rows, 80
     // of them 62.7 against 54.5, and 160 tiles of 128 rows 54.5 against 49.5 with 64.
-    auto enough = [&](Form f) {
+    auto enough = [&](Mx4Form f) {
       return (M / kRowsOf[f] + (E < M ? E : M) / 2) * (int64_t)((N * (swiglu ? 2 : 1) + kColumnsOf[f] - 1) / kColumnsOf[f]) >= (f == TILE_256 ? 160 : 200);
     };
     // 64 rows: 64 against 128 rows a tile 43.9 and 47.3 (64 experts 2048 x 1024);
@@ -765,14 +761,14 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
     // 316; down 1024 x 2048 of 384 rows 132 and 128, 768 rows 234 and 241; over a
     // long K (8 experts, down 14336 x 4096) of 192 rows 111 and 133.
     if (avg >= (K >= 8192 ? 192 : 512) && enough(TILE_256)) return plan(TILE_256);
-    const Form f = avg >= 96 && enough(TILE_128) ? TILE_128 : TILE_64;
+    const Mx4Form f = avg >= 96 && enough(TILE_128) ? TILE_128 : TILE_64;
     // K in shares where tiles are few, and the combination adds their sums: 28 rows
     // of 6 experts 4544 x 1120 16.6 against 14.3, 400 of 8 experts 14336 x 1024 41.8
     // against 36.0.
     return plan(f, swiglu ? 1 : split_of((int64_t)std::max(std::min(E, M), M / kRowsOf[f] + std::min(E, M) / 2) * ((N + 127) / 128), 2));
   }
   if (M <= 16) return plan(STREAM_1);
-  auto tiles = [&](Form f) { return (int64_t)((M + kRowsOf[f] - 1) / kRowsOf[f]) * ((N + kColumnsOf[f] - 1) / kColumnsOf[f]); };
+  auto tiles = [&](Mx4Form f) { return (int64_t)((M + kRowsOf[f] - 1) / kRowsOf[f]) * ((N + kColumnsOf[f] - 1) / kColumnsOf[f]); };
   // Few rows or little to read: 128 rows of 4096 x 4096 14.3 against 14.8, 32 of
   // 8192 x 8192 15.3 against 21; but 28672 x 8192 39.2 against 31.6, 8192 x 28672
   // 38.5 against 35.
@@ -795,8 +791,10 @@ Plan plan_of(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
   return plan(TILE_128, split_of(tiles(TILE_128), 2));
 }
 
+namespace {
+
 template <Mx4Epilogue EPI>
-void launch_form(const Plan& p, const Mx4Args& a, int blocks, hipStream_t st) {
+void launch_form(const Mx4Plan& p, const Mx4Args& a, int blocks, hipStream_t st) {
   switch (p.form) {
     case STREAM_RAW: return launch_stream<8, 1, 2, true, EPI>(a, blocks, st);
     case STREAM_1: return launch_stream<8, 1, 2, false, EPI>(a, blocks, st);
@@ -814,7 +812,9 @@ void launch_form(const Plan& p, const Mx4Args& a, int blocks, hipStream_t st) {
 int launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   // rows that the product may read itself: within a 2 GiB buffer, not overwritten
   const uint64_t x_bytes = ((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2;
-  const Plan p = plan_of(L.M, L.E, L.K, L.N, L.epi == MX4_SWIGLU, L.offsets, x_bytes < kOutside && !L.x_written);
+  const Mx4Plan p = plan_mx4_gemm(L.M, L.E, L.K, L.N, L.epi == MX4_SWIGLU, L.offsets, x_bytes < kOutside && !L.x_written);
+  // 32 rows a workgroup: one matrix whose K is whole
+  if (p.form == STREAM_2 && (L.offsets || p.split > 1)) return 0;
   Mx4Map map = {};
   map.offsets = L.offsets;
   map.E = L.E;
@@ -880,7 +880,7 @@ int launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
 bool mx4_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped) {
   if (M < 1) return true;
   for (bool raw : {false, true}) {
-    const Plan p = plan_of(M, E, K, N, swiglu, grouped, raw);
+    const Mx4Plan p = plan_mx4_gemm(M, E, K, N, swiglu, grouped, raw);
     const int64_t blocks = grouped ? mx4_row_blocks(M, E, p.tm) : (M + p.tm - 1) / p.tm;
     const int64_t columns = ((int64_t)N * (swiglu ? 2 : 1) + kColumnsOf[p.form] - 1) / kColumnsOf[p.form];
     if (blocks * columns * (p.form <= STREAM_2 ? 512 : 256) >= 1ll << 32) return false;
@@ -889,14 +889,14 @@ bool mx4_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped) {
 }
 
 size_t mx4_part_bytes(int M, int K, int N) {
-  const Plan p = plan_of(M, 1, K, N, false, false, false);
+  const Mx4Plan p = plan_mx4_gemm(M, 1, K, N, false, false, false);
   return p.split > 1 ? (size_t)p.split * M * N * sizeof(float) : 0;
 }
 
 size_t mx4_part_bytes_most(int M, int K, int N) {
-  // at most 256 tiles' worth of parts, and no more shares than plan_of allows
+  // at most 256 tiles' worth of parts, and no more shares than plan_mx4_gemm allows
   const int64_t G4 = (mx4_groups(K) + 3) / 4;
-  auto most = [&](Form f, int64_t split) {
+  auto most = [&](Mx4Form f, int64_t split) {
     const int64_t all = 256ll * kRowsOf[f] * kColumnsOf[f], mine = split * M * N;
     return split > 1 ? (size_t)(all < mine ? all : mine) * sizeof(float) : 0;
   };
@@ -905,11 +905,11 @@ size_t mx4_part_bytes_most(int M, int K, int N) {
 }
 
 size_t mx4_rows_bytes(int M, int E, int K, int N) {
-  return (size_t)plan_of(M, E, K, N, false, true, false).split * M * N * sizeof(float);
+  return (size_t)plan_mx4_gemm(M, E, K, N, false, true, false).split * M * N * sizeof(float);
 }
 
 size_t mx4_rows_bytes_most(int64_t M, int K, int N) {
-  // one part, or as many as plan_of allows of at most 256 tiles
+  // one part, or as many as plan_mx4_gemm allows of at most 256 tiles
   const size_t one = (size_t)M * N * sizeof(float), all = std::max<int64_t>((mx4_groups(K) + 3) / 4 / 2, 1) * one;
   return std::max(one, std::min(all, (size_t)256 * 128 * 128 * sizeof(float)));
 }

@@ -78,7 +78,16 @@ bool mx4_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped);
 // of the fp32 rows of an experts' product (ROWS), exactly, and the most of up to M rows
 size_t mx4_rows_bytes(int M, int E, int K, int N);
 size_t mx4_rows_bytes_most(int64_t M, int K, int N);
-// quantises the activations, then multiplies; the parts [M][N] that ROWS left
+// The form of a product, the rows of its row blocks and the shares of K.  raw: the
+// product may read the rows itself.
+enum Mx4Form { STREAM_RAW, STREAM_1, STREAM_2, TILE_64, TILE_128, TILE_256 };
+struct Mx4Plan {
+  Mx4Form form;
+  int tm, split;
+};
+Mx4Plan plan_mx4_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw);
+// quantises the activations, then multiplies; the parts [M][N] that ROWS left, or 0
+// (and nothing launched) if the plan's form has no kernel for this product
 int launch_mx4_gemm(const Mx4Launch& L, hipStream_t st);
 // y[t] = fp16(res[t] + sum over j < k with pos[t][j] >= 0 of weights[t][j] part[pos[t][j]]),
 // part the sum of `split` parts [T k][N] in order; map as the product's launch left it

@@ -662,7 +662,7 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
   L.ldr = ldr;
   L.part = reinterpret_cast<float*>(base + w.part);
   L.ws = ws;
-  ss::launch_mx4_gemm(L, st);
+  if (!ss::launch_mx4_gemm(L, st)) return SWIFTSPEC_UNSUPPORTED;
   return check_launch();
 }
 
@@ -742,7 +742,7 @@ int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, c
   L.y = h;
   L.ldy = ldh;
   L.ws = ws;
-  ss::launch_mx4_gemm(L, st);
+  if (!ss::launch_mx4_gemm(L, st)) return SWIFTSPEC_UNSUPPORTED;
   return check_launch();
 }
 
@@ -792,6 +792,7 @@ int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t l
   L.part = part;
   L.ws = ws;
   const int split = ss::launch_mx4_gemm(L, st);
+  if (!split) return SWIFTSPEC_UNSUPPORTED;
   ss::launch_moe_combine(part, split, groups->T, groups->k, Wd->N, groups->pos, L.map, d_weights, y, ldy,
                          residual, ldr, ws, st);
   return check_launch();
