@@ -561,9 +561,15 @@ class DraftTree:
 # microseconds: the checks below keep to a handful of attribute reads
 _cuda = None  # (handle of a device's current stream, current device)
 _half = None  # torch.float16
+_TOP = 2**31 - 1  # the largest number that the library takes for a size
 
 
-def _rows(t, what, cols, most=2**31 - 1):
+def _size(name, *n):
+    """A size query; numbers of more than 32 bits are as far outside as the largest of 32."""
+    return int(getattr(_load(), "swiftspec_" + name)(*(max(-1, min(v, _TOP)) for v in n)))
+
+
+def _rows(t, what, cols, most=_TOP):
     """(rows, row stride) of an fp16 matrix of `cols` contiguous columns: the
     library takes a pointer and a leading dimension (both of them 32-bit numbers
     but in the quantisation), so a tensor that it would read differently is
@@ -579,7 +585,7 @@ def _rows(t, what, cols, most=2**31 - 1):
         raise SwiftSpecError(INVALID_ARG, what)
     if M <= 1 and ld <= K:
         ld = K
-    if M > most or ld > most:
+    if M > most or ld > most or K > _TOP:
         raise SwiftSpecError(UNSUPPORTED, what)
     return M, ld
 
@@ -631,6 +637,8 @@ def make_mx4(codes, scales, packed=None) -> MX4:
     if codes.dim() not in (2, 3) or not codes.is_contiguous() or codes.element_size() != 1:
         raise SwiftSpecError(INVALID_ARG, "make_mx4")
     _dense(scales, "make_mx4", (*codes.shape[:-1], codes.shape[-1] // 16), 1)
+    if max(*codes.shape, 2 * codes.shape[-1]) > _TOP:
+        raise SwiftSpecError(UNSUPPORTED, "make_mx4")
     E = codes.shape[0] if codes.dim() == 3 else 1
     W = MX4(codes.data_ptr(), scales.data_ptr(), 2 * codes.shape[-1], codes.shape[-2], E,
             packed.data_ptr() if packed is not None else None)
@@ -639,7 +647,7 @@ def make_mx4(codes, scales, packed=None) -> MX4:
 
 
 def mx4_packed_bytes(K: int, N: int, E: int = 1) -> int:
-    return int(_load().swiftspec_mx4_packed_bytes(K, N, E))
+    return _size("mx4_packed_bytes", K, N, E)
 
 
 def prepack_mx4(W: MX4, device="cuda", stream=None):
@@ -674,7 +682,7 @@ def mx4_dequantize(codes, scales, y, stream=None):
 
 
 def mx4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
-    return int(_load().swiftspec_mx4_gemm_workspace_bytes(M, K, N))
+    return _size("mx4_gemm_workspace_bytes", M, K, N)
 
 
 def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
@@ -698,6 +706,8 @@ class MoeGroups:
 
     def __init__(self, T: int, k: int, E: int, offsets=None, rows=None, pos=None, device="cuda"):
         import torch
+        if max(T, k, E) > _TOP:
+            raise SwiftSpecError(UNSUPPORTED, "MoeGroups")
         new = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
         self.T, self.k, self.E = T, k, E
         self.offsets = _dense(new(E + 1) if offsets is None else offsets, "MoeGroups", (E + 1,), 4, real=False)
@@ -714,7 +724,7 @@ class MoeGroups:
 
 
 def moe_route_workspace_bytes(T: int, E: int, k: int) -> int:
-    return int(_load().swiftspec_moe_route_workspace_bytes(T, E, k))
+    return _size("moe_route_workspace_bytes", T, E, k)
 
 
 def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True, stream=None):
@@ -738,7 +748,7 @@ def moe_group(experts, groups: MoeGroups, ws, stream=None):
 
 
 def moe_mx4_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
-    return int(_load().swiftspec_moe_mx4_swiglu_workspace_bytes(T, k, E, K, N))
+    return _size("moe_mx4_swiglu_workspace_bytes", T, k, E, K, N)
 
 
 def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
@@ -753,7 +763,7 @@ def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
 
 
 def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
-    return int(_load().swiftspec_moe_mx4_down_workspace_bytes(T, k, E, K, N))
+    return _size("moe_mx4_down_workspace_bytes", T, k, E, K, N)
 
 
 def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, stream=None):

@@ -55,3 +55,30 @@ def test_size_queries_outside_what_the_calls_take(ss):  # noqa: F811
                           (4, 17, 64, 128, 16), (4, 2, 8, 128, top), (2**25, 1, 8, 128, 16), (4, 2, 512, 65536, 4096)):
         assert swiglu(T, k, E, K, N) == down(T, k, E, K, N) == head, (T, k, E, K, N)
     assert down(2**24, 2, 8, 128, 16) == head < swiglu(2**24, 2, 8, 128, 16)  # its rows are the pairs
+
+
+def test_numbers_of_more_than_32_bits(ss):  # noqa: F811
+    """The binding hands the library 32-bit numbers: longer ones would lose their
+    upper bits, and a call would answer for other sizes."""
+    torch = pytest.importorskip("torch")
+    wide = 1 << 32
+    new = lambda *shape, dtype=torch.uint8: torch.empty(shape, dtype=dtype, device="meta")  # noqa: E731
+    # one row of 2^32 + 32 columns is no row of 32
+    K = wide + 32
+    x, codes, scales = new(1, K, dtype=torch.float16), new(1, K // 2), new(1, K // 32)
+    refused(ss, ss.UNSUPPORTED, ss.mx4_quantize, x, codes, scales)
+    refused(ss, ss.UNSUPPORTED, ss.mx4_dequantize, codes, scales, x)
+    # nor matrices of 2^32 + 16 rows, of 2^32 + 64 columns, or 2^32 + 1 of them
+    for shape in ((wide + 16, 64), (16, wide // 2 + 32), (wide + 1, 16, 64)):
+        refused(ss, ss.UNSUPPORTED, ss.make_mx4, new(*shape), new(*shape[:-1], shape[-1] // 16))
+    for T, k, E in ((wide + 4, 1, 8), (4, wide + 1, 8), (4, 1, wide + 8)):
+        lists = new(E + 1, dtype=torch.int32), new(T * k, dtype=torch.int32), new(T * k, dtype=torch.int32)
+        refused(ss, ss.UNSUPPORTED, ss.MoeGroups, T, k, E, *lists)
+    head = ss.WS_HEADER_BYTES
+    for n in (wide + 128, wide * wide + 128, -wide + 128):
+        assert ss.mx4_packed_bytes(n, 16) == ss.mx4_packed_bytes(128, n) == ss.mx4_packed_bytes(128, 16, n) == 0
+        for f, args in ((ss.mx4_gemm_workspace_bytes, (4, 128, 16)), (ss.moe_route_workspace_bytes, (4, 8, 2)),
+                        (ss.moe_mx4_swiglu_workspace_bytes, (4, 2, 8, 128, 16)), (ss.moe_mx4_down_workspace_bytes, (4, 2, 8, 128, 16))):
+            for i in range(len(args)):
+                assert f(*args[:i], n, *args[i + 1:]) == head, (f.__name__, i, n)
+            assert f(*args) > head
