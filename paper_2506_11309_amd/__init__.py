@@ -633,13 +633,17 @@ def _same_device(where, W, t, *others):
 def make_mx4(codes, scales, packed=None) -> MX4:
     """Describe an MXFP4 matrix held in device tensors codes [N][K/2] u8 and
     scales [N][K/32] u8, or E of them (codes [E][N][K/2], scales [E][N][K/32]),
-    and optionally its kernel-native copy `packed` (see prepack_mx4)."""
+    and optionally its kernel-native copy `packed` (see prepack_mx4), all of it:
+    mx4_packed_bytes contiguous bytes."""
     if codes.dim() not in (2, 3) or not codes.is_contiguous() or codes.element_size() != 1:
         raise SwiftSpecError(INVALID_ARG, "make_mx4")
     _dense(scales, "make_mx4", (*codes.shape[:-1], codes.shape[-1] // 16), 1)
     if max(*codes.shape, 2 * codes.shape[-1]) > _TOP:
         raise SwiftSpecError(UNSUPPORTED, "make_mx4")
     E = codes.shape[0] if codes.dim() == 3 else 1
+    if packed is not None and (not packed.is_contiguous() or
+                               packed.numel() * packed.itemsize < mx4_packed_bytes(2 * codes.shape[-1], codes.shape[-2], E)):
+        raise SwiftSpecError(INVALID_ARG, "make_mx4")
     W = MX4(codes.data_ptr(), scales.data_ptr(), 2 * codes.shape[-1], codes.shape[-2], E,
             packed.data_ptr() if packed is not None else None)
     W.device = _same_device("make_mx4", None, codes, scales, packed)

@@ -82,3 +82,18 @@ def test_numbers_of_more_than_32_bits(ss):  # noqa: F811
             for i in range(len(args)):
                 assert f(*args[:i], n, *args[i + 1:]) == head, (f.__name__, i, n)
             assert f(*args) > head
+
+
+def test_packed_copies_that_do_not_hold_the_matrix(ss, monkeypatch):  # noqa: F811
+    """Products read mx4_packed_bytes of the copy that make_mx4 is given: a smaller
+    or a strided one is refused."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(ss, "_same_device", lambda *a: 0)
+    for shape in ((16, 64), (3, 32, 96)):
+        codes, scales = torch.zeros(shape, dtype=torch.uint8), torch.zeros(*shape[:-1], shape[-1] // 16, dtype=torch.uint8)
+        n = ss.mx4_packed_bytes(2 * shape[-1], shape[-2], shape[0] if len(shape) == 3 else 1)
+        for packed in (torch.zeros(n - 1, dtype=torch.uint8), torch.zeros(0, dtype=torch.uint8), torch.zeros(2 * n, dtype=torch.uint8)[::2],
+                       torch.zeros(n // 4 - 1, dtype=torch.int32), torch.zeros(1, dtype=torch.uint8).expand(n)):
+            refused(ss, ss.INVALID_ARG, ss.make_mx4, codes, scales, packed)
+        for packed in (torch.zeros(n, dtype=torch.uint8), torch.zeros(n + 16, dtype=torch.uint8), torch.zeros(n // 4, dtype=torch.int32)):
+            assert ss.make_mx4(codes, scales, packed).packed == packed.data_ptr()
