@@ -601,13 +601,18 @@ def _dense(t, what, shape, dtype_bytes, real=None):
 
 
 def _run(where, fn, stream, dev, *args):
-    """Call fn(*args, stream handle) with device `dev` current, on `stream` or on
-    the device's current stream."""
+    """Call fn(*args, stream handle) with device `dev` current, on `stream` (of
+    that device) or on the device's current stream."""
     global _cuda
     if _cuda is None:
         import torch
         _cuda = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-    s = _cuda[0](dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        s = _cuda[0](dev)
+    elif getattr(stream, "device_index", dev) == dev:
+        s = stream.cuda_stream
+    else:
+        raise SwiftSpecError(INVALID_ARG, where)
     if _cuda[1]() == dev:
         st = fn(*args, s)
     else:

@@ -97,3 +97,25 @@ def test_packed_copies_that_do_not_hold_the_matrix(ss, monkeypatch):  # noqa: F8
             refused(ss, ss.INVALID_ARG, ss.make_mx4, codes, scales, packed)
         for packed in (torch.zeros(n, dtype=torch.uint8), torch.zeros(n + 16, dtype=torch.uint8), torch.zeros(n // 4, dtype=torch.int32)):
             assert ss.make_mx4(codes, scales, packed).packed == packed.data_ptr()
+
+
+def test_stream_of_another_device(ss, monkeypatch):  # noqa: F811
+    """A call launches on the GPU of its tensors: a stream of another one is
+    refused, one that does not name its GPU (a bare handle) is taken at its word."""
+
+    class Stream:
+        cuda_stream = 0x77
+
+    def on(index):
+        s = Stream()
+        s.device_index = index
+        return s
+
+    calls = []
+    monkeypatch.setattr(ss, "_cuda", (lambda dev: 0x55, lambda: 1))  # the current stream, the current device
+    launch = lambda *a: calls.append(a) or 0  # noqa: E731
+    refused(ss, ss.INVALID_ARG, ss._run, "", launch, on(0), 1, "x")
+    assert calls == []
+    for stream, handle in ((on(1), 0x77), (Stream(), 0x77), (None, 0x55)):
+        ss._run("", launch, stream, 1, "x")
+        assert calls.pop() == ("x", handle)
