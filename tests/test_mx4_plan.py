@@ -7,6 +7,7 @@ import random
 import pytest
 
 import test_gpu_moe
+import test_gpu_moe_forms as forms
 import test_gpu_mx4
 from test_abi import ss  # noqa: F401  (fixture: the built library)
 
@@ -131,3 +132,18 @@ def test_gpu_tests_of_experts_reach_every_form(plan):
         for T, E, k, K, N, kind in test_gpu_moe.CASES:
             got.setdefault(plan(T * k, E, K, N, swiglu, True)[0], set()).add(kind)
         assert got == {form: set(kinds) for form, kinds in want.items()}
+
+
+def test_gpu_tests_run_the_forms_they_name(plan):
+    for T, E, k, K, N, kind, form in forms.SWIGLU:
+        assert plan(T * k, E, K, N, True, True) == (form, 1), (T, E, k, K, N)
+    for T, E, k, K, N, kind, form, split in forms.DOWN:
+        assert plan(T * k, E, K, N, False, True) == (form, split), (T, E, k, K, N)
+    for M, form in forms.LARGE:
+        assert plan(M, 1, forms.LARGE_K, forms.LARGE_N, False, False) == (form, 1)
+    # several scale words in every tile form, and stores past the caches (h of more than 32 MiB) in two
+    for cases in (forms.SWIGLU, forms.DOWN):
+        assert {c[6] for c in cases if c[3] > 1024} >= {"tile 64", "tile 128", "tile 256", "raw", "stream"}
+    assert {c[6] for c in forms.SWIGLU if c[0] * c[2] * c[4] * 2 > 32 << 20} == {"tile 128", "tile 256"}
+    T, E, k, H, F = forms.PROMPT
+    assert plan(T * k, E, H, F, True, True) == ("tile 256", 1) and plan(T * k, E, F, H, False, True) == ("tile 128", 1)
