@@ -10,8 +10,10 @@
 // and ranks its pairs in order (few tokens: one workgroup, one launch).  Counts are
 // integers, so the order of the LDS atomics that add them does not show.
 // Bound by latency: launches, dependent reads, k rounds of row maxima.  64 tokens,
-// 8 of 64 experts: 4.6 us in one launch; 16000 tokens, 8 of 256 (8 MB of scores):
-// 7.7 us to choose and count, 7.3 us to place.
+// 8 of 64 experts: 4.6 to 5 us in one launch; 16000 tokens, 8 of 256 (8 MB of
+// scores): 7.7 us to choose and count, 7.3 us to place; 8 of 512 18.8 and 9.6 us (a
+// lane's 32 scores and both ways of reading them spill to scratch); of given experts
+// 1.9 us to count for 256, 3.1 us for 64 tokens in one launch.
 #include "mx4_device.h"
 #include "mx4_internal.h"
 

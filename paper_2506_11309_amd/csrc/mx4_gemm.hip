@@ -175,8 +175,8 @@ __device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f3
 // kilobyte, read once from memory by the wave that multiplies it, U groups of
 // each tile at a time and the next U on their way.
 // RAW: a single launch for very few rows, which each wave quantises itself as it
-// reads them (16 instructions a kilobyte of weights and tile); the block's expert
-// is found from the offsets.
+// reads them (66 vector instructions a group of 128 columns: 33 to each kilobyte of
+// weights); the block's expert is found from the offsets.
 // Bound by launch, first loads and drain for small matrices, by the weights' bytes
 // for large ones: 32 rows of 8192 x 8192 (36 MB) 11.4 us, 3.1 TB/s; SwiGLU of a
 // token through 8 experts 2048 x 1024 (18 MB) 8.0 us in one launch.
@@ -345,7 +345,8 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 // 4 waves (WM x WN) own a tile of 16 WM MTW rows and 16 WN NTW columns; each
 // wave multiplies MTW x NTW blocks of 16, two by two through the 32 x 32 x 64
 // form of the instruction (one wave a SIMD issues it at 9.0 PFLOP/s, the
-// 16 x 16 x 128 form at 5.1).  Both operands pass through LDS, loaded there
+// 16 x 16 x 128 form at 5.1; on random operands, at the clock that the power then
+// leaves, 6.7 and 5.1).  Both operands pass through LDS, loaded there
 // directly: the weights group by group as they are packed, four groups ahead;
 // the activations two groups at a time, so that a row's piece is a whole
 // 128-byte line however the rows are gathered.  The 16-byte pieces of a line
@@ -357,12 +358,14 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 // Where the tiles are too few for the chip, K is split between workgroups whose
 // parts another kernel adds in order.
 // With few rows an expert it is bound by the weights: SwiGLU of 32 tokens through 8
-// experts 4096 x 14336 (499 MB) 82-92 us, 5.4-6.1 TB/s.  With many it is bound by
-// the matrix cores at the clock that the card's power leaves (1.9 GHz), and by the
-// first loads and last stores of a tile where K is short: 8192 x 8192 x 8192 4.8
-// PFLOP/s, 4001 rows of 4096 x 14336 3.6 (matrix instructions in 49 % of the
-// cycles).  256 rows a tile halve the LDS reads of a product against 128, but one
-// workgroup fills a compute unit's registers.
+// experts 4096 x 14336 (499 MB) 82-92 us, 5.4-6.1 TB/s.  With many no unit alone
+// is the bound: with one wave a SIMD the times of a wave's matrix instructions,
+// vector instructions and waits add up, and the first loads and last stores of a
+// tile count where K is short.  8192 x 8192 x 8192 4.5 PFLOP/s (the instruction
+// alone, on random operands: 6.7), 4001 rows of 4096 x 14336 3.7 (matrix
+// instructions in 49 % of the cycles), SwiGLU of 8191 tokens through 8 of 64
+// experts 2048 x 1024 in 37 %.  256 rows a tile halve the LDS reads of a product
+// against 128, but one workgroup fills a compute unit's registers.
 // The waits count this wave's loads in issue order.  Step g loads, in order,
 // the scales of the next four groups (g % 4 == 0), the activations of groups
 // g + 3 and g + 4 (g odd), the weights of group g + 4.
@@ -750,8 +753,10 @@ Mx4Plan plan_mx4_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
     if (M < (K <= 1024 ? 1 : 4) * (int64_t)E) return plan(STREAM_1);
     // Larger tiles as long as there are enough of them for the chip (blocks of
     // rows: an expert's last is half full): down 5536 x 864, 10 experts of 899 rows,
-    // 160 tiles of 256 rows 72.5 against 78.3; 8192 x 2048, 8 experts of 200 rows, 80
-    // of them 62.7 against 54.5, and 160 tiles of 128 rows 54.5 against 49.5 with 64.
+    // 160 tiles of 256 rows 73.7 against 78.8 with 128; 8192 x 2048, 8 experts of 200
+    // rows, 80 of them 63.1 against 56.1.  128 against 64 rows: 288 tiles (4096 x
+    // 4096, 5 experts of 200 rows) 37.5 and 38.0; but 256 (8192 x 2048) 56.1 and 50.2,
+    // 160 (8192 x 1280) 40.1 and 46.6: their number alone does not decide it.
     auto enough = [&](Mx4Form f) {
       return (M / kRowsOf[f] + (E < M ? E : M) / 2) * (int64_t)((N * (swiglu ? 2 : 1) + kColumnsOf[f] - 1) / kColumnsOf[f]) >= (f == TILE_256 ? 160 : 200);
     };
