@@ -502,6 +502,59 @@ int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int
                        const uint16_t* residual, int32_t ldr, void* ws, size_t ws_bytes, void* stream);
 size_t swiftspec_mx4_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N);
 
+/* ------------------------------------------- block-scaled 8-bit matrices
+ * E matrices W (N output rows x K inputs) of e4m3 codes (sign, four exponent
+ * and three mantissa bits of bias 7: largest 448, no infinities, 0x7F and 0xFF
+ * are NaN) with a float scale for each block of 128 rows and 128 columns, as
+ * models trained in 8 bits are published; value
+ * W'[e][n][k] = code[e][n][k] * scales[e][n/128][k/128].
+ *   codes : [E][N][K] bytes;
+ *   scales: [E][ceil(N/128)][ceil(K/128)] float (any value; a product applies it
+ *           to the sum over its 128 columns);
+ *   packed: kernel-native copy written once by swiftspec_fp8_prepack
+ *           (swiftspec_fp8_packed_bytes(K, N, E) bytes, 16-byte aligned, owned
+ *           by the caller), the only one that the products read.
+ * K % 16 == 0 (K is padded to whole blocks in the packed copy), N % 16 == 0,
+ * 1 <= E <= SWIFTSPEC_MAX_EXPERTS, one matrix's packed copy below 4 GiB and all
+ * of them below 32 GiB; a product whose launch would need 2^32 threads or more is
+ * refused (UNSUPPORTED in each case).  For sizes that the calls refuse for these
+ * limits, packed_bytes is 0 and a workspace query answers the header alone.
+ * Products take fp16 activations and quantise them first, each row's 128 columns
+ * as a block: both operands are in 8 bits, the sums in fp32. */
+typedef struct {
+  const uint8_t* codes;
+  const float* scales;
+  int32_t K, N, E;
+  const void* packed;
+} swiftspec_fp8;
+
+size_t swiftspec_fp8_packed_bytes(int32_t K, int32_t N, int32_t E);
+int swiftspec_fp8_prepack(const swiftspec_fp8* W, void* packed, size_t packed_bytes, void* stream);
+
+/* Quantise M rows x [M][ldx] fp16 (16-byte aligned, ldx % 8 == 0) of K columns
+ * into codes [M][K] (8-byte aligned) and scales [ceil(M/block_rows)][ceil(K/128)],
+ * block_rows 1 (activations) or 128 (a matrix).  With a block's largest magnitude
+ * a: s is the least power of two with a <= 448 s, every value goes to the nearest
+ * code of v / s, ties to the even code; a = 0: s = 1.  A block that holds an
+ * infinity or a NaN gets s = NaN and codes 0: it stands for NaN.  K % 16 == 0;
+ * M K, K rounded up to 128, < 2^35 (also of dequantize). */
+int swiftspec_fp8_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx, int32_t block_rows, uint8_t* codes,
+                           float* scales, void* stream);
+/* y [M][ldy] fp16 (16-byte aligned, ldy % 8 == 0): code times scale, rounded once,
+ * to nearest even; above the fp16 range infinity. */
+int swiftspec_fp8_dequantize(const uint8_t* codes, const float* scales, int64_t M, int32_t K, int32_t block_rows,
+                             uint16_t* y, int64_t ldy, void* stream);
+
+/* y[m][n] = fp16( sum_g scales[n/128][g] * (sum_{k in g} Q(x)[m][k] * code[n][k])
+ * + residual[m][n] ) over blocks g of 128 columns, Q(x) as swiftspec_fp8_quantize
+ * gives it with block_rows = 1, fp32 sums; W->E == 1.  Any M >= 0 with M rows of
+ * K, rounded up to 128, bytes below 2 GiB (UNSUPPORTED otherwise).  Aliasing,
+ * alignment, rows that hold an infinity or a NaN, and the workspace query as
+ * swiftspec_mx4_gemm. */
+int swiftspec_fp8_gemm(const swiftspec_fp8* W, const uint16_t* x, int32_t M, int32_t ldx, uint16_t* y, int32_t ldy,
+                       const uint16_t* residual, int32_t ldr, void* ws, size_t ws_bytes, void* stream);
+size_t swiftspec_fp8_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N);
+
 /* ------------------------------------------------- mixture of experts
  * The feed-forward block of a target model whose tokens each go through k of
  * E experts: route, then swiglu and down over the groups that it made.  T
@@ -530,6 +583,35 @@ typedef struct {
 int swiftspec_moe_route(const uint16_t* logits, int32_t ldl, int32_t renormalize, int32_t* d_experts,
                         float* d_weights, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
                         void* stream);
+/* Router by probabilities or gates.  For each of T rows of scores (logits
+ * [T][ldl], E columns, fp16 or float by logit_bits 16 or 32, aligned to their
+ * type):
+ *   s_e = softmax over all E experts, or sigmoid, of the score, computed in 64
+ *         bits and rounded to fp32;
+ *   c_e = s_e + bias[e] in fp32 (bias NULL: s_e);
+ *   experts e with the same e / (E / groups) form a group, whose value is its
+ *         largest c, or with group_best = 2 the sum (fp32) of its two largest (of
+ *         a single one itself); the top_groups groups of largest value compete;
+ *   the k experts of largest c among them go to d_experts [T][k], in that order
+ *         (equal values: lower index first, of groups as of experts);
+ *   d_weights [T][k] (float) = scale * s_e, with renormalize != 0
+ *         scale * s_e / (sum of the k; 0 where that is 0).
+ * A score of -inf or NaN is masked: it has no probability and is never chosen;
+ * nor is an expert whose bias is -inf or NaN.  Slots left without an expert get
+ * -1, weight 0 and no place in a group.  +inf counts as the largest finite value
+ * of its type.  Then the groups of pairs, as swiftspec_moe_group makes them.
+ * groups divides E; workspace as swiftspec_moe_route. */
+enum { SWIFTSPEC_SCORE_SOFTMAX = 0, SWIFTSPEC_SCORE_SIGMOID = 1 };
+typedef struct {
+  int32_t score;
+  int32_t groups, top_groups, group_best;
+  int32_t renormalize;
+  float scale;
+  const float* bias; /* device, [E], or NULL */
+} swiftspec_moe_scoring;
+int swiftspec_moe_route_scored(const void* logits, int32_t logit_bits, int32_t ldl, const swiftspec_moe_scoring* scoring,
+                               int32_t* d_experts, float* d_weights, const swiftspec_moe_groups* groups, void* ws,
+                               size_t ws_bytes, void* stream);
 /* The groups of experts that were chosen otherwise: d_experts [T][k]; an index
  * outside [0, E) means no expert, one that a token names twice counts twice.
  * ws 8-byte aligned. */
@@ -562,6 +644,17 @@ int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t l
                            const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr,
                            void* ws, size_t ws_bytes, void* stream);
 size_t swiftspec_moe_mx4_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N);
+
+/* The same two halves with block-scaled 8-bit matrices; Q and the sums as
+ * swiftspec_fp8_gemm, everything else as above. */
+int swiftspec_moe_fp8_swiglu(const swiftspec_fp8* Wg, const swiftspec_fp8* Wu, const uint16_t* x, int32_t ldx,
+                             const swiftspec_moe_groups* groups, uint16_t* h, int32_t ldh, void* ws, size_t ws_bytes,
+                             void* stream);
+size_t swiftspec_moe_fp8_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N);
+int swiftspec_moe_fp8_down(const swiftspec_fp8* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
+                           const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr,
+                           void* ws, size_t ws_bytes, void* stream);
+size_t swiftspec_moe_fp8_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N);
 
 /* -------------------------------------------------------- decoder layer */
 typedef struct {

@@ -51,6 +51,16 @@ class MX4(ctypes.Structure):
     device = None  # index of the GPU that make_mx4 found the codes on
 
 
+class FP8(ctypes.Structure):
+    _fields_ = [("codes", vp), ("scales", vp), ("K", i32), ("N", i32), ("E", i32), ("packed", vp)]
+    device = None  # index of the GPU that make_fp8 found the codes on
+
+
+class _Scoring(ctypes.Structure):
+    _fields_ = [("score", i32), ("groups", i32), ("top_groups", i32), ("group_best", i32), ("renormalize", i32), ("scale", f32),
+                ("bias", vp)]
+
+
 class _Groups(ctypes.Structure):
     _fields_ = [("T", i32), ("k", i32), ("E", i32), ("offsets", vp), ("rows", vp), ("pos", vp)]
 
@@ -132,7 +142,15 @@ _SIGS = {
     "swiftspec_mx4_dequantize": ([vp, vp, i64, i32, vp, i64, vp], ctypes.c_int),
     "swiftspec_mx4_gemm": ([ctypes.POINTER(MX4), vp, i32, i32, vp, i32, vp, i32, vp, sz, vp], ctypes.c_int),
     "swiftspec_mx4_gemm_workspace_bytes": ([i32, i32, i32], sz),
+    "swiftspec_fp8_packed_bytes": ([i32, i32, i32], sz),
+    "swiftspec_fp8_prepack": ([ctypes.POINTER(FP8), vp, sz, vp], ctypes.c_int),
+    "swiftspec_fp8_quantize": ([vp, i64, i32, i64, i32, vp, vp, vp], ctypes.c_int),
+    "swiftspec_fp8_dequantize": ([vp, vp, i64, i32, i32, vp, i64, vp], ctypes.c_int),
+    "swiftspec_fp8_gemm": ([ctypes.POINTER(FP8), vp, i32, i32, vp, i32, vp, i32, vp, sz, vp], ctypes.c_int),
+    "swiftspec_fp8_gemm_workspace_bytes": ([i32, i32, i32], sz),
     "swiftspec_moe_route": ([vp, i32, i32, vp, vp, ctypes.POINTER(_Groups), vp, sz, vp], ctypes.c_int),
+    "swiftspec_moe_route_scored": ([vp, i32, i32, ctypes.POINTER(_Scoring), vp, vp, ctypes.POINTER(_Groups), vp, sz, vp],
+                                   ctypes.c_int),
     "swiftspec_moe_group": ([vp, ctypes.POINTER(_Groups), vp, sz, vp], ctypes.c_int),
     "swiftspec_moe_route_workspace_bytes": ([i32, i32, i32], sz),
     "swiftspec_moe_mx4_swiglu": ([ctypes.POINTER(MX4), ctypes.POINTER(MX4), vp, i32, ctypes.POINTER(_Groups), vp, i32,
@@ -141,6 +159,12 @@ _SIGS = {
     "swiftspec_moe_mx4_down": ([ctypes.POINTER(MX4), vp, i32, ctypes.POINTER(_Groups), vp, vp, i32, vp, i32, vp, sz,
                                 vp], ctypes.c_int),
     "swiftspec_moe_mx4_down_workspace_bytes": ([i32, i32, i32, i32, i32], sz),
+    "swiftspec_moe_fp8_swiglu": ([ctypes.POINTER(FP8), ctypes.POINTER(FP8), vp, i32, ctypes.POINTER(_Groups), vp, i32,
+                                  vp, sz, vp], ctypes.c_int),
+    "swiftspec_moe_fp8_swiglu_workspace_bytes": ([i32, i32, i32, i32, i32], sz),
+    "swiftspec_moe_fp8_down": ([ctypes.POINTER(FP8), vp, i32, ctypes.POINTER(_Groups), vp, vp, i32, vp, i32, vp, sz,
+                                vp], ctypes.c_int),
+    "swiftspec_moe_fp8_down_workspace_bytes": ([i32, i32, i32, i32, i32], sz),
     "swiftspec_graph_begin": ([vp], ctypes.c_int),
     "swiftspec_graph_end": ([vp, ctypes.POINTER(vp)], ctypes.c_int),
     "swiftspec_graph_launch": ([vp, vp], ctypes.c_int),
@@ -555,12 +579,13 @@ class DraftTree:
                 "pending": [int(x) for x in pend[:out[3]]]}
 
 
-# ------------------------- microscaled 4-bit matrices, mixture of experts
+# ---- microscaled 4-bit and block-scaled 8-bit matrices, mixture of experts
 
 # a call's own cost on the host counts where the kernels take a few
 # microseconds: the checks below keep to a handful of attribute reads
 _cuda = None  # (handle of a device's current stream, current device)
 _half = None  # torch.float16
+_single = None  # torch.float32
 _TOP = 2**31 - 1  # the largest number that the library takes for a size
 
 
@@ -569,8 +594,8 @@ def _size(name, *n):
     return int(getattr(_load(), "swiftspec_" + name)(*(max(-1, min(v, _TOP)) for v in n)))
 
 
-def _rows(t, what, cols, most=_TOP):
-    """(rows, row stride) of an fp16 matrix of `cols` contiguous columns: the
+def _rows(t, what, cols, most=_TOP, dtype=None):
+    """(rows, row stride) of an fp16 matrix (or of `dtype`) of `cols` contiguous columns: the
     library takes a pointer and a leading dimension (both of them 32-bit numbers
     but in the quantisation), so a tensor that it would read differently is
     refused here."""
@@ -581,7 +606,7 @@ def _rows(t, what, cols, most=_TOP):
     if t.dim() != 2:
         raise SwiftSpecError(INVALID_ARG, what)
     (M, K), (ld, step) = t.shape, t.stride()
-    if K != cols or t.dtype is not _half or (step != 1 and K > 1):
+    if K != cols or t.dtype is not (dtype or _half) or (step != 1 and K > 1):
         raise SwiftSpecError(INVALID_ARG, what)
     if M <= 1 and ld <= K:
         ld = K
@@ -635,39 +660,52 @@ def _same_device(where, W, t, *others):
     return dev
 
 
+def _matrix(kind, where, codes, scales, K, packed):
+    """The description of a matrix, or of E of them, whose scales were checked;
+    codes [..., N][bytes of a row], `packed` all of its kernel-native copy or None."""
+    if max(*codes.shape, K) > _TOP:
+        raise SwiftSpecError(UNSUPPORTED, where)
+    E, N = codes.shape[0] if codes.dim() == 3 else 1, codes.shape[-2]
+    size = mx4_packed_bytes if kind is MX4 else fp8_packed_bytes
+    if packed is not None and (not packed.is_contiguous() or packed.numel() * packed.itemsize < size(K, N, E)):
+        raise SwiftSpecError(INVALID_ARG, where)
+    W = kind(codes.data_ptr(), scales.data_ptr(), K, N, E, packed.data_ptr() if packed is not None else None)
+    W.device = _same_device(where, None, codes, scales, packed)
+    return W
+
+
+def _codes(where, codes):
+    if codes.dim() not in (2, 3) or not codes.is_contiguous() or codes.element_size() != 1:
+        raise SwiftSpecError(INVALID_ARG, where)
+
+
 def make_mx4(codes, scales, packed=None) -> MX4:
     """Describe an MXFP4 matrix held in device tensors codes [N][K/2] u8 and
     scales [N][K/32] u8, or E of them (codes [E][N][K/2], scales [E][N][K/32]),
     and optionally its kernel-native copy `packed` (see prepack_mx4), all of it:
     mx4_packed_bytes contiguous bytes."""
-    if codes.dim() not in (2, 3) or not codes.is_contiguous() or codes.element_size() != 1:
-        raise SwiftSpecError(INVALID_ARG, "make_mx4")
+    _codes("make_mx4", codes)
     _dense(scales, "make_mx4", (*codes.shape[:-1], codes.shape[-1] // 16), 1)
-    if max(*codes.shape, 2 * codes.shape[-1]) > _TOP:
-        raise SwiftSpecError(UNSUPPORTED, "make_mx4")
-    E = codes.shape[0] if codes.dim() == 3 else 1
-    if packed is not None and (not packed.is_contiguous() or
-                               packed.numel() * packed.itemsize < mx4_packed_bytes(2 * codes.shape[-1], codes.shape[-2], E)):
-        raise SwiftSpecError(INVALID_ARG, "make_mx4")
-    W = MX4(codes.data_ptr(), scales.data_ptr(), 2 * codes.shape[-1], codes.shape[-2], E,
-            packed.data_ptr() if packed is not None else None)
-    W.device = _same_device("make_mx4", None, codes, scales, packed)
-    return W
+    return _matrix(MX4, "make_mx4", codes, scales, 2 * codes.shape[-1], packed)
 
 
 def mx4_packed_bytes(K: int, N: int, E: int = 1) -> int:
     return _size("mx4_packed_bytes", K, N, E)
 
 
+def _prepack(where, W, size, device, stream):
+    import torch
+    t = torch.empty(size, dtype=torch.uint8, device=device)
+    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, W, t), ctypes.byref(W), t.data_ptr(), t.numel())
+    W.packed = t.data_ptr()
+    return t
+
+
 def prepack_mx4(W: MX4, device="cuda", stream=None):
     """Allocate and fill the kernel-native copy of W on `device` (the GPU that
     holds its codes; another one is refused); returns the uint8 device tensor and
     sets W.packed to it (keep the tensor alive)."""
-    import torch
-    t = torch.empty(mx4_packed_bytes(W.K, W.N, W.E), dtype=torch.uint8, device=device)
-    _run("mx4_prepack", _load().swiftspec_mx4_prepack, stream, _same_device("mx4_prepack", W, t), ctypes.byref(W), t.data_ptr(), t.numel())
-    W.packed = t.data_ptr()
-    return t
+    return _prepack("mx4_prepack", W, mx4_packed_bytes(W.K, W.N, W.E), device, stream)
 
 
 def mx4_quantize(x, codes, scales, stream=None):
@@ -694,18 +732,76 @@ def mx4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
     return _size("mx4_gemm_workspace_bytes", M, K, N)
 
 
-def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
-    """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
-    M, ldx = _rows(x, "mx4_gemm", W.K)
-    m, ldy = _rows(y, "mx4_gemm", W.N)
+def _gemm(where, W, x, y, ws, residual, stream):
+    M, ldx = _rows(x, where, W.K)
+    m, ldy = _rows(y, where, W.N)
     r, ldr, res = M, 0, None
     if residual is not None:
-        r, ldr = _rows(residual, "mx4_gemm", W.N)
+        r, ldr = _rows(residual, where, W.N)
         res = residual.data_ptr()
     if m != M or r != M:
-        raise SwiftSpecError(INVALID_ARG, "mx4_gemm")
-    _run("mx4_gemm", _load().swiftspec_mx4_gemm, stream, _same_device("mx4_gemm", W, x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M, ldx,
-         y.data_ptr(), ldy, res, ldr, ws.data_ptr(), ws.numel() * ws.element_size())
+        raise SwiftSpecError(INVALID_ARG, where)
+    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, W, x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M,
+         ldx, y.data_ptr(), ldy, res, ldr, ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
+    """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
+    _gemm("mx4_gemm", W, x, y, ws, residual, stream)
+
+
+def make_fp8(codes, scales, packed=None) -> FP8:
+    """Describe an 8-bit matrix held in device tensors codes [N][K] (e4m3: uint8 or
+    torch.float8_e4m3fn) and scales [ceil(N/128)][ceil(K/128)] float32, or E of them
+    (codes [E][N][K], scales [E][...][...]), and optionally its kernel-native copy
+    `packed` (see prepack_fp8), all of it: fp8_packed_bytes contiguous bytes."""
+    _codes("make_fp8", codes)
+    if codes.dtype.is_floating_point and "e4m3fn" not in str(codes.dtype).split("_"):
+        raise SwiftSpecError(INVALID_ARG, "make_fp8")
+    _dense(scales, "make_fp8", (*codes.shape[:-2], -(-codes.shape[-2] // 128), -(-codes.shape[-1] // 128)), 4, real=True)
+    return _matrix(FP8, "make_fp8", codes, scales, codes.shape[-1], packed)
+
+
+def fp8_packed_bytes(K: int, N: int, E: int = 1) -> int:
+    return _size("fp8_packed_bytes", K, N, E)
+
+
+def prepack_fp8(W: FP8, device="cuda", stream=None):
+    """Allocate and fill the kernel-native copy of W, as prepack_mx4."""
+    return _prepack("fp8_prepack", W, fp8_packed_bytes(W.K, W.N, W.E), device, stream)
+
+
+def _fp8_convert(where, values, codes, scales, rows, stream):
+    K = values.shape[-1]
+    M, ld = _rows(values, where, K, 2**63 - 1)
+    if rows not in (1, 128):
+        raise SwiftSpecError(INVALID_ARG, where)
+    _dense(codes, where, (M, K), 1)
+    _dense(scales, where, (-(-M // rows), -(-K // 128)), 4, real=True)
+    return M, K, ld, _same_device(where, None, values, codes, scales)
+
+
+def fp8_quantize(x, codes, scales, rows=1, stream=None):
+    """x [M][K] fp16 (rows contiguous) -> codes [M][K] (e4m3 in bytes), scales
+    [ceil(M/rows)][ceil(K/128)] float32 of blocks of `rows` (1 or 128) rows and 128
+    columns."""
+    M, K, ld, dev = _fp8_convert("fp8_quantize", x, codes, scales, rows, stream)
+    _run("fp8_quantize", _load().swiftspec_fp8_quantize, stream, dev, x.data_ptr(), M, K, ld, rows, codes.data_ptr(), scales.data_ptr())
+
+
+def fp8_dequantize(codes, scales, y, rows=1, stream=None):
+    """codes [M][K], scales [ceil(M/rows)][ceil(K/128)] -> y [M][K] fp16 (rows contiguous)."""
+    M, K, ld, dev = _fp8_convert("fp8_dequantize", y, codes, scales, rows, stream)
+    _run("fp8_dequantize", _load().swiftspec_fp8_dequantize, stream, dev, codes.data_ptr(), scales.data_ptr(), M, K, rows, y.data_ptr(), ld)
+
+
+def fp8_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
+    return _size("fp8_gemm_workspace_bytes", M, K, N)
+
+
+def fp8_gemm(W: FP8, x, y, ws, residual=None, stream=None):
+    """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
+    _gemm("fp8_gemm", W, x, y, ws, residual, stream)
 
 
 class MoeGroups:
@@ -749,6 +845,47 @@ def moe_route(logits, experts, weights, groups: MoeGroups, ws, renormalize=True,
          ws.data_ptr(), ws.numel() * ws.element_size())
 
 
+class MoeScoring:
+    """How moe_route_scored makes scores and compares experts: `score` "softmax" or
+    "sigmoid"; `bias` [E] float32 (device) added before they are compared, not to the
+    weights; of `groups` groups of consecutive experts only the `top_groups` with the
+    largest sum of `group_best` (1 or 2) largest compete; weights divided by their sum
+    (`renormalize`) and multiplied by `scale`."""
+
+    def __init__(self, score="softmax", bias=None, groups: int = 1, top_groups: int = 1, group_best: int = 1, renormalize=True,
+                 scale: float = 1.0):
+        if score not in ("softmax", "sigmoid"):
+            raise SwiftSpecError(INVALID_ARG, "MoeScoring")
+        if max(groups, top_groups, group_best) > _TOP or min(groups, top_groups, group_best) < 1:
+            raise SwiftSpecError(INVALID_ARG, "MoeScoring")
+        if bias is not None:
+            _dense(bias, "MoeScoring", (bias.numel(),), 4, real=True)
+            _same_device("MoeScoring", None, bias)
+        self.bias = bias
+        self._c = _Scoring(("softmax", "sigmoid").index(score), groups, top_groups, group_best, int(bool(renormalize)), scale,
+                           bias.data_ptr() if bias is not None else None)
+
+
+def moe_route_scored(logits, scoring: MoeScoring, experts, weights, groups: MoeGroups, ws, stream=None):
+    """logits [T][E] fp16 or float32 (rows contiguous) -> experts [T][k] int32 and
+    weights [T][k] float32 of the k experts that `scoring` puts first, and the groups;
+    the workspace is that of moe_route."""
+    global _single
+    if _single is None:
+        import torch
+        _single = torch.float32
+    wide = logits.dtype is _single
+    T, ldl = _rows(logits, "moe_route_scored", groups.E, dtype=_single if wide else None)
+    if T != groups.T or (scoring.bias is not None and scoring.bias.numel() != groups.E):
+        raise SwiftSpecError(INVALID_ARG, "moe_route_scored")
+    _dense(experts, "moe_route_scored", (T, groups.k), 4, real=False)
+    _dense(weights, "moe_route_scored", (T, groups.k), 4, real=True)
+    _run("moe_route_scored", _load().swiftspec_moe_route_scored, stream,
+         _same_device("moe_route_scored", None, groups.offsets, logits, scoring.bias, experts, weights, ws), logits.data_ptr(),
+         32 if wide else 16, ldl, ctypes.byref(scoring._c), experts.data_ptr(), weights.data_ptr(), groups._ref(), ws.data_ptr(),
+         ws.numel() * ws.element_size())
+
+
 def moe_group(experts, groups: MoeGroups, ws, stream=None):
     """The groups of given experts [T][k] int32 (outside [0, E): none)."""
     _dense(experts, "moe_group", (groups.T, groups.k), 4, real=False)
@@ -760,15 +897,33 @@ def moe_mx4_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> in
     return _size("moe_mx4_swiglu_workspace_bytes", T, k, E, K, N)
 
 
+def _swiglu(where, Wg, Wu, x, groups, h, ws, stream):
+    T, ldx = _rows(x, where, Wg.K)
+    P, ldh = _rows(h, where, Wg.N)
+    if T != groups.T or P != groups.T * groups.k or Wu.device not in (None, Wg.device):
+        raise SwiftSpecError(INVALID_ARG, where)
+    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, Wg, groups.offsets, x, h, ws), ctypes.byref(Wg),
+         ctypes.byref(Wu), x.data_ptr(), ldx, groups._ref(), h.data_ptr(), ldh, ws.data_ptr(), ws.numel() * ws.element_size())
+
+
+def _down(where, Wd, h, groups, weights, y, ws, residual, stream):
+    P, ldh = _rows(h, where, Wd.K)
+    T, ldy = _rows(y, where, Wd.N)
+    r, ldr, res = T, 0, None
+    if residual is not None:
+        r, ldr = _rows(residual, where, Wd.N)
+        res = residual.data_ptr()
+    if T != groups.T or r != T or P != T * groups.k:
+        raise SwiftSpecError(INVALID_ARG, where)
+    _dense(weights, where, (T, groups.k), 4, real=True)
+    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, Wd, groups.offsets, h, weights, y, ws, residual),
+         ctypes.byref(Wd), h.data_ptr(), ldh, groups._ref(), weights.data_ptr(), y.data_ptr(), ldy, res, ldr, ws.data_ptr(),
+         ws.numel() * ws.element_size())
+
+
 def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
     """x [T][K] fp16 -> h [T k][N] fp16, a row for each place of the groups."""
-    T, ldx = _rows(x, "moe_mx4_swiglu", Wg.K)
-    P, ldh = _rows(h, "moe_mx4_swiglu", Wg.N)
-    if T != groups.T or P != groups.T * groups.k or Wu.device not in (None, Wg.device):
-        raise SwiftSpecError(INVALID_ARG, "moe_mx4_swiglu")
-    _run("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, stream, _same_device("moe_mx4_swiglu", Wg, groups.offsets, x, h, ws), ctypes.byref(Wg),
-         ctypes.byref(Wu), x.data_ptr(), ldx, groups._ref(), h.data_ptr(), ldh, ws.data_ptr(),
-         ws.numel() * ws.element_size())
+    _swiglu("moe_mx4_swiglu", Wg, Wu, x, groups, h, ws, stream)
 
 
 def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
@@ -778,18 +933,25 @@ def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
 def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, stream=None):
     """h [T k][K] fp16 (as moe_mx4_swiglu wrote it), weights [T][k] float32 ->
     y [T][N] fp16, the weighted sum of each token's experts plus residual."""
-    P, ldh = _rows(h, "moe_mx4_down", Wd.K)
-    T, ldy = _rows(y, "moe_mx4_down", Wd.N)
-    r, ldr, res = T, 0, None
-    if residual is not None:
-        r, ldr = _rows(residual, "moe_mx4_down", Wd.N)
-        res = residual.data_ptr()
-    if T != groups.T or r != T or P != T * groups.k:
-        raise SwiftSpecError(INVALID_ARG, "moe_mx4_down")
-    _dense(weights, "moe_mx4_down", (T, groups.k), 4, real=True)
-    _run("moe_mx4_down", _load().swiftspec_moe_mx4_down, stream, _same_device("moe_mx4_down", Wd, groups.offsets, h, weights, y, ws, residual),
-         ctypes.byref(Wd), h.data_ptr(), ldh, groups._ref(), weights.data_ptr(), y.data_ptr(), ldy, res, ldr,
-         ws.data_ptr(), ws.numel() * ws.element_size())
+    _down("moe_mx4_down", Wd, h, groups, weights, y, ws, residual, stream)
+
+
+def moe_fp8_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
+    return _size("moe_fp8_swiglu_workspace_bytes", T, k, E, K, N)
+
+
+def moe_fp8_swiglu(Wg: FP8, Wu: FP8, x, groups: MoeGroups, h, ws, stream=None):
+    """moe_mx4_swiglu with 8-bit matrices."""
+    _swiglu("moe_fp8_swiglu", Wg, Wu, x, groups, h, ws, stream)
+
+
+def moe_fp8_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
+    return _size("moe_fp8_down_workspace_bytes", T, k, E, K, N)
+
+
+def moe_fp8_down(Wd: FP8, h, groups: MoeGroups, weights, y, ws, residual=None, stream=None):
+    """moe_mx4_down with 8-bit matrices."""
+    _down("moe_fp8_down", Wd, h, groups, weights, y, ws, residual, stream)
 
 
 def make_dims(H, Hq, Hkv, D, F, S_max, eps=1e-5, rope_theta=500000.0) -> Dims:

@@ -14,43 +14,13 @@
 // scores): 7.7 us to choose and count, 7.3 us to place; 8 of 512 18.8 and 9.6 us (a
 // lane's 32 scores and both ways of reading them spill to scratch); of given experts
 // 1.9 us to count for 256, 3.1 us for 64 tokens in one launch.
-#include "mx4_device.h"
-#include "mx4_internal.h"
+#include "moe_group_device.h"
 
 namespace ss {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kMaxE = SWIFTSPEC_MAX_EXPERTS;
-constexpr int kUnits = 2;          // units that a workgroup groups
-
-// Tokens of a unit: as many as its waves take at one time, so that a prompt fills
-// the chip, but at most 256 units (each grouping workgroup reads all their
-// counts) as long as a unit's counts fit 16 bits.
-constexpr int kLeast = 4 * kWaves;
-inline int unit_tokens(int T, int k) {
-  const int most = 65535 / k, need = (T + 255) / 256;
-  return need < kLeast ? kLeast : need > most ? most : need;
-}
-
-// Over the 16 lanes of a row (rotations within it): every lane gets the result.
-template <int kRotate>
-__device__ __forceinline__ uint32_t rotated(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x120 + kRotate, 0xF, 0xF, true);  // row_ror
-}
-__device__ __forceinline__ uint32_t row_max(uint32_t v) {
-  v = max(v, rotated<8>(v));
-  v = max(v, rotated<4>(v));
-  v = max(v, rotated<2>(v));
-  return max(v, rotated<1>(v));
-}
-__device__ __forceinline__ float row_sum(float v) {
-  v += bitcast<float>(rotated<8>(bitcast<uint32_t>(v)));
-  v += bitcast<float>(rotated<4>(bitcast<uint32_t>(v)));
-  v += bitcast<float>(rotated<2>(bitcast<uint32_t>(v)));
-  return v + bitcast<float>(rotated<1>(bitcast<uint32_t>(v)));
-}
+constexpr int kUnits = 2;  // units that a workgroup groups
 
 // ascending 16-bit key of an fp16 score, 0 where masked (-inf, NaN); +inf counts as 65504
 __device__ __forceinline__ uint32_t score_key(uint32_t h) {
@@ -63,15 +33,11 @@ __device__ __forceinline__ float key_score(uint32_t key) {
   return h2f((uint16_t)(key & 0x8000u ? key - 0x8000u : 0xFFFFu - key));
 }
 
-struct RouteArgs {
+struct RouteArgs : GroupArgs {
   const uint16_t* logits;
   int64_t ldl;
-  int T, E, k, renormalize, tokens;
+  int renormalize;
   bool lines;  // rows can be read 16 bytes at a time
-  int32_t* experts;
-  float* weights;
-  int32_t *offsets, *rows, *pos;
-  uint16_t* hist;  // [units][E rounded up to 4]
 };
 
 // 16 lanes take the top k of a token's row, V scores each (in whole 16-byte pieces,
@@ -170,78 +136,6 @@ __device__ __forceinline__ void route_tokens(const RouteArgs& a, int t0, int t1,
   __syncthreads();
 }
 
-struct GroupLds {
-  int base[kMaxE];           // next place of each expert's pairs
-  int count[kWaves][kMaxE];  // pairs of each wave
-  int wave_total[kWaves];
-};
-
-// The places of the pairs of tokens t0 .. t1.  Thread e brings the number of expert
-// e's pairs, of all tokens and of those before t0.
-__device__ __forceinline__ void group_tokens(const RouteArgs& a, int t0, int t1, int all, int before, bool writes_offsets,
-                                             const int16_t* chosen, int e_first, GroupLds& s) {
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
-  const int scan = wave_scan_add(all);
-  if (lane == 63) s.wave_total[wave] = scan;
-  __syncthreads();
-  int lead = 0, used = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const int n = s.wave_total[w];
-    lead += w < wave ? n : 0;
-    used += n;
-  }
-  if (tid < a.E) {
-    const int off = lead + scan - all;
-    s.base[tid] = off + before;
-    if (writes_offsets) {
-      a.offsets[tid] = off;
-      if (tid == a.E - 1) a.offsets[a.E] = off + all;
-    }
-  }
-  const int n0 = t0 * a.k, n1 = t1 * a.k;
-  // places past the last pair
-  for (int i = n0 + tid; i < n1; i += kThreads)
-    if (i >= used) a.rows[i] = -1;
-  for (int i0 = n0; i0 < n1; i0 += kThreads) {
-    if (tid < a.E)
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) s.count[w][tid] = 0;
-    __syncthreads();
-    const int i = i0 + tid;
-    int e = i >= n1 ? -1 : chosen ? chosen[i] : i0 == n0 ? e_first : a.experts[i];
-    if (e >= a.E) e = -1;
-    const bool has = e >= 0;
-    // lanes of this wave with the same expert
-    uint64_t same = __ballot(has);
-#pragma unroll
-    for (int bit = 0; (1 << bit) < kMaxE; ++bit) {
-      const uint64_t m = __ballot((e >> bit) & 1);
-      same &= (e >> bit) & 1 ? m : ~m;
-    }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    if (has && rank == 0) s.count[wave][e] = __popcll(same);
-    __syncthreads();
-    int place = -1;
-    if (has) {
-      place = s.base[e] + rank;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) place += w < wave ? s.count[w][e] : 0;
-      a.rows[place] = i;
-    }
-    if (i < n1) a.pos[i] = place;
-    if (i0 + kThreads >= n1) break;
-    __syncthreads();
-    if (tid < a.E) {
-      int c = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) c += s.count[w][tid];
-      s.base[tid] += c;
-    }
-    __syncthreads();
-  }
-}
-
 // Few tokens (up to 1024 pairs): everything in one workgroup.
 template <int V>
 __global__ __launch_bounds__(kThreads) void route_one_kernel(RouteArgs a) {
@@ -262,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
   for (int e = threadIdx.x; e < Ep; e += kThreads) a.hist[(int64_t)blockIdx.x * Ep + e] = e < a.E ? (uint16_t)counts[e] : 0;
 }
 
-__global__ __launch_bounds__(kThreads) void group_kernel(RouteArgs a, int units) {
+__global__ __launch_bounds__(kThreads) void group_kernel(GroupArgs a, int units) {
   __shared__ int part_all[kThreads][4], part_before[kThreads][4];
   __shared__ GroupLds s;
   // four experts a thread, a power of two of threads side by side, the units
@@ -313,10 +207,14 @@ void launch_route(const RouteArgs& a, hipStream_t st) {
   }
   const int units = (a.T + a.tokens - 1) / a.tokens;
   hipLaunchKernelGGL(route_kernel<V>, dim3((unsigned)units), dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL(group_kernel, dim3((unsigned)((units + kUnits - 1) / kUnits)), dim3(kThreads), 0, st, a, units);
+  launch_group_units(a, units, st);
 }
 
 }  // namespace
+
+void launch_group_units(const GroupArgs& a, int units, hipStream_t st) {
+  hipLaunchKernelGGL(group_kernel, dim3((unsigned)((units + kUnits - 1) / kUnits)), dim3(kThreads), 0, st, a, units);
+}
 
 size_t route_hist_bytes(int T, int E, int k) {
   // what any smaller number of tokens may need too: up to 256 units of the least

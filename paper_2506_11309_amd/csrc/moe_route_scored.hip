@@ -1,0 +1,240 @@
+// Router of a mixture of experts by probabilities or gates: scores, a bias for
+// balance, groups of experts, top-k, renormalised weights; then the grouping of
+// moe_route.hip.
+//
+// s_e is the softmax or the sigmoid of a score, computed in 64 bits and rounded to 32;
+// c_e = s_e + b_e in 32 bits decides.  64 bits, because experts whose c differ by a
+// step of 2^-24 must come out in the same order whatever computes them.  A group's
+// value is its largest c, or the sum of its two largest; the best groups' experts are
+// compared.  c is compared as a 32-bit key that ascends with the value, 0 where the
+// expert is masked; equal keys go to the lower index.
+#include "moe_group_device.h"
+
+namespace ss {
+
+namespace {
+
+struct ScoredArgs : GroupArgs {
+  const void* logits;
+  int64_t ldl;
+  const float* bias;
+  int groups, size, top_groups, best;  // size: experts of a group
+  uint32_t per;                        // ceil(2^18 / size): e * per >> 18 is e's group
+  bool renormalize;
+  float scale;
+};
+
+__device__ __forceinline__ uint32_t row_min(uint32_t v) { return ~row_max(~v); }
+__device__ __forceinline__ double row_sum(double v) {
+  auto rotate = [](double d, auto by) {
+    constexpr int kBy = decltype(by)::value;
+    const uint64_t b = bitcast<uint64_t>(d);
+    return bitcast<double>((uint64_t)rotated<kBy>((uint32_t)(b >> 32)) << 32 | rotated<kBy>((uint32_t)b));
+  };
+  v += rotate(v, std::integral_constant<int, 8>{});
+  v += rotate(v, std::integral_constant<int, 4>{});
+  v += rotate(v, std::integral_constant<int, 2>{});
+  return v + rotate(v, std::integral_constant<int, 1>{});
+}
+
+// ascending key of a float, 0 for -inf and NaN
+__device__ __forceinline__ uint32_t value_key(float c) {
+  const uint32_t b = bitcast<uint32_t>(c);
+  return c > -__builtin_inff() ? (b & 0x80000000u ? ~b : b | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float key_value(uint32_t key) {
+  return bitcast<float>(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
+
+// score e of a row, +inf as the largest finite value
+template <typename T>
+__device__ __forceinline__ float score_at(const T* row, int e) {
+  if constexpr (sizeof(T) == 2) {
+    const float x = h2f(row[e]);
+    return x == __builtin_inff() ? 65504.f : x;
+  } else {
+    const float x = row[e];
+    return x == __builtin_inff() ? 3.4028234663852886e38f : x;
+  }
+}
+
+// 16 lanes take a token, V scores each: e = lane + 16 i.  room: V * 16 words of LDS of
+// this token.  Lane j < k keeps the j-th expert.  Where t >= T nothing is written.
+template <int V, bool SIGMOID, typename T>
+__device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, int* counts, int16_t* chosen, uint32_t* room) {
+  const int l = lane_id() & 15;
+  const bool there = t < a.T;
+  const T* row = static_cast<const T*>(a.logits) + (int64_t)(there ? t : 0) * a.ldl;
+  float x[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = l + 16 * i < a.E ? score_at(row, l + 16 * i) : -__builtin_inff();
+  float top = 0.f;
+  double total = 1.0;
+  if constexpr (!SIGMOID) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m = max(m, value_key(x[i]));
+    m = row_max(m);
+    top = m ? key_value(m) : 0.f;
+    total = 0.0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (x[i] > -__builtin_inff()) total += exp((double)x[i] - (double)top);
+    total = row_sum(total);
+  }
+  auto gate = [&](float v) {
+    return (float)(SIGMOID ? 1.0 / (1.0 + exp(-(double)v)) : exp((double)v - (double)top) / total);
+  };
+  uint32_t key[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = l + 16 * i;
+    key[i] = 0;
+    if (x[i] > -__builtin_inff()) key[i] = value_key(gate(x[i]) + (a.bias ? a.bias[e] : 0.f));
+  }
+  if (a.top_groups < a.groups) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (l + 16 * i < a.E) room[l + 16 * i] = key[i];
+    __builtin_amdgcn_wave_barrier();
+    for (int g = l; g < a.groups; g += 16) {
+      // its two largest; the lanes start at different members, so that they read
+      // different banks
+      uint32_t* mine = room + g * a.size;
+      uint32_t first = 0, second = 0;
+      int at = l % a.size;
+      for (int i = 0; i < a.size; ++i) {
+        const uint32_t v = mine[at];
+        second = max(second, min(first, v));
+        first = max(first, v);
+        at = at + 1 == a.size ? 0 : at + 1;
+      }
+      if (a.best == 2 && second) first = value_key(key_value(first) + key_value(second));
+      mine[0] = first;  // only this lane reads it as a member
+    }
+    __builtin_amdgcn_wave_barrier();
+    uint32_t taken = 0;
+    for (int g = l, i = 0; g < a.groups; g += 16, ++i) {
+      const uint32_t v = room[g * a.size];
+      int before = 0;
+      for (int o = 0; o < a.groups; ++o) {
+        const uint32_t w = room[o * a.size];
+        before += w > v || (w == v && o < g);
+      }
+      taken |= (uint32_t)(before < a.top_groups) << i;
+    }
+    __builtin_amdgcn_wave_barrier();
+    for (int g = l, i = 0; g < a.groups; g += 16, ++i) room[g * a.size] = taken >> i & 1;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int e = min(l + 16 * i, a.E - 1);
+      if (!room[((uint32_t)e * a.per >> 18) * a.size]) key[i] = 0;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  int mine = -1;
+  for (int j = 0; j < a.k; ++j) {
+    uint32_t m = 0, e = ~0u;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m = max(m, key[i]);
+    m = row_max(m);
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i) e = key[i] == m ? (uint32_t)(l + 16 * i) : e;
+    e = row_min(e);
+    if (!m) break;  // of this token: its lanes leave together
+    if (l == j) mine = (int)e;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if ((uint32_t)(l + 16 * i) == e) key[i] = 0;
+  }
+  const float s = mine >= 0 ? gate(score_at(row, mine)) : 0.f;
+  const double sum = a.renormalize ? row_sum((double)s) : 1.0;
+  if (l < a.k && there) {
+    a.experts[(int64_t)t * a.k + l] = mine;
+    a.weights[(int64_t)t * a.k + l] = sum > 0.0 ? (float)((double)s / sum * (double)a.scale) : 0.f;
+    if (chosen) chosen[t * a.k + l] = (int16_t)mine;
+    if (mine >= 0) atomicAdd(counts + mine, 1);
+  }
+}
+
+// Choose the experts of tokens t0 .. t1 and count them; `chosen` (LDS, nullable)
+// receives them too, -1 for none.  room: V * 16 words for each of 64 tokens.
+template <int V, bool SIGMOID, typename T>
+__device__ __forceinline__ void route_scored_tokens(const ScoredArgs& a, int t0, int t1, int* counts, int16_t* chosen, uint32_t* room) {
+  for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
+  __syncthreads();
+  for (int t = t0 + 4 * (int)(threadIdx.x >> 6); t < t1; t += kThreads / 16) {
+    const int mine = t + (lane_id() >> 4);
+    route_scored_token<V, SIGMOID, T>(a, mine < t1 ? mine : a.T, counts, chosen, room + (threadIdx.x >> 4) * (V * 16));
+  }
+  __syncthreads();
+}
+
+// Few tokens (up to 1024 pairs): everything in one workgroup.
+template <int V, bool SIGMOID, typename T>
+__global__ __launch_bounds__(kThreads) void route_scored_one_kernel(ScoredArgs a) {
+  __shared__ int counts[kMaxE];
+  __shared__ int16_t chosen[kThreads];
+  __shared__ union {
+    uint32_t room[kThreads / 16 * V * 16];
+    GroupLds group;
+  } s;
+  route_scored_tokens<V, SIGMOID, T>(a, 0, a.T, counts, chosen, s.room);
+  group_tokens(a, 0, a.T, (int)threadIdx.x < a.E ? counts[threadIdx.x] : 0, 0, true, chosen, -1, s.group);
+}
+
+// More: count, then place.
+template <int V, bool SIGMOID, typename T>
+__global__ __launch_bounds__(kThreads) void route_scored_kernel(ScoredArgs a) {
+  __shared__ int counts[kMaxE];
+  __shared__ uint32_t room[kThreads / 16 * V * 16];
+  const int t0 = blockIdx.x * a.tokens;
+  route_scored_tokens<V, SIGMOID, T>(a, t0, min(a.T, t0 + a.tokens), counts, nullptr, room);
+  const int Ep = (a.E + 3) & ~3;
+  for (int e = threadIdx.x; e < Ep; e += kThreads) a.hist[(int64_t)blockIdx.x * Ep + e] = e < a.E ? (uint16_t)counts[e] : 0;
+}
+
+template <int V, bool SIGMOID, typename T>
+void launch_scored(const ScoredArgs& a, hipStream_t st) {
+  if ((int64_t)a.T * a.k <= kThreads && a.T <= kLeast) {
+    hipLaunchKernelGGL((route_scored_one_kernel<V, SIGMOID, T>), dim3(1), dim3(kThreads), 0, st, a);
+    return;
+  }
+  const int units = (a.T + a.tokens - 1) / a.tokens;
+  hipLaunchKernelGGL((route_scored_kernel<V, SIGMOID, T>), dim3((unsigned)units), dim3(kThreads), 0, st, a);
+  launch_group_units(a, units, st);
+}
+
+template <bool SIGMOID, typename T>
+void launch_width(const ScoredArgs& a, hipStream_t st) {
+  const int v = (a.E + 15) / 16;  // scores of a lane
+  if (v <= 1) launch_scored<1, SIGMOID, T>(a, st);
+  else if (v <= 2) launch_scored<2, SIGMOID, T>(a, st);
+  else if (v <= 4) launch_scored<4, SIGMOID, T>(a, st);
+  else if (v <= 8) launch_scored<8, SIGMOID, T>(a, st);
+  else if (v <= 16) launch_scored<16, SIGMOID, T>(a, st);
+  else launch_scored<32, SIGMOID, T>(a, st);
+}
+
+}  // namespace
+
+void launch_moe_route_scored(const ScoredLaunch& L, hipStream_t st) {
+  ScoredArgs a;
+  static_cast<GroupArgs&>(a) = L.group;
+  a.tokens = unit_tokens(a.T, a.k);
+  a.logits = L.logits;
+  a.ldl = L.ldl;
+  a.bias = L.bias;
+  a.groups = L.groups;
+  a.size = a.E / L.groups;
+  a.top_groups = L.top_groups;
+  a.best = L.best;
+  a.per = ((1u << 18) + a.size - 1) / a.size;
+  a.renormalize = L.renormalize;
+  a.scale = L.scale;
+  if (L.sigmoid) L.wide ? launch_width<true, float>(a, st) : launch_width<true, uint16_t>(a, st);
+  else L.wide ? launch_width<false, float>(a, st) : launch_width<false, uint16_t>(a, st);
+}
+
+}  // namespace ss

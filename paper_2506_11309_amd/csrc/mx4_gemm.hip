@@ -19,13 +19,6 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// A lane offset past the end of every buffer of activations (they stay below 2 GiB):
-// such a load gives zeros.  The uniform offset beside it may not count in the range
-// check: it stays inside the buffer, and is 0 where all lanes are outside.  (Of a
-// matrix of more than 2 GiB the load reads other codes of it, which then meet rows
-// of zeros or none.)
-constexpr uint32_t kOutside = 0x80000000u;
-
 // c += W (16 columns x 128) . A (16 rows x 128); byte J of the weights' scale word, JA of the rows'
 template <int J, int JA = J>
 __device__ __forceinline__ f32x4 mfma_mx4(const u32x4& w, uint32_t ws, const u32x4& a, uint32_t as, const f32x4& c) {
@@ -42,131 +35,15 @@ __device__ __forceinline__ f32x16 mfma_mx4_32(const u32x4& w, uint32_t ws, const
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w8, a8, c, 4, 4, J, (int)ws, J, (int)as);
 }
 
-struct Mx4Args {
+struct Mx4Args : ProductArgs {
   const uint8_t *w0, *w1;    // codes; the scales follow all codes
   const uint8_t *s0, *s1;
   int64_t w_stride, s_stride;  // bytes of one expert
-  int G, G4, Nt, N;
+  int G, G4;
   const uint8_t *a, *as;
   uint32_t a_bytes, as_bytes;
-  int M;
-  const int32_t* map;   // {expert, first row, rows, 0} per row block, or null
-  const int32_t* rows;
-  int div;
-  uint16_t* y;
-  int64_t ldy;
-  const uint16_t* res;
-  int64_t ldr;
-  float* part;
-  void* ws;
-  int col_blocks;
-  int split;  // shares of K, each with its own part [M][N]
-  bool past;  // results go past the caches
-  // rows quantised by the product itself
-  const uint16_t* x;
-  uint32_t x_row, x_bytes;  // bytes from row to row, of all rows
   int blocks;               // blocks of 32 columns of a row
-  const int32_t* offsets;
-  int E;
 };
-
-__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
-
-// the row block of a workgroup: expert, first output row, number of rows
-struct RowBlock {
-  int e, m0, n;
-};
-__device__ __forceinline__ RowBlock row_block(const Mx4Args& a, int rb, int TM) {
-  if (!a.map) return RowBlock{0, rb * TM, min(TM, a.M - rb * TM)};
-  // written by an earlier launch: read through the scalar cache
-  const auto* p = (const __attribute__((address_space(4))) int32_t*)(a.map + 4 * ((int64_t)rb + 1));
-  return RowBlock{p[0], p[1], p[2]};
-}
-
-// The same from the offsets (as Mx4Map describes it), by each wave for itself.
-__device__ __forceinline__ RowBlock find_block(const Mx4Args& a, int rb, int TM, bool first) {
-  if (!a.offsets) return RowBlock{0, rb * TM, min(TM, a.M - rb * TM)};
-  const int lane = lane_id();
-  RowBlock r{0, 0, 0};
-  bool bad = false;
-  int base = 0;
-  for (int e0 = 0; e0 < a.E; e0 += kWave) {
-    const int e = e0 + lane;
-    const int lo = e < a.E ? a.offsets[e] : 0, hi = e < a.E ? a.offsets[e + 1] : 0;
-    bad = bad || __any(lo < 0 || hi < lo || hi > a.M || (e == 0 && lo != 0));
-    const int n = bad ? 0 : (hi - lo + TM - 1) / TM;
-    const int s = wave_scan_add(n);
-    const uint64_t past = __ballot(base + s > rb);
-    if (past && r.n == 0) {
-      const int l = __builtin_ctzll(past);
-      r.e = e0 + l;
-      r.m0 = __builtin_amdgcn_readlane(lo + (rb - (base + s - n)) * TM, l);
-      r.n = min(TM, __builtin_amdgcn_readlane(hi, l) - r.m0);
-    }
-    base += __builtin_amdgcn_readlane(s, 63);
-  }
-  if (first && lane == 0) {  // one wave of the launch
-    if (bad) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-    int32_t* map = const_cast<int32_t*>(a.map);
-    map[0] = !bad;
-    map[1] = bad ? 0 : a.offsets[a.E];
-  }
-  if (bad) r.n = 0;
-  return RowBlock{__builtin_amdgcn_readfirstlane(r.e), __builtin_amdgcn_readfirstlane(r.m0), __builtin_amdgcn_readfirstlane(r.n)};
-}
-
-// Workgroup -> row and column block of a tile.  Tiles are taken in bands of 4 row
-// blocks, column by column, and stretches of 32 of them (what a chiplet's
-// compute units run at one time) go to the 8 chiplets in turn, as workgroups do:
-// what a chiplet reads is then a few row blocks and 8 column blocks, out of its
-// own L2, and the empty row blocks at the end of a list of experts (they come
-// last) are no chiplet's alone.
-__device__ __forceinline__ void place_of(const Mx4Args& a, int& rb, int& cb) {
-  const int all = gridDim.x, x = blockIdx.x & 7, s = blockIdx.x >> 3;
-  const int id = (int)blockIdx.x < (all & ~255) ? (((s >> 5) << 3) + x) * 32 + (s & 31) : (int)blockIdx.x;
-  const int band = id / (4 * a.col_blocks), in = id - band * 4 * a.col_blocks;
-  const int high = min(4, all / a.col_blocks - 4 * band);
-  rb = 4 * band + in % high;
-  cb = in / high;
-}
-
-// activation row that output row m reads, or -1 where the caller's list is wrong
-__device__ __forceinline__ int source_of(const Mx4Args& a, int listed) {
-  const uint32_t r = (uint32_t)listed;
-  if (r >= (uint32_t)a.M) {
-    report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-    return -1;
-  }
-  return (int)(r / (uint32_t)a.div);
-}
-__device__ __forceinline__ int source_row(const Mx4Args& a, int m) { return a.rows ? source_of(a, a.rows[m]) : m; }
-
-// four columns n .. n + 3 of output row m
-__device__ __forceinline__ u32x2 residual(const Mx4Args& a, int64_t m, int n) {
-  return *reinterpret_cast<const u32x2*>(a.res + m * a.ldr + n);
-}
-__device__ __forceinline__ void add_residual(f32x4& v, u32x2 r) {
-  v[0] += h2f((uint16_t)r[0]);
-  v[1] += h2f((uint16_t)(r[0] >> 16));
-  v[2] += h2f((uint16_t)r[1]);
-  v[3] += h2f((uint16_t)(r[1] >> 16));
-}
-__device__ __forceinline__ u32x2 pack4(const f32x4& v) {
-  return u32x2{f2h(v[0]) | (uint32_t)f2h(v[1]) << 16, f2h(v[2]) | (uint32_t)f2h(v[3]) << 16};
-}
-// 16 bytes to an address of 8-byte alignment
-__device__ __forceinline__ void store_rows16(uint16_t* p, const u32x4& v, bool past) {
-  typedef uint32_t Line __attribute__((ext_vector_type(4), aligned(8)));
-  if (past) __builtin_nontemporal_store(v, reinterpret_cast<Line*>(p));
-  else *reinterpret_cast<Line*>(p) = v;
-}
-template <Mx4Epilogue EPI>
-__device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f32x4 v) {
-  if constexpr (EPI == MX4_ROWS)
-    *reinterpret_cast<f32x4*>(a.part + m * a.N + n) = v;
-  else
-    *reinterpret_cast<u32x2*>(a.y + m * a.ldy + n) = pack4(v);
-}
 
 // ------------------------------------------------------------ few rows
 // W waves of a workgroup own NT column tiles (SwiGLU: NT/2 gate and NT/2 up
@@ -180,9 +57,9 @@ __device__ __forceinline__ void write_out(const Mx4Args& a, int64_t m, int n, f3
 // Bound by launch, first loads and drain for small matrices, by the weights' bytes
 // for large ones: 32 rows of 8192 x 8192 (36 MB) 11.4 us, 3.1 TB/s; SwiGLU of a
 // token through 8 experts 2048 x 1024 (18 MB) 8.0 us in one launch.
-template <int W, int MT, int NT, int U, bool RAW, Mx4Epilogue EPI>
+template <int W, int MT, int NT, int U, bool RAW, Epilogue EPI>
 __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
-  constexpr bool SW = EPI == MX4_SWIGLU;
+  constexpr bool SW = EPI == OUT_SWIGLU;
   constexpr int kC = SW ? NT / 2 : NT;
   __shared__ f32x4 red[W][MT * NT][kWave];
   const int lane = lane_id();
@@ -311,7 +188,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
   for (int j = 0; j < MT; ++j) writes = writes && (j != mt || live[j]);
   u32x2 add = {0u, 0u};
-  if (EPI == MX4_RESIDUAL && writes) add = residual(a, m, n);
+  if (EPI == OUT_RESIDUAL && writes) add = residual(a, m, n);
   for (int c = c0; c < c1; c += 2) {
     if (c + 1 < c1) load(s[1], c + 1);
     multiply(s[0], c);
@@ -337,7 +214,7 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = silu(v[i]) * u[i];
   }
-  if constexpr (EPI == MX4_RESIDUAL) add_residual(v, add);
+  if constexpr (EPI == OUT_RESIDUAL) add_residual(v, add);
   write_out<EPI>(a, m, n, v);
 }
 
@@ -371,9 +248,9 @@ __global__ __launch_bounds__(64 * W) void mx4_stream_kernel(Mx4Args a) {
 // g + 3 and g + 4 (g odd), the weights of group g + 4.
 constexpr int kTurnRow = 144;  // bytes of a 128-byte line with its padding
 
-template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
+template <int WM, int WN, int MTW, int NTW, Epilogue EPI>
 __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
-  constexpr bool SW = EPI == MX4_SWIGLU;
+  constexpr bool SW = EPI == OUT_SWIGLU;
   constexpr int AT = WM * MTW, WT = WN * NTW, TM = 16 * AT;
   constexpr int kA = 2 * AT / 4, kW = WT / 4, kS = (AT + WT) / 4;  // loads of a wave: two groups of rows, a group of weights, scales
   constexpr int kC = SW ? WT / 2 : WT;   // output column tiles of the workgroup
@@ -560,7 +437,7 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   // row lane % 32 (SwiGLU: gate columns for q < 2, their up columns after them).
   // Through LDS the rows come out as whole 128-byte lines: 64 fp16 columns, or 32
   // fp32 ones (results that a residual or another sum awaits).
-  constexpr bool wide = EPI == MX4_ROWS || EPI == MX4_RESIDUAL;
+  constexpr bool wide = EPI == OUT_ROWS || EPI == OUT_RESIDUAL;
   constexpr int kPC = SW ? 16 : 32;             // columns of a pair
   constexpr int kPL = wide ? 1 : 64 / kPC;      // pairs of a line
   constexpr int kLines = (kNP + kPL - 1) / kPL;  // of 32 rows, all in LDS at one time
@@ -571,8 +448,8 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   // The residual is loaded at once, into the registers that the operands leave: eight
   // rows at a time cost 16 latencies (1946 rows of 2208 x 5296: 42 against 31 us,
   // 2048 of 8192 x 8192 90 against 84).
-  u32x2 add[EPI == MX4_RESIDUAL ? kMP : 1][4][kLines];
-  if constexpr (EPI == MX4_RESIDUAL) {
+  u32x2 add[EPI == OUT_RESIDUAL ? kMP : 1][4][kLines];
+  if constexpr (EPI == OUT_RESIDUAL) {
 #pragma unroll
     for (int i = 0; i < kMP; ++i)
 #pragma unroll
@@ -616,11 +493,11 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
         constexpr int kAll = kPC * kNP;  // columns of the wave
         const int in = kPC * kPL * l + (wide ? 4 : 8) * tc, col = 16 * (t0 + wn * kCW) + in;
         if (!write || in >= kAll || col >= a.N) continue;
-        if constexpr (EPI == MX4_ROWS) {
+        if constexpr (EPI == OUT_ROWS) {
           u32x4* p = reinterpret_cast<u32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + col);
           if (a.past) __builtin_nontemporal_store(v[l], p);
           else *p = v[l];
-        } else if constexpr (EPI == MX4_RESIDUAL) {
+        } else if constexpr (EPI == OUT_RESIDUAL) {
           f32x4 f = bitcast<f32x4>(v[l]);
           add_residual(f, add[i][u][l]);
           *reinterpret_cast<u32x2*>(a.y + m * a.ldy + col) = pack4(f);
@@ -633,88 +510,16 @@ __global__ __launch_bounds__(256, 1) void mx4_tile_kernel(Mx4Args a) {
   }
 }
 
-// ---------------------------------------------------------------- combine
-// One thread per 4 columns of a token; the addends in slot order, KU of them
-// loaded at a time, each the sum of `split` parts in order.  Nothing is written where the offsets were invalid (map[0]).
-// Bound by the fp32 rows that it reads: 5000 tokens of 8 slots (10 % of them masked)
-// x 2048 columns, 295 MB, 50 us (5.9 TB/s).
-template <int KU>
-__global__ __launch_bounds__(256) void moe_combine_kernel(const float* __restrict__ part, int split, int T, int k, int N,
-                                                          const int32_t* __restrict__ pos,
-                                                          const int32_t* __restrict__ map,
-                                                          const float* __restrict__ weights, uint16_t* y, int64_t ldy,
-                                                          const uint16_t* res, int64_t ldr, void* ws) {
-  const int per = N / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t t = i / per;
-  if (t >= T) return;
-  const int n = (int)(i - t * per) * 4;
-  // the lists and the residual are read side by side
-  const int valid = map[0], used = map[1];
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (res) add_residual(v, *reinterpret_cast<const u32x2*>(res + t * ldr + n));
-  for (int j0 = 0; j0 < k; j0 += KU) {
-    int p[KU];
-    float w[KU];
-    f32x4 o[KU];
-#pragma unroll
-    for (int j = 0; j < KU; ++j) {
-      const int64_t at = t * k + min(j0 + j, k - 1);
-      p[j] = pos[at];
-      w[j] = weights[at];
-    }
-    if (!valid) return;
-#pragma unroll
-    for (int j = 0; j < KU; ++j) {
-      if (j0 + j >= k) p[j] = -1;
-      if (p[j] >= used) {
-        report_error(ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-        p[j] = -1;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < KU; ++j)
-      if (p[j] >= 0) o[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(part + (int64_t)p[j] * N + n));
-#pragma unroll
-    for (int j = 0; j < KU; ++j)
-      if (p[j] >= 0) {
-        for (int s = 1; s < split; ++s) o[j] += *reinterpret_cast<const f32x4*>(part + ((int64_t)s * T * k + p[j]) * N + n);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = __builtin_fmaf(w[j], o[j][c], v[c]);
-      }
-  }
-  *reinterpret_cast<u32x2*>(y + t * ldy + n) = pack4(v);
-}
-
-// y = fp16(the sum of `split` parts [M][N] in order + residual); 4 columns a thread.
-// The parts were just written: bound by its launch and one round of reads.
-__global__ __launch_bounds__(256) void mx4_sum_kernel(const float* __restrict__ part, int split, int M, int N, uint16_t* y, int64_t ldy,
-                                                      const uint16_t* res, int64_t ldr) {
-  const int per = N / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t m = i / per;
-  if (m >= M) return;
-  const int n = (int)(i - m * per) * 4;
-  const float* p = part + m * N + n;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  u32x2 r = {0u, 0u};
-  if (res) r = *reinterpret_cast<const u32x2*>(res + m * ldr + n);
-#pragma unroll 8
-  for (int s = 0; s < split; ++s) v += *reinterpret_cast<const f32x4*>(p + (int64_t)s * M * N);
-  add_residual(v, r);
-  *reinterpret_cast<u32x2*>(y + m * ldy + n) = pack4(v);
-}
-
-template <int W, int MT, int NT, bool RAW, Mx4Epilogue EPI>
+template <int W, int MT, int NT, bool RAW, Epilogue EPI>
 void launch_stream(Mx4Args a, int blocks, hipStream_t st) {
-  constexpr int kC = EPI == MX4_SWIGLU ? NT / 2 : NT;
+  constexpr int kC = EPI == OUT_SWIGLU ? NT / 2 : NT;
   a.col_blocks = (a.Nt + kC - 1) / kC;
   hipLaunchKernelGGL((mx4_stream_kernel<W, MT, NT, 2, RAW, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(64 * W), 0, st, a);
 }
 
-template <int WM, int WN, int MTW, int NTW, Mx4Epilogue EPI>
+template <int WM, int WN, int MTW, int NTW, Epilogue EPI>
 void launch_tile(Mx4Args a, int blocks, hipStream_t st) {
-  constexpr int kC = EPI == MX4_SWIGLU ? WN * NTW / 2 : WN * NTW;
+  constexpr int kC = EPI == OUT_SWIGLU ? WN * NTW / 2 : WN * NTW;
   a.col_blocks = (a.Nt + kC - 1) / kC;
   hipLaunchKernelGGL((mx4_tile_kernel<WM, WN, MTW, NTW, EPI>), dim3((unsigned)blocks * a.col_blocks, a.split), dim3(256), 0, st, a);
 }
@@ -798,13 +603,13 @@ Mx4Plan plan_mx4_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
 
 namespace {
 
-template <Mx4Epilogue EPI>
+template <Epilogue EPI>
 void launch_form(const Mx4Plan& p, const Mx4Args& a, int blocks, hipStream_t st) {
   switch (p.form) {
     case STREAM_RAW: return launch_stream<8, 1, 2, true, EPI>(a, blocks, st);
     case STREAM_1: return launch_stream<8, 1, 2, false, EPI>(a, blocks, st);
     case STREAM_2:
-      if constexpr (EPI == MX4_PLAIN || EPI == MX4_RESIDUAL) launch_stream<8, 2, 2, false, EPI>(a, blocks, st);
+      if constexpr (EPI == OUT_PLAIN || EPI == OUT_RESIDUAL) launch_stream<8, 2, 2, false, EPI>(a, blocks, st);
       return;
     case TILE_64: return launch_tile<1, 4, 4, 2, EPI>(a, blocks, st);
     case TILE_128: return launch_tile<2, 2, 4, 4, EPI>(a, blocks, st);
@@ -814,18 +619,18 @@ void launch_form(const Mx4Plan& p, const Mx4Args& a, int blocks, hipStream_t st)
 
 }  // namespace
 
-int launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
+int launch_mx4_gemm(const ProductLaunch& L, hipStream_t st) {
   // rows that the product may read itself: within a 2 GiB buffer, not overwritten
   const uint64_t x_bytes = ((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2;
-  const Mx4Plan p = plan_mx4_gemm(L.M, L.E, L.K, L.N, L.epi == MX4_SWIGLU, L.offsets, x_bytes < kOutside && !L.x_written);
+  const Mx4Plan p = plan_mx4_gemm(L.M, L.E, L.K, L.N, L.epi == OUT_SWIGLU, L.offsets, x_bytes < kOutside && !L.x_written);
   // 32 rows a workgroup: one matrix whose K is whole
   if (p.form == STREAM_2 && (L.offsets || p.split > 1)) return 0;
-  Mx4Map map = {};
+  RowMap map = {};
   map.offsets = L.offsets;
   map.E = L.E;
   map.M = L.M;
   map.tm = p.tm;
-  map.blocks = L.offsets ? mx4_row_blocks(L.M, L.E, p.tm) : (L.M + p.tm - 1) / p.tm;
+  map.blocks = L.offsets ? row_blocks(L.M, L.E, p.tm) : (L.M + p.tm - 1) / p.tm;
   map.map = L.map;
   map.ws = L.ws;
   if (p.form != STREAM_RAW) launch_mx4_prepare(L.x, L.a_rows, L.K, L.ldx, L.a, L.a_scales, L.rows ? nullptr : L.offsets, map, st);
@@ -862,22 +667,21 @@ int launch_mx4_gemm(const Mx4Launch& L, hipStream_t st) {
   // An expert product's results of more than the L2s hold go past them, so that
   // the weights stay (8191 tokens' SwiGLU 194 -> 186 us; 5000 tokens' down product
   // with its combination 203 -> 179 us); parts of a split K are read at once.
-  a.past = L.offsets && (int64_t)L.M * L.N * (L.epi == MX4_ROWS ? 4 : 2) > (32 << 20);
+  a.past = L.offsets && (int64_t)L.M * L.N * (L.epi == OUT_ROWS ? 4 : 2) > (32 << 20);
   a.blocks = L.K / 32;
   a.offsets = L.offsets;
   a.E = L.E;
-  if (L.epi == MX4_SWIGLU) {
-    launch_form<MX4_SWIGLU>(p, a, map.blocks, st);
-  } else if (L.epi == MX4_ROWS) {
-    launch_form<MX4_ROWS>(p, a, map.blocks, st);
+  if (L.epi == OUT_SWIGLU) {
+    launch_form<OUT_SWIGLU>(p, a, map.blocks, st);
+  } else if (L.epi == OUT_ROWS) {
+    launch_form<OUT_ROWS>(p, a, map.blocks, st);
   } else if (p.split > 1) {
-    launch_form<MX4_ROWS>(p, a, map.blocks, st);
-    hipLaunchKernelGGL(mx4_sum_kernel, dim3((unsigned)(((int64_t)L.M * (L.N / 4) + 255) / 256)), dim3(256), 0, st, L.part, p.split,
-                       L.M, L.N, L.y, L.ldy, L.res, L.ldr);
+    launch_form<OUT_ROWS>(p, a, map.blocks, st);
+    launch_product_sum(L.part, p.split, L.M, L.N, L.y, L.ldy, L.res, L.ldr, st);
   } else if (L.res) {
-    launch_form<MX4_RESIDUAL>(p, a, map.blocks, st);
+    launch_form<OUT_RESIDUAL>(p, a, map.blocks, st);
   } else {
-    launch_form<MX4_PLAIN>(p, a, map.blocks, st);
+    launch_form<OUT_PLAIN>(p, a, map.blocks, st);
   }
   return p.split;
 }
@@ -886,7 +690,7 @@ bool mx4_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped) {
   if (M < 1) return true;
   for (bool raw : {false, true}) {
     const Mx4Plan p = plan_mx4_gemm(M, E, K, N, swiglu, grouped, raw);
-    const int64_t blocks = grouped ? mx4_row_blocks(M, E, p.tm) : (M + p.tm - 1) / p.tm;
+    const int64_t blocks = grouped ? row_blocks(M, E, p.tm) : (M + p.tm - 1) / p.tm;
     const int64_t columns = ((int64_t)N * (swiglu ? 2 : 1) + kColumnsOf[p.form] - 1) / kColumnsOf[p.form];
     if (blocks * columns * (p.form <= STREAM_2 ? 512 : 256) >= 1ll << 32) return false;
   }
@@ -917,15 +721,6 @@ size_t mx4_rows_bytes_most(int64_t M, int K, int N) {
   // one part, or as many as plan_mx4_gemm allows of at most 256 tiles
   const size_t one = (size_t)M * N * sizeof(float), all = std::max<int64_t>((mx4_groups(K) + 3) / 4 / 2, 1) * one;
   return std::max(one, std::min(all, (size_t)256 * 128 * 128 * sizeof(float)));
-}
-
-void launch_moe_combine(const float* part, int split, int T, int k, int N, const int32_t* pos, const int32_t* map,
-                        const float* weights, uint16_t* y, int64_t ldy, const uint16_t* res, int64_t ldr, void* ws,
-                        hipStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)T * (N / 4) + 255) / 256));
-  if (k <= 2) hipLaunchKernelGGL(moe_combine_kernel<2>, grid, dim3(256), 0, st, part, split, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
-  else if (k <= 4) hipLaunchKernelGGL(moe_combine_kernel<4>, grid, dim3(256), 0, st, part, split, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
-  else hipLaunchKernelGGL(moe_combine_kernel<8>, grid, dim3(256), 0, st, part, split, T, k, N, pos, map, weights, y, ldy, res, ldr, ws);
 }
 
 }  // namespace ss

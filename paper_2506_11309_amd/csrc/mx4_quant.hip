@@ -29,65 +29,6 @@ __device__ __forceinline__ uint32_t quantize8(const u32x4& v, uint32_t& scale) {
   return mx4_codes(v, scale);
 }
 
-// One workgroup writes the row blocks of a product (Mx4Map).
-__device__ void write_map(const Mx4Map& m) {
-  constexpr int kPer = SWIFTSPEC_MAX_EXPERTS / 256;
-  __shared__ int first[SWIFTSPEC_MAX_EXPERTS + 1];  // blocks before expert e
-  __shared__ int begin[SWIFTSPEC_MAX_EXPERTS], end[SWIFTSPEC_MAX_EXPERTS];
-  __shared__ int wave_sum[4];
-  __shared__ int bad;
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
-  if (tid == 0) bad = 0;
-  __syncthreads();
-  int n[kPer], sum = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = tid * kPer + i;
-    n[i] = 0;
-    if (e < m.E) {
-      const int lo = m.offsets[e], hi = m.offsets[e + 1];
-      begin[e] = lo;
-      end[e] = hi;
-      if (lo < 0 || hi < lo || hi > m.M || (e == 0 && lo != 0)) bad = 1;
-      else n[i] = (hi - lo + m.tm - 1) / m.tm;
-    }
-    sum += n[i];
-  }
-  const int s = wave_scan_add(sum);
-  if (lane == 63) wave_sum[wave] = s;
-  __syncthreads();
-  int at = s - sum;
-  for (int w = 0; w < wave; ++w) at += wave_sum[w];
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = tid * kPer + i;
-    if (e < m.E) first[e] = at;
-    at += n[i];
-    if (e == m.E - 1) first[m.E] = at;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    if (bad) report_error(m.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
-    m.map[0] = !bad;
-    m.map[1] = bad ? 0 : end[m.E - 1];
-  }
-  const int used = bad ? 0 : first[m.E];
-  for (int i = tid; i < m.blocks; i += 256) {
-    u32x4 v = {0u, 0u, 0u, 0u};
-    if (i < used) {
-      int lo = 0, hi = m.E - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (first[mid] <= i) lo = mid;
-        else hi = mid - 1;
-      }
-      const int m0 = begin[lo] + (i - first[lo]) * m.tm;
-      v = u32x4{(uint32_t)lo, (uint32_t)m0, (uint32_t)min(m.tm, end[lo] - m0), 0u};
-    }
-    *reinterpret_cast<u32x4*>(m.map + 4 * ((int64_t)i + 1)) = v;
-  }
-}
-
 // One thread per 8 values, kUnits of them 256 apart; 4 neighbouring lanes hold a
 // block (whole rows are multiples of 4 pieces, so a block never spans waves).
 // OPERAND: rows padded to whole groups of 128, scales in the operand order; for
@@ -96,7 +37,7 @@ __device__ void write_map(const Mx4Map& m) {
 template <bool OPERAND>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const uint16_t* __restrict__ x, int64_t M, int K, int64_t ldx,
                                                            uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                                           const int32_t* last, Mx4Map map) {
+                                                           const int32_t* last, RowMap map) {
   if constexpr (OPERAND) {
     if (map.offsets && blockIdx.x == 0) return write_map(map);
     if (last) M = min(M, (int64_t)max(last[map.E], 0));
@@ -230,11 +171,11 @@ void launch_mx4_prepack(const uint8_t* codes, const uint8_t* scales, int K, int6
 
 void launch_mx4_quantize(const uint16_t* x, int64_t M, int K, int64_t ldx, uint8_t* codes, uint8_t* scales, hipStream_t st) {
   hipLaunchKernelGGL((mx4_quantize_kernel<false>), dim3(blocks_for(M * (K / 8))), dim3(256), 0, st, x, M, K, ldx, codes, scales,
-                     (const int32_t*)nullptr, Mx4Map{});
+                     (const int32_t*)nullptr, RowMap{});
 }
 
 void launch_mx4_prepare(const uint16_t* x, int64_t M, int K, int64_t ldx, uint8_t* codes, uint8_t* scales,
-                        const int32_t* last, const Mx4Map& map, hipStream_t st) {
+                        const int32_t* last, const RowMap& map, hipStream_t st) {
   hipLaunchKernelGGL((mx4_quantize_kernel<true>), dim3(blocks_for(M * mx4_groups(K) * 16) + (map.offsets ? 1 : 0)), dim3(256), 0,
                      st, x, M, K, ldx, codes, scales, last, map);
 }

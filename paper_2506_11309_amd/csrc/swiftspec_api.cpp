@@ -9,6 +9,8 @@
 #include <new>
 
 #include "../../include/swiftspec.h"
+#include "fp8_internal.h"
+#include "moe_internal.h"
 #include "mx4_internal.h"
 #include "ss_internal.h"
 
@@ -316,57 +318,97 @@ size_t layer_ws_query(const swiftspec_dims* d, int T) {
   return most;
 }
 
-// ---- microscaled 4-bit matrices
-// Positive sizes that the calls take, before their divisibility; outside them
-// the size queries answer as if there were nothing to do, and their arithmetic
-// would not fit its types.
-bool mx4_matrices_fit(int K, int N, int E) {
-  if (E > SWIFTSPEC_MAX_EXPERTS) return false;
-  // the kernels address one matrix through a 32-bit buffer range
-  if (ss::mx4_packed_bytes(K, N, 1) > 0xFFFFFFFFull) return false;
-  // a launch has fewer than 2^32 threads
-  return ss::mx4_packed_bytes(K, N, E) < 1ull << 36;
-}
+// ---- microscaled 4-bit and block-scaled 8-bit matrices
+inline bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// What the products with the two kinds of matrix differ in.
+struct Format {
+  int k_step;          // K is a multiple of it
+  uint64_t all_bytes;  // the packed copies of all experts stay below
+  size_t (*packed_bytes)(int K, int N, int E);
+  size_t (*code_bytes)(int64_t M, int K);  // of activations in operand form
+  size_t (*scale_bytes)(int64_t M, int K);
+  size_t (*part_bytes)(int M, int K, int N);
+  size_t (*part_bytes_most)(int M, int K, int N);
+  size_t (*rows_bytes)(int M, int E, int K, int N);
+  size_t (*rows_bytes_most)(int64_t M, int K, int N);
+  bool (*grid_fits)(int M, int E, int K, int N, bool swiglu, bool grouped);
+  int (*launch)(const ss::ProductLaunch& L, hipStream_t st);
+
+  // Positive sizes that the calls take, before their divisibility; outside them
+  // the size queries answer as if there were nothing to do, and their arithmetic
+  // would not fit its types.
+  bool matrices_fit(int K, int N, int E) const {
+    if (E > SWIFTSPEC_MAX_EXPERTS) return false;
+    // the kernels address one matrix through a 32-bit buffer range
+    if (packed_bytes(K, N, 1) > 0xFFFFFFFFull) return false;
+    // a launch has fewer than 2^32 threads
+    return packed_bytes(K, N, E) < all_bytes;
+  }
+  // the quantised activations of a product lie in one 2 GiB buffer range
+  bool rows_fit(int64_t M, int K) const { return code_bytes(M, K) < 0x80000000ull; }
+};
+constexpr Format kMx4 = {32, 1ull << 36, ss::mx4_packed_bytes, ss::mx4_code_bytes, ss::mx4_scale_bytes, ss::mx4_part_bytes,
+                         ss::mx4_part_bytes_most, ss::mx4_rows_bytes, ss::mx4_rows_bytes_most, ss::mx4_grid_fits, ss::launch_mx4_gemm};
+constexpr Format kFp8 = {16, 1ull << 35, ss::fp8_packed_bytes, ss::fp8_code_bytes, ss::fp8_scale_bytes, ss::fp8_part_bytes,
+                         ss::fp8_part_bytes_most, ss::fp8_rows_bytes, ss::fp8_rows_bytes_most, ss::fp8_grid_fits, ss::launch_fp8_gemm};
+
 bool groups_fit(int T, int k, int E) {
   return E <= SWIFTSPEC_MAX_EXPERTS && k <= SWIFTSPEC_MAX_TOPK && (int64_t)T * k < (1 << 28);
 }
 
-int check_mx4_shape(const swiftspec_mx4* W) {
-  if (!W || W->K <= 0 || W->N <= 0 || W->E <= 0) return SWIFTSPEC_INVALID_ARG;
-  if (W->K % 32 || W->N % 16 || !mx4_matrices_fit(W->K, W->N, W->E)) return SWIFTSPEC_UNSUPPORTED;
+// W: swiftspec_mx4 or swiftspec_fp8
+template <typename W>
+int check_matrix_shape(const Format& f, const W* w) {
+  if (!w || w->K <= 0 || w->N <= 0 || w->E <= 0) return SWIFTSPEC_INVALID_ARG;
+  if (w->K % f.k_step || w->N % 16 || !f.matrices_fit(w->K, w->N, w->E)) return SWIFTSPEC_UNSUPPORTED;
   return SWIFTSPEC_OK;
 }
 
-int check_mx4(const swiftspec_mx4* W) {
-  int rc = check_mx4_shape(W);
+template <typename W>
+int check_matrix(const Format& f, const W* w) {
+  int rc = check_matrix_shape(f, w);
   if (rc) return rc;
-  if (!W->packed) return SWIFTSPEC_INVALID_ARG;
-  if (!aligned16(W->packed)) return SWIFTSPEC_MISALIGNED;
+  if (!w->packed) return SWIFTSPEC_INVALID_ARG;
+  if (!aligned16(w->packed)) return SWIFTSPEC_MISALIGNED;
   return SWIFTSPEC_OK;
 }
 
-inline bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
-inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+template <typename W>
+int check_prepack(const Format& f, const W* w, void* packed, size_t bytes) {
+  int rc = check_matrix_shape(f, w);
+  if (rc) return rc;
+  if (!w->codes || !w->scales || !packed) return SWIFTSPEC_INVALID_ARG;
+  if (!aligned16(w->codes) || !aligned16(packed)) return SWIFTSPEC_MISALIGNED;
+  return bytes < f.packed_bytes(w->K, w->N, w->E) ? SWIFTSPEC_WORKSPACE_TOO_SMALL : SWIFTSPEC_OK;
+}
 
-// the quantised activations of a product lie in one 2 GiB buffer range
-bool mx4_rows_fit(int64_t M, int K) { return ss::mx4_code_bytes(M, K) < 0x80000000ull; }
+// rows of K columns, rounded up to `unit`: below 2^35 values, 16 of which a thread
+// takes: a launch has fewer than 2^32 threads
+int check_quantized_rows(int64_t M, int32_t K, int64_t ld, int k_step, int unit) {
+  if (M < 0 || K <= 0 || ld < K) return SWIFTSPEC_INVALID_ARG;
+  const int64_t columns = ((int64_t)K + unit - 1) / unit * unit;
+  if (K % k_step || M > (((int64_t)1 << 35) - 1) / columns) return SWIFTSPEC_UNSUPPORTED;
+  return SWIFTSPEC_OK;
+}
 
 // Workspace of a product: the header, the activations in operand form, the map
 // of row blocks (experts; E = 0: none), fp32 results that another kernel adds.
-struct Mx4Ws {
+struct ProductWs {
   size_t codes, scales, map, part, total;
 };
-Mx4Ws mx4_ws(int64_t a_rows, int64_t M, int E, int K, size_t part) {
-  Mx4Ws w;
+ProductWs product_ws(const Format& f, int64_t a_rows, int64_t M, int E, int K, size_t part) {
+  ProductWs w;
   size_t off = kHeader;
   auto take = [&](size_t bytes) {
     const size_t o = off;
     off += align_up(bytes);
     return o;
   };
-  w.codes = take(ss::mx4_code_bytes(a_rows, K));
-  w.scales = take(ss::mx4_scale_bytes(a_rows, K));
-  w.map = take(E ? ss::mx4_map_bytes((int)M, E) : 0);
+  w.codes = take(f.code_bytes(a_rows, K));
+  w.scales = take(f.scale_bytes(a_rows, K));
+  w.map = take(E ? ss::row_map_bytes((int)M, E) : 0);
   w.part = take(part);
   w.total = off;
   return w;
@@ -380,10 +422,16 @@ int check_groups(const swiftspec_moe_groups* g) {
   return SWIFTSPEC_OK;
 }
 
-int run_route(ss::RouteLaunch& L, const swiftspec_moe_groups* g, void* ws, size_t ws_bytes, hipStream_t st) {
+int check_route_ws(const swiftspec_moe_groups* g, void* ws, size_t ws_bytes) {
   if (!ws) return SWIFTSPEC_INVALID_ARG;
   if (!aligned8(ws)) return SWIFTSPEC_MISALIGNED;  // the counts are read eight bytes at a time
   if (ws_bytes < kHeader + align_up(ss::route_hist_bytes(g->T, g->E, g->k))) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  return SWIFTSPEC_OK;
+}
+
+int run_route(ss::RouteLaunch& L, const swiftspec_moe_groups* g, void* ws, size_t ws_bytes, hipStream_t st) {
+  int rc = check_route_ws(g, ws, ws_bytes);
+  if (rc) return rc;
   L.T = g->T;
   L.E = g->E;
   L.k = g->k;
@@ -392,6 +440,159 @@ int run_route(ss::RouteLaunch& L, const swiftspec_moe_groups* g, void* ws, size_
   L.pos = g->pos;
   L.hist = reinterpret_cast<uint16_t*>(static_cast<char*>(ws) + kHeader);
   ss::launch_moe_route(L, st);
+  return check_launch();
+}
+
+int check_scoring(const swiftspec_moe_scoring* s, int E) {
+  if (!s || (s->score != SWIFTSPEC_SCORE_SOFTMAX && s->score != SWIFTSPEC_SCORE_SIGMOID)) return SWIFTSPEC_INVALID_ARG;
+  if (s->groups < 1 || E % s->groups || s->top_groups < 1 || s->top_groups > s->groups) return SWIFTSPEC_INVALID_ARG;
+  if (s->group_best != 1 && s->group_best != 2) return SWIFTSPEC_INVALID_ARG;
+  return aligned4(s->bias) ? SWIFTSPEC_OK : SWIFTSPEC_MISALIGNED;
+}
+
+// ---- products with either kind of matrix
+size_t gemm_bytes(const Format& f, int32_t M, int32_t K, int32_t N) {
+  if (M < 1 || K < 1 || N < 1 || !f.matrices_fit(K, N, 1) || !f.rows_fit(M, K)) return kHeader;
+  return product_ws(f, M, M, 0, K, f.part_bytes_most(M, K, N)).total;
+}
+
+template <typename W>
+int run_product(const Format& f, const W* w, const uint16_t* x, int32_t M, int32_t ldx, uint16_t* y, int32_t ldy,
+                const uint16_t* residual, int32_t ldr, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_matrix(f, w);
+  if (rc) return rc;
+  if ((M && (!x || !y || !ws)) || w->E != 1) return SWIFTSPEC_INVALID_ARG;
+  if (M < 0 || ldx < w->K || ldy < w->N || (residual && ldr < w->N)) return SWIFTSPEC_INVALID_ARG;
+  if (!f.rows_fit(M, w->K) || !f.grid_fits(M, 1, w->K, w->N, false, false)) return SWIFTSPEC_UNSUPPORTED;
+  if (!aligned16(x) || ldx % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
+  if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
+  if (M == 0) return SWIFTSPEC_OK;
+  if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
+  const ProductWs room = product_ws(f, M, M, 0, w->K, f.part_bytes(M, w->K, w->N));
+  if (ws_bytes < room.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  hipStream_t st = S(stream);
+  ss::ProductLaunch L = {};
+  L.epi = ss::OUT_PLAIN;
+  L.w0 = w->packed;
+  L.K = w->K;
+  L.N = w->N;
+  L.E = 1;
+  L.x = x;
+  L.ldx = ldx;
+  L.a = base + room.codes;
+  L.a_scales = base + room.scales;
+  L.a_rows = L.M = M;
+  L.x_written = M <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, w->K, M, y, ldy, w->N, M);  // more rows are quantised first anyway
+  L.div = 1;
+  L.y = y;
+  L.ldy = ldy;
+  L.res = residual;
+  L.ldr = ldr;
+  L.part = reinterpret_cast<float*>(base + room.part);
+  L.ws = ws;
+  if (!f.launch(L, st)) return SWIFTSPEC_UNSUPPORTED;
+  return check_launch();
+}
+
+size_t swiglu_bytes(const Format& f, int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
+  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1 || !groups_fit(T, k, E) || !f.matrices_fit(K, N, E)) return kHeader;
+  if (!f.rows_fit(T, K)) return kHeader;
+  return product_ws(f, T, (int64_t)T * k, E, K, 0).total;
+}
+
+template <typename W>
+int run_swiglu(const Format& f, const W* Wg, const W* Wu, const uint16_t* x, int32_t ldx, const swiftspec_moe_groups* groups,
+               uint16_t* h, int32_t ldh, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_matrix(f, Wg);
+  if (rc) return rc;
+  if ((rc = check_matrix(f, Wu))) return rc;
+  if ((rc = check_groups(groups))) return rc;
+  if (Wg->K != Wu->K || Wg->N != Wu->N || Wg->E != Wu->E || Wg->E != groups->E) return SWIFTSPEC_INVALID_ARG;
+  if ((groups->T && (!x || !h || !ws)) || ldx < Wg->K || ldh < Wg->N) return SWIFTSPEC_INVALID_ARG;
+  const int64_t pairs = (int64_t)groups->T * groups->k;
+  if (!f.rows_fit(groups->T, Wg->K) || !f.grid_fits((int)pairs, Wg->E, Wg->K, Wg->N, true, true)) return SWIFTSPEC_UNSUPPORTED;
+  if (!aligned16(x) || ldx % 8 || !aligned8(h) || ldh % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
+  if (groups->T == 0) return SWIFTSPEC_OK;
+  const ProductWs w = product_ws(f, groups->T, pairs, Wg->E, Wg->K, 0);
+  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  hipStream_t st = S(stream);
+  ss::ProductLaunch L = {};
+  L.epi = ss::OUT_SWIGLU;
+  L.w0 = Wg->packed;
+  L.w1 = Wu->packed;
+  L.K = Wg->K;
+  L.N = Wg->N;
+  L.E = Wg->E;
+  L.x = x;
+  L.ldx = ldx;
+  L.a = base + w.codes;
+  L.a_scales = base + w.scales;
+  L.a_rows = groups->T;
+  L.x_written = pairs <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, Wg->K, groups->T, h, ldh, Wg->N, (int)pairs);
+  L.M = (int)pairs;
+  L.offsets = groups->offsets;
+  L.rows = groups->rows;
+  L.div = groups->k;
+  L.map = reinterpret_cast<int32_t*>(base + w.map);
+  L.y = h;
+  L.ldy = ldh;
+  L.ws = ws;
+  if (!f.launch(L, st)) return SWIFTSPEC_UNSUPPORTED;
+  return check_launch();
+}
+
+size_t down_bytes(const Format& f, int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
+  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1 || !groups_fit(T, k, E) || !f.matrices_fit(K, N, E)) return kHeader;
+  const int64_t pairs = (int64_t)T * k;
+  if (!f.rows_fit(pairs, K)) return kHeader;
+  return product_ws(f, pairs, pairs, E, K, f.rows_bytes_most(pairs, K, N)).total;
+}
+
+template <typename W>
+int run_down(const Format& f, const W* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
+             const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr, void* ws,
+             size_t ws_bytes, void* stream) {
+  int rc = check_matrix(f, Wd);
+  if (rc) return rc;
+  if ((rc = check_groups(groups))) return rc;
+  if (Wd->E != groups->E) return SWIFTSPEC_INVALID_ARG;
+  if (groups->T && (!h || !d_weights || !y || !ws)) return SWIFTSPEC_INVALID_ARG;
+  if (ldh < Wd->K || ldy < Wd->N || (residual && ldr < Wd->N)) return SWIFTSPEC_INVALID_ARG;
+  const int64_t pairs = (int64_t)groups->T * groups->k;
+  if (!f.rows_fit(pairs, Wd->K) || !f.grid_fits((int)pairs, Wd->E, Wd->K, Wd->N, false, true)) return SWIFTSPEC_UNSUPPORTED;
+  if ((int64_t)groups->T * Wd->N >= (int64_t)1 << 33) return SWIFTSPEC_UNSUPPORTED;  // four results a thread of the last launch
+  if (!aligned16(h) || ldh % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws) || !aligned4(d_weights)) return SWIFTSPEC_MISALIGNED;
+  if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
+  if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
+  if (groups->T == 0) return SWIFTSPEC_OK;
+  const ProductWs w = product_ws(f, pairs, pairs, Wd->E, Wd->K, f.rows_bytes((int)pairs, Wd->E, Wd->K, Wd->N));
+  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  float* part = reinterpret_cast<float*>(base + w.part);
+  hipStream_t st = S(stream);
+  ss::ProductLaunch L = {};
+  L.epi = ss::OUT_ROWS;
+  L.w0 = Wd->packed;
+  L.K = Wd->K;
+  L.N = Wd->N;
+  L.E = Wd->E;
+  L.x = h;
+  L.ldx = ldh;
+  L.a = base + w.codes;
+  L.a_scales = base + w.scales;
+  L.a_rows = pairs;
+  L.M = (int)pairs;
+  L.offsets = groups->offsets;
+  L.div = 1;
+  L.map = reinterpret_cast<int32_t*>(base + w.map);
+  L.part = part;
+  L.ws = ws;
+  const int split = f.launch(L, st);
+  if (!split) return SWIFTSPEC_UNSUPPORTED;
+  ss::launch_moe_combine(part, split, groups->T, groups->k, Wd->N, groups->pos, L.map, d_weights, y, ldy,
+                         residual, ldr, ws, st);
   return check_launch();
 }
 
@@ -579,32 +780,21 @@ int swiftspec_rmsnorm_w4a16_swiglu(const swiftspec_w4* Wg, const swiftspec_w4* W
 // ---- microscaled 4-bit matrices and mixtures of experts
 
 size_t swiftspec_mx4_packed_bytes(int32_t K, int32_t N, int32_t E) {
-  if (K <= 0 || N <= 0 || E <= 0 || !mx4_matrices_fit(K, N, E)) return 0;
+  if (K <= 0 || N <= 0 || E <= 0 || !kMx4.matrices_fit(K, N, E)) return 0;
   return ss::mx4_packed_bytes(K, N, E);
 }
 
 int swiftspec_mx4_prepack(const swiftspec_mx4* W, void* packed, size_t packed_bytes, void* stream) {
-  int rc = check_mx4_shape(W);
+  int rc = check_prepack(kMx4, W, packed, packed_bytes);
   if (rc) return rc;
-  if (!W->codes || !W->scales || !packed) return SWIFTSPEC_INVALID_ARG;
-  if (!aligned16(W->codes) || !aligned16(packed)) return SWIFTSPEC_MISALIGNED;
-  if (packed_bytes < ss::mx4_packed_bytes(W->K, W->N, W->E)) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
   ss::launch_mx4_prepack(W->codes, W->scales, W->K, (int64_t)W->E * W->N, packed, S(stream));
   return check_launch();
-}
-
-// rows of K columns: below 2^35 values, 16 of which a thread takes: a launch has
-// fewer than 2^32 threads
-static int check_mx4_rows(int64_t M, int32_t K, int64_t ld) {
-  if (M < 0 || K <= 0 || ld < K) return SWIFTSPEC_INVALID_ARG;
-  if (K % 32 || M > (((int64_t)1 << 35) - 1) / K) return SWIFTSPEC_UNSUPPORTED;
-  return SWIFTSPEC_OK;
 }
 
 int swiftspec_mx4_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx, uint8_t* codes, uint8_t* scales,
                            void* stream) {
   if (M && (!x || !codes || !scales)) return SWIFTSPEC_INVALID_ARG;
-  int rc = check_mx4_rows(M, K, ldx);
+  int rc = check_quantized_rows(M, K, ldx, 32, 32);
   if (rc) return rc;
   if (!aligned16(x) || ldx % 8 || !aligned4(codes)) return SWIFTSPEC_MISALIGNED;
   if (M == 0) return SWIFTSPEC_OK;
@@ -615,7 +805,7 @@ int swiftspec_mx4_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx,
 int swiftspec_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t M, int32_t K, uint16_t* y,
                              int64_t ldy, void* stream) {
   if (M && (!codes || !scales || !y)) return SWIFTSPEC_INVALID_ARG;
-  int rc = check_mx4_rows(M, K, ldy);
+  int rc = check_quantized_rows(M, K, ldy, 32, 32);
   if (rc) return rc;
   if (!aligned16(y) || ldy % 8 || !aligned4(codes)) return SWIFTSPEC_MISALIGNED;
   if (M == 0) return SWIFTSPEC_OK;
@@ -623,47 +813,55 @@ int swiftspec_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_
   return check_launch();
 }
 
-size_t swiftspec_mx4_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N) {
-  if (M < 1 || K < 1 || N < 1 || !mx4_matrices_fit(K, N, 1) || !mx4_rows_fit(M, K)) return kHeader;
-  return mx4_ws(M, M, 0, K, ss::mx4_part_bytes_most(M, K, N)).total;
-}
+size_t swiftspec_mx4_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N) { return gemm_bytes(kMx4, M, K, N); }
 
 int swiftspec_mx4_gemm(const swiftspec_mx4* W, const uint16_t* x, int32_t M, int32_t ldx, uint16_t* y, int32_t ldy,
                        const uint16_t* residual, int32_t ldr, void* ws, size_t ws_bytes, void* stream) {
-  int rc = check_mx4(W);
+  return run_product(kMx4, W, x, M, ldx, y, ldy, residual, ldr, ws, ws_bytes, stream);
+}
+
+// ---- block-scaled 8-bit matrices
+
+size_t swiftspec_fp8_packed_bytes(int32_t K, int32_t N, int32_t E) {
+  if (K <= 0 || N <= 0 || E <= 0 || !kFp8.matrices_fit(K, N, E)) return 0;
+  return ss::fp8_packed_bytes(K, N, E);
+}
+
+int swiftspec_fp8_prepack(const swiftspec_fp8* W, void* packed, size_t packed_bytes, void* stream) {
+  int rc = check_prepack(kFp8, W, packed, packed_bytes);
   if (rc) return rc;
-  if ((M && (!x || !y || !ws)) || W->E != 1) return SWIFTSPEC_INVALID_ARG;
-  if (M < 0 || ldx < W->K || ldy < W->N || (residual && ldr < W->N)) return SWIFTSPEC_INVALID_ARG;
-  if (!mx4_rows_fit(M, W->K) || !ss::mx4_grid_fits(M, 1, W->K, W->N, false, false)) return SWIFTSPEC_UNSUPPORTED;
-  if (!aligned16(x) || ldx % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
-  if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
-  if (M == 0) return SWIFTSPEC_OK;
-  if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
-  const Mx4Ws w = mx4_ws(M, M, 0, W->K, ss::mx4_part_bytes(M, W->K, W->N));
-  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
-  uint8_t* base = static_cast<uint8_t*>(ws);
-  hipStream_t st = S(stream);
-  ss::Mx4Launch L = {};
-  L.epi = ss::MX4_PLAIN;
-  L.w0 = W->packed;
-  L.K = W->K;
-  L.N = W->N;
-  L.E = 1;
-  L.x = x;
-  L.ldx = ldx;
-  L.a = base + w.codes;
-  L.a_scales = base + w.scales;
-  L.a_rows = L.M = M;
-  L.x_written = M <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, W->K, M, y, ldy, W->N, M);  // more rows are quantised first anyway
-  L.div = 1;
-  L.y = y;
-  L.ldy = ldy;
-  L.res = residual;
-  L.ldr = ldr;
-  L.part = reinterpret_cast<float*>(base + w.part);
-  L.ws = ws;
-  if (!ss::launch_mx4_gemm(L, st)) return SWIFTSPEC_UNSUPPORTED;
+  if (!aligned4(W->scales)) return SWIFTSPEC_MISALIGNED;
+  ss::launch_fp8_prepack(W->codes, W->scales, W->K, W->N, W->E, packed, S(stream));
   return check_launch();
+}
+
+int swiftspec_fp8_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx, int32_t block_rows, uint8_t* codes,
+                           float* scales, void* stream) {
+  if ((M && (!x || !codes || !scales)) || (block_rows != 1 && block_rows != 128)) return SWIFTSPEC_INVALID_ARG;
+  int rc = check_quantized_rows(M, K, ldx, 16, 128);
+  if (rc) return rc;
+  if (!aligned16(x) || ldx % 8 || !aligned8(codes) || !aligned4(scales)) return SWIFTSPEC_MISALIGNED;
+  if (M == 0) return SWIFTSPEC_OK;
+  ss::launch_fp8_quantize(x, M, K, ldx, block_rows, codes, scales, S(stream));
+  return check_launch();
+}
+
+int swiftspec_fp8_dequantize(const uint8_t* codes, const float* scales, int64_t M, int32_t K, int32_t block_rows,
+                             uint16_t* y, int64_t ldy, void* stream) {
+  if ((M && (!codes || !scales || !y)) || (block_rows != 1 && block_rows != 128)) return SWIFTSPEC_INVALID_ARG;
+  int rc = check_quantized_rows(M, K, ldy, 16, 128);
+  if (rc) return rc;
+  if (!aligned16(y) || ldy % 8 || !aligned8(codes) || !aligned4(scales)) return SWIFTSPEC_MISALIGNED;
+  if (M == 0) return SWIFTSPEC_OK;
+  ss::launch_fp8_dequantize(codes, scales, M, K, block_rows, y, ldy, S(stream));
+  return check_launch();
+}
+
+size_t swiftspec_fp8_gemm_workspace_bytes(int32_t M, int32_t K, int32_t N) { return gemm_bytes(kFp8, M, K, N); }
+
+int swiftspec_fp8_gemm(const swiftspec_fp8* W, const uint16_t* x, int32_t M, int32_t ldx, uint16_t* y, int32_t ldy,
+                       const uint16_t* residual, int32_t ldr, void* ws, size_t ws_bytes, void* stream) {
+  return run_product(kFp8, W, x, M, ldx, y, ldy, residual, ldr, ws, ws_bytes, stream);
 }
 
 size_t swiftspec_moe_route_workspace_bytes(int32_t T, int32_t E, int32_t k) {
@@ -687,6 +885,41 @@ int swiftspec_moe_route(const uint16_t* logits, int32_t ldl, int32_t renormalize
   return run_route(L, groups, ws, ws_bytes, S(stream));
 }
 
+int swiftspec_moe_route_scored(const void* logits, int32_t logit_bits, int32_t ldl, const swiftspec_moe_scoring* scoring,
+                               int32_t* d_experts, float* d_weights, const swiftspec_moe_groups* groups, void* ws,
+                               size_t ws_bytes, void* stream) {
+  int rc = check_groups(groups);
+  if (rc) return rc;
+  if ((rc = check_scoring(scoring, groups->E))) return rc;
+  if ((groups->T && (!logits || !d_experts || !d_weights)) || ldl < groups->E) return SWIFTSPEC_INVALID_ARG;
+  if (logit_bits != 16 && logit_bits != 32) return SWIFTSPEC_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(logits) & (logit_bits / 8 - 1)) return SWIFTSPEC_MISALIGNED;
+  if (!aligned4(d_experts) || !aligned4(d_weights)) return SWIFTSPEC_MISALIGNED;
+  if ((rc = check_route_ws(groups, ws, ws_bytes))) return rc;
+  ss::ScoredLaunch L = {};
+  L.group.T = groups->T;
+  L.group.E = groups->E;
+  L.group.k = groups->k;
+  L.group.experts = d_experts;
+  L.group.weights = d_weights;
+  L.group.offsets = groups->offsets;
+  L.group.rows = groups->rows;
+  L.group.pos = groups->pos;
+  L.group.hist = reinterpret_cast<uint16_t*>(static_cast<char*>(ws) + kHeader);
+  L.logits = logits;
+  L.ldl = ldl;
+  L.wide = logit_bits == 32;
+  L.sigmoid = scoring->score == SWIFTSPEC_SCORE_SIGMOID;
+  L.renormalize = scoring->renormalize != 0;
+  L.bias = scoring->bias;
+  L.groups = scoring->groups;
+  L.top_groups = scoring->top_groups;
+  L.best = scoring->group_best;
+  L.scale = scoring->scale;
+  ss::launch_moe_route_scored(L, S(stream));
+  return check_launch();
+}
+
 int swiftspec_moe_group(const int32_t* d_experts, const swiftspec_moe_groups* groups, void* ws, size_t ws_bytes,
                         void* stream) {
   int rc = check_groups(groups);
@@ -699,103 +932,43 @@ int swiftspec_moe_group(const int32_t* d_experts, const swiftspec_moe_groups* gr
 }
 
 size_t swiftspec_moe_mx4_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
-  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1 || !groups_fit(T, k, E) || !mx4_matrices_fit(K, N, E)) return kHeader;
-  if (!mx4_rows_fit(T, K)) return kHeader;
-  return mx4_ws(T, (int64_t)T * k, E, K, 0).total;
+  return swiglu_bytes(kMx4, T, k, E, K, N);
 }
 
 int swiftspec_moe_mx4_swiglu(const swiftspec_mx4* Wg, const swiftspec_mx4* Wu, const uint16_t* x, int32_t ldx,
                              const swiftspec_moe_groups* groups, uint16_t* h, int32_t ldh, void* ws, size_t ws_bytes,
                              void* stream) {
-  int rc = check_mx4(Wg);
-  if (rc) return rc;
-  if ((rc = check_mx4(Wu))) return rc;
-  if ((rc = check_groups(groups))) return rc;
-  if (Wg->K != Wu->K || Wg->N != Wu->N || Wg->E != Wu->E || Wg->E != groups->E) return SWIFTSPEC_INVALID_ARG;
-  if ((groups->T && (!x || !h || !ws)) || ldx < Wg->K || ldh < Wg->N) return SWIFTSPEC_INVALID_ARG;
-  const int64_t pairs = (int64_t)groups->T * groups->k;
-  if (!mx4_rows_fit(groups->T, Wg->K) || !ss::mx4_grid_fits((int)pairs, Wg->E, Wg->K, Wg->N, true, true)) return SWIFTSPEC_UNSUPPORTED;
-  if (!aligned16(x) || ldx % 8 || !aligned8(h) || ldh % 4 || !aligned16(ws)) return SWIFTSPEC_MISALIGNED;
-  if (groups->T == 0) return SWIFTSPEC_OK;
-  const Mx4Ws w = mx4_ws(groups->T, pairs, Wg->E, Wg->K, 0);
-  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
-  uint8_t* base = static_cast<uint8_t*>(ws);
-  hipStream_t st = S(stream);
-  ss::Mx4Launch L = {};
-  L.epi = ss::MX4_SWIGLU;
-  L.w0 = Wg->packed;
-  L.w1 = Wu->packed;
-  L.K = Wg->K;
-  L.N = Wg->N;
-  L.E = Wg->E;
-  L.x = x;
-  L.ldx = ldx;
-  L.a = base + w.codes;
-  L.a_scales = base + w.scales;
-  L.a_rows = groups->T;
-  L.x_written = pairs <= SWIFTSPEC_MAX_M && rows_overlap(x, ldx, Wg->K, groups->T, h, ldh, Wg->N, (int)pairs);
-  L.M = (int)pairs;
-  L.offsets = groups->offsets;
-  L.rows = groups->rows;
-  L.div = groups->k;
-  L.map = reinterpret_cast<int32_t*>(base + w.map);
-  L.y = h;
-  L.ldy = ldh;
-  L.ws = ws;
-  if (!ss::launch_mx4_gemm(L, st)) return SWIFTSPEC_UNSUPPORTED;
-  return check_launch();
+  return run_swiglu(kMx4, Wg, Wu, x, ldx, groups, h, ldh, ws, ws_bytes, stream);
 }
 
 size_t swiftspec_moe_mx4_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
-  if (T < 1 || k < 1 || E < 1 || K < 1 || N < 1 || !groups_fit(T, k, E) || !mx4_matrices_fit(K, N, E)) return kHeader;
-  const int64_t pairs = (int64_t)T * k;
-  if (!mx4_rows_fit(pairs, K)) return kHeader;
-  return mx4_ws(pairs, pairs, E, K, ss::mx4_rows_bytes_most(pairs, K, N)).total;
+  return down_bytes(kMx4, T, k, E, K, N);
 }
 
 int swiftspec_moe_mx4_down(const swiftspec_mx4* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
                            const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr,
                            void* ws, size_t ws_bytes, void* stream) {
-  int rc = check_mx4(Wd);
-  if (rc) return rc;
-  if ((rc = check_groups(groups))) return rc;
-  if (Wd->E != groups->E) return SWIFTSPEC_INVALID_ARG;
-  if (groups->T && (!h || !d_weights || !y || !ws)) return SWIFTSPEC_INVALID_ARG;
-  if (ldh < Wd->K || ldy < Wd->N || (residual && ldr < Wd->N)) return SWIFTSPEC_INVALID_ARG;
-  const int64_t pairs = (int64_t)groups->T * groups->k;
-  if (!mx4_rows_fit(pairs, Wd->K) || !ss::mx4_grid_fits((int)pairs, Wd->E, Wd->K, Wd->N, false, true)) return SWIFTSPEC_UNSUPPORTED;
-  if ((int64_t)groups->T * Wd->N >= (int64_t)1 << 33) return SWIFTSPEC_UNSUPPORTED;  // four results a thread of the last launch
-  if (!aligned16(h) || ldh % 8 || !aligned8(y) || ldy % 4 || !aligned16(ws) || !aligned4(d_weights)) return SWIFTSPEC_MISALIGNED;
-  if (residual && (!aligned8(residual) || ldr % 4)) return SWIFTSPEC_MISALIGNED;
-  if (residual == y && ldr != ldy) return SWIFTSPEC_INVALID_ARG;
-  if (groups->T == 0) return SWIFTSPEC_OK;
-  const Mx4Ws w = mx4_ws(pairs, pairs, Wd->E, Wd->K, ss::mx4_rows_bytes((int)pairs, Wd->E, Wd->K, Wd->N));
-  if (ws_bytes < w.total) return SWIFTSPEC_WORKSPACE_TOO_SMALL;
-  uint8_t* base = static_cast<uint8_t*>(ws);
-  float* part = reinterpret_cast<float*>(base + w.part);
-  hipStream_t st = S(stream);
-  ss::Mx4Launch L = {};
-  L.epi = ss::MX4_ROWS;
-  L.w0 = Wd->packed;
-  L.K = Wd->K;
-  L.N = Wd->N;
-  L.E = Wd->E;
-  L.x = h;
-  L.ldx = ldh;
-  L.a = base + w.codes;
-  L.a_scales = base + w.scales;
-  L.a_rows = pairs;
-  L.M = (int)pairs;
-  L.offsets = groups->offsets;
-  L.div = 1;
-  L.map = reinterpret_cast<int32_t*>(base + w.map);
-  L.part = part;
-  L.ws = ws;
-  const int split = ss::launch_mx4_gemm(L, st);
-  if (!split) return SWIFTSPEC_UNSUPPORTED;
-  ss::launch_moe_combine(part, split, groups->T, groups->k, Wd->N, groups->pos, L.map, d_weights, y, ldy,
-                         residual, ldr, ws, st);
-  return check_launch();
+  return run_down(kMx4, Wd, h, ldh, groups, d_weights, y, ldy, residual, ldr, ws, ws_bytes, stream);
+}
+
+size_t swiftspec_moe_fp8_swiglu_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
+  return swiglu_bytes(kFp8, T, k, E, K, N);
+}
+
+int swiftspec_moe_fp8_swiglu(const swiftspec_fp8* Wg, const swiftspec_fp8* Wu, const uint16_t* x, int32_t ldx,
+                             const swiftspec_moe_groups* groups, uint16_t* h, int32_t ldh, void* ws, size_t ws_bytes,
+                             void* stream) {
+  return run_swiglu(kFp8, Wg, Wu, x, ldx, groups, h, ldh, ws, ws_bytes, stream);
+}
+
+size_t swiftspec_moe_fp8_down_workspace_bytes(int32_t T, int32_t k, int32_t E, int32_t K, int32_t N) {
+  return down_bytes(kFp8, T, k, E, K, N);
+}
+
+int swiftspec_moe_fp8_down(const swiftspec_fp8* Wd, const uint16_t* h, int32_t ldh, const swiftspec_moe_groups* groups,
+                           const float* d_weights, uint16_t* y, int32_t ldy, const uint16_t* residual, int32_t ldr,
+                           void* ws, size_t ws_bytes, void* stream) {
+  return run_down(kFp8, Wd, h, ldh, groups, d_weights, y, ldy, residual, ldr, ws, ws_bytes, stream);
 }
 
 size_t swiftspec_prepared_bytes(int32_t M, int32_t K) {
