@@ -26,7 +26,10 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall",
 # accumulators in ordinary vector registers (the default accumulation-register
 # form makes the compiler copy the output tiles between the two register
 # files around every key tile)
-EXTRA = {"tree_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]}
+# (in fp8_gemm the results of the matrix instructions go into multiply-adds, which
+# read ordinary registers only)
+EXTRA = {"tree_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
+         "fp8_gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str, verbose: bool) -> str:

@@ -190,6 +190,261 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
   write_out<EPI>(a, m, n, v);
 }
 
+// ----------------------------------------------------------- many rows
+// WM x WN waves own a tile of 16 WM MTW rows and 16 WN NTW columns, each wave MTW x NTW
+// blocks of 16.  Both operands pass through LDS, loaded there directly, a group of 128 k
+// at a time in a ring of ST stages.  The 16-byte pieces of a row stand in LDS at piece ^
+// (row / 2 % 8), so that a column of 16 rows covers the 64 banks once.
+// A step multiplies one group: the weights' blocks of the wave stay in registers, the
+// rows' blocks follow one another, the next on its way from LDS.  Each instruction's
+// result is multiplied and added two instructions later, so that its latency does not
+// show.  Before the last block of rows the wave has read all it needs of this stage: it
+// waits for its loads of the next one and for the other waves, and reads the first
+// operands of the next step while the last block is multiplied; the stage's place is
+// loaded anew during the next step.  One barrier a step.
+// A wave's columns lie in one block of 128, so that the matrix's scale is uniform: 64
+// groups of them are one load, a lane each.
+constexpr int kTurnPad = 16;  // bytes behind a row of results on its way through LDS
+
+template <int WM, int WN, int MTW, int NTW, int ST, Epilogue EPI>
+__global__ __launch_bounds__(64 * WM * WN) void fp8_tile_kernel(Fp8Args a) {
+  constexpr bool SW = EPI == OUT_SWIGLU;
+  constexpr int kWv = WM * WN;
+  constexpr int AT = WM * MTW, WT = WN * NTW, TM = 16 * AT, kMine = TM / kWv;
+  constexpr int kA = kMine / 8, kW = 2 * WT / kWv, kLoads = kA + kW;  // loads of a wave for a stage
+  constexpr int kC = SW ? WT / 2 : WT;     // output column tiles of the workgroup
+  constexpr int kCW = SW ? NTW / 2 : NTW;  // and of a wave
+  static_assert(kA % 2 == 0 && kMine <= kWave && (ST == 2 || ST == 4) && MTW % 2 == 0 && MTW >= 4, "the pipeline's counts");
+  static_assert(8 % kCW == 0 && (MTW * NTW) % 4 == 0 && kLoads <= (MTW - 1) * NTW, "a wave's columns lie in one block; results go round in fours");
+  struct Operands {
+    u32x4 ax[ST][TM * 8];
+    u32x4 wx[ST][WT][128];
+  };
+  __shared__ Operands room;
+  __shared__ uint32_t sc[2][kWv][kWave];  // the rows' scale words of four groups, twice
+  __shared__ uint32_t row_list[kWv][kWave];
+  __shared__ uint8_t live[TM];  // rows that are written
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave - wm * WN;
+  const int r16 = lane & 15, kq = lane >> 4;
+  int rb, cb;
+  place_of(a, rb, cb);
+  const RowBlock b = row_block(a, rb, TM);
+  if (b.n <= 0) return;
+  const int t0 = cb * kC;
+  // this workgroup's share of K: whole scale words
+  const int first = blockIdx.y * a.G4 / a.split, G4 = (blockIdx.y + 1) * a.G4 / a.split - first;
+  const int G = min(a.G - 4 * first, 4 * G4);
+  const uint32_t wb = (uint32_t)a.w_stride;
+  const i32x4 rw0 = raw_rsrc(a.w0 + b.e * a.w_stride, wb);
+  const i32x4 rw1 = raw_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
+  const i32x4 ra = raw_rsrc(a.a, a.a_bytes), ras = raw_rsrc(a.as, a.as_bytes);
+  // load l of the weights: half l % 2 of tile l / 2 of the workgroup, which is a tile of
+  // wave column l / 2 / NTW, for SwiGLU a gate tile and its up tile in turn
+  uint32_t wt[kW];
+#pragma unroll
+  for (int i = 0; i < kW; ++i) {
+    const int w = (wave * kW + i) >> 1, own = w / NTW, j = w - own * NTW;
+    wt[i] = (uint32_t)min(t0 + own * kCW + (SW ? j / 2 : j), a.Nt - 1);
+  }
+  const uint32_t ax_lds = lds_address(&room.ax[0][0]), wx_lds = lds_address(&room.wx[0][0][0]), sc_lds = lds_address(&sc[0][0][0]);
+  uint32_t va[kA], vs;
+  // loads 0 .. kLoads - 1 of group g (weights first) into stage s; past the last group
+  // the last one again (without a condition, which would cut the step into blocks that
+  // the compiler moves instructions between)
+  auto load = [&](int i, int g, int s) {
+    const uint32_t at = (uint32_t)(min(g, G - 1) + 4 * first);
+    if (i < kW) {
+      const int l = wave * kW + i;
+      buffer_load_lds16(SW && ((l >> 1) & 1) ? rw1 : rw0, (uint32_t)lane * 16u, (wt[i] * a.G + at) * 2048u + (uint32_t)(l & 1) * 1024u,
+                        wx_lds + (uint32_t)s * (WT * 2048u) + (uint32_t)l * 1024u);
+    } else {
+      buffer_load_lds16(ra, va[i - kW], at * 128u, ax_lds + (uint32_t)s * (TM * 128u) + (uint32_t)(wave * kA + i - kW) * 1024u);
+    }
+  };
+  auto load_scales = [&](int c) {
+    buffer_load_lds4(ras, vs, (uint32_t)(min(c, G4 - 1) + first) * 4u, sc_lds + (uint32_t)((c & 1) * kWv + wave) * 256u);
+  };
+  // First what needs no list of rows, behind the list itself (through LDS: the
+  // wait for it then leaves the weights on their way).
+  const int mine = wave * kMine + lane;
+  if (a.rows)
+    buffer_load_lds4(raw_rsrc(a.rows, (uint32_t)a.M * 4u), lane < kMine && mine < b.n ? (uint32_t)(b.m0 + mine) * 4u : kOutside, 0u,
+                     lds_address(&row_list[wave][0]));
+#pragma unroll
+  for (int i = 0; i < kW; ++i) load(i, 0, 0);
+  if (a.rows) {
+    vm_wait<kW>();
+    asm volatile("" ::: "memory");
+  }
+  // lane m: the activation row of row m of this wave's share; -1: none, or the
+  // caller's list is wrong
+  int src = lane < kMine && mine < b.n ? b.m0 + mine : -1;
+  if (a.rows && src >= 0) {
+    const uint32_t r = row_list[wave][lane];
+    src = r < (uint32_t)a.M ? (int)(r / (uint32_t)a.div) : -1;
+    if (src < 0) report_error(a.ws, SWIFTSPEC_DEVERR_BAD_GROUPS);
+  }
+  if (lane < kMine) live[mine] = src >= 0;
+#pragma unroll
+  for (int i = 0; i < kA; ++i) {
+    const int from = __shfl(src, 8 * i + (lane >> 3), kWave);
+    va[i] = from >= 0 ? (uint32_t)from * (uint32_t)(a.G * 128) + (uint32_t)((lane & 7) ^ (4 * (i & 1) + (lane >> 4))) * 16u : kOutside;
+  }
+  vs = src >= 0 ? (uint32_t)src * (uint32_t)(a.G4 * 4) : kOutside;
+  load_scales(0);
+#pragma unroll
+  for (int i = kW; i < kLoads; ++i) load(i, 0, 0);
+#pragma unroll
+  for (int s = 1; s < ST - 1; ++s)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(i, s, s);
+  // the scales of this wave's columns: lane l those of group l of 64
+  const int64_t sblock = (int64_t)b.e * (a.s_stride / 4) + (int64_t)(min(t0 + wn * kCW, a.Nt - 1) >> 3) * a.G + 4 * first;
+  float sv0 = 0.f, sv1 = 0.f;
+  auto load_weight_scales = [&](int g) {
+    sv0 = g + lane < G ? a.s0[sblock + g + lane] : 0.f;
+    if constexpr (SW) sv1 = g + lane < G ? a.s1[sblock + g + lane] : 0.f;
+    asm volatile("" : "+v"(sv0), "+v"(sv1));  // waited for here, not in every step
+  };
+  load_weight_scales(0);
+  // operands: the weights' blocks, two blocks of rows in turn and their scale words
+  u32x4 w[NTW][2], x[2][2];
+  uint32_t xs[2];
+  f32x4 acc[MTW][NTW], p[4];
+#pragma unroll
+  for (int i = 0; i < MTW; ++i)
+#pragma unroll
+    for (int j = 0; j < NTW; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) p[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto read_w = [&](int j, int s) {
+    w[j][0] = room.wx[s][wn * NTW + j][lane];
+    w[j][1] = room.wx[s][wn * NTW + j][64 + lane];
+  };
+  const int row0 = 16 * wm * MTW + r16, twist = (r16 >> 1) & 7;
+  auto read_x = [&](int i, int s, int c) {
+    const int row = row0 + 16 * i;
+    x[i & 1][0] = room.ax[s][row * 8 + (kq ^ twist)];
+    x[i & 1][1] = room.ax[s][row * 8 + ((kq + 4) ^ twist)];
+    xs[i & 1] = sc[c & 1][row / kMine][row % kMine];
+  };
+  float before0 = 0.f, before1 = 0.f;  // scales of the group before
+  vm_lds_barrier<(ST - 2) * kLoads>();  // the first group; the rows' scales came before its rows
+#pragma unroll
+  for (int j = 0; j < NTW; ++j) read_w(j, 0);
+  read_x(0, 0, 0);
+  // Group 4 c + J.
+  auto step = [&](auto jc, int c) {
+    constexpr int J = decltype(jc)::value, kS = J % ST, kNext = (J + 1) % ST, kFree = (J + ST - 1) % ST;
+    constexpr int kMfma = MTW * NTW, kLast = kMfma - NTW;
+    const int g = 4 * c + J;
+    const float now0 = bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(sv0), g & 63));
+    const float now1 = SW ? bitcast<float>(__builtin_amdgcn_readlane(bitcast<int>(sv1), g & 63)) : 0.f;
+    if constexpr (J == 0) load_scales(c + 1);
+#pragma unroll
+    for (int q = 0; q < kMfma; ++q) {
+      const int i = q / NTW, j = q % NTW;
+      if (q == kLast)  // all of this stage is in registers; the loads of later groups than the next may be on their way
+        vm_lds_barrier<(ST - 2) * kLoads + (ST == 4 && J <= 1 ? 1 : 0)>();
+      p[q & 3] = mfma_fp8<J>(w[j], x[i & 1], xs[i & 1]);
+      asm volatile("" : "+v"(p[q & 3]));  // the compiler leaves it in its place
+      if (j == 0 && i + 1 < MTW) read_x(i + 1, kS, c);
+      if (q == kLast) read_x(0, kNext, c + (J == 3 ? 1 : 0));
+      if (q >= kLast) read_w(j, kNext);
+      if (q < kLoads) load(q, g + ST - 1, kFree);
+      // the result of two instructions before
+      const int o = (q + kMfma - 2) % kMfma, oi = o / NTW, oj = o % NTW;
+      const bool up = SW && (oj & 1);
+      const float s = q < 2 ? (up ? before1 : before0) : (up ? now1 : now0);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) acc[oi][oj][v] = __builtin_fmaf(s, p[(q + 2) & 3][v], acc[oi][oj][v]);
+      asm volatile("" : "+v"(acc[oi][oj]));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    before0 = now0;
+    before1 = now1;
+  };
+  for (int c = 0; c < G4; ++c) {
+    if (c && (c & 15) == 0) load_weight_scales(4 * c);
+    step(std::integral_constant<int, 0>{}, c);
+    if (4 * c + 1 < G) step(std::integral_constant<int, 1>{}, c);
+    if (4 * c + 2 < G) step(std::integral_constant<int, 2>{}, c);
+    if (4 * c + 3 < G) step(std::integral_constant<int, 3>{}, c);
+  }
+  // the last two results
+#pragma unroll
+  for (int o = MTW * NTW - 2; o < MTW * NTW; ++o) {
+    const float s = SW && ((o % NTW) & 1) ? before1 : before0;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) acc[o / NTW][o % NTW][v] = __builtin_fmaf(s, p[o & 3][v], acc[o / NTW][o % NTW][v]);
+  }
+  vm_lds_barrier<0>();  // loads past the last group still write LDS, other waves read theirs
+  // A lane holds columns 4 kq .. 4 kq + 3 of row r16 of each block.  Through LDS the rows
+  // come out in whole: 16 columns of fp16, or of fp32 (results that a residual or another
+  // sum awaits) for each of the wave's tiles.
+  constexpr bool wide = EPI == OUT_ROWS || EPI == OUT_RESIDUAL;
+  constexpr int kBytes = 16 * kCW * (wide ? 4 : 2), kPitch = kBytes + kTurnPad;
+  constexpr int kLanes = kBytes / 16, kRows = kWave / kLanes;  // lanes of a row, rows at a time
+  constexpr int kBatch = kRows > 16 ? kRows / 16 : 1;          // blocks of rows at a time
+  constexpr int kTurns = 16 * kBatch / kRows;
+  static_assert(sizeof(Operands) >= kWv * 16 * kBatch * kPitch && 16 * kBatch % kRows == 0 && MTW % kBatch == 0, "the rows' room");
+  uint8_t* my = reinterpret_cast<uint8_t*>(&room) + wave * (16 * kBatch * kPitch);
+  const int tr = lane / kLanes, tc = lane % kLanes;
+  const int col = 16 * (t0 + wn * kCW) + tc * (wide ? 4 : 8);
+  const bool inside = col < a.N;
+  u32x2 add[EPI == OUT_RESIDUAL ? MTW : 1][kTurns];
+  if constexpr (EPI == OUT_RESIDUAL) {  // all of it at once
+#pragma unroll
+    for (int i = 0; i < MTW; i += kBatch)
+#pragma unroll
+      for (int u = 0; u < kTurns; ++u) {
+        const int r = 16 * (wm * MTW + i) + u * kRows + tr;
+        add[i][u] = u32x2{0u, 0u};
+        if (live[r] && inside) add[i][u] = residual(a, b.m0 + r, col);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < MTW; i += kBatch) {
+#pragma unroll
+    for (int h = 0; h < kBatch; ++h)
+#pragma unroll
+      for (int j = 0; j < kCW; ++j) {
+        f32x4 v = acc[i + h][SW ? 2 * j : j];
+        if constexpr (SW) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = silu(v[e]) * acc[i + h][2 * j + 1][e];
+        }
+        uint8_t* at = my + (16 * h + r16) * kPitch + (16 * j + 4 * kq) * (wide ? 4 : 2);
+        if constexpr (wide) *reinterpret_cast<f32x4*>(at) = v;
+        else *reinterpret_cast<u32x2*>(at) = pack4(v);
+      }
+    __builtin_amdgcn_wave_barrier();
+    u32x4 v[kTurns];
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) v[u] = *reinterpret_cast<const u32x4*>(my + (u * kRows + tr) * kPitch + 16 * tc);
+#pragma unroll
+    for (int u = 0; u < kTurns; ++u) {
+      const int r = 16 * (wm * MTW + i) + u * kRows + tr;
+      const int64_t m = b.m0 + r;
+      if (!live[r] || !inside) continue;
+      if constexpr (EPI == OUT_ROWS) {
+        u32x4* to = reinterpret_cast<u32x4*>(a.part + ((int64_t)blockIdx.y * a.M + m) * a.N + col);
+        if (a.past) __builtin_nontemporal_store(v[u], to);
+        else *to = v[u];
+      } else if constexpr (EPI == OUT_RESIDUAL) {
+        f32x4 f = bitcast<f32x4>(v[u]);
+        add_residual(f, add[i][u]);
+        *reinterpret_cast<u32x2*>(a.y + m * a.ldy + col) = pack4(f);
+      } else {
+        store_rows16(a.y + m * a.ldy + col, v[u], SW && a.past);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 template <int W, int MT, int NT, Epilogue EPI>
 void launch_stream(Fp8Args a, int blocks, hipStream_t st) {
   constexpr int kC = EPI == OUT_SWIGLU ? NT / 2 : NT;
@@ -197,13 +452,29 @@ void launch_stream(Fp8Args a, int blocks, hipStream_t st) {
   hipLaunchKernelGGL((fp8_stream_kernel<W, MT, NT, 2, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(64 * W), 0, st, a);
 }
 
+template <int WM, int WN, int MTW, int NTW, int ST, Epilogue EPI>
+void launch_tile(Fp8Args a, int blocks, hipStream_t st) {
+  constexpr int kC = EPI == OUT_SWIGLU ? WN * NTW / 2 : WN * NTW;
+  a.col_blocks = (a.Nt + kC - 1) / kC;
+  hipLaunchKernelGGL((fp8_tile_kernel<WM, WN, MTW, NTW, ST, EPI>), dim3((unsigned)blocks * a.col_blocks, a.split), dim3(64 * WM * WN), 0,
+                     st, a);
+}
+
 // of each Fp8Form
-constexpr int kRowsOf[] = {16};
-constexpr int kColumnsOf[] = {32};
+constexpr int kRowsOf[] = {16, 64, 128, 256};
+constexpr int kColumnsOf[] = {32, 128, 128, 256};
+constexpr int kThreadsOf[] = {512, 256, 256, 512};
 
 }  // namespace
 
-Fp8Plan plan_fp8_gemm(int, int, int, int, bool, bool, bool) { return Fp8Plan{Fp8Form::STREAM_1, kRowsOf[0], 1}; }
+Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
+  auto plan = [](Fp8Form f, int split = 1) { return Fp8Plan{f, kRowsOf[(int)f], split}; };
+  const int64_t avg = grouped ? M / E : M;
+  if (avg < 8) return plan(Fp8Form::STREAM_1);
+  if (avg <= 64) return plan(Fp8Form::TILE_64);
+  if (avg <= 256) return plan(Fp8Form::TILE_128);
+  return plan(Fp8Form::TILE_256);
+}
 
 namespace {
 
@@ -211,6 +482,9 @@ template <Epilogue EPI>
 void launch_form(const Fp8Plan& p, const Fp8Args& a, int blocks, hipStream_t st) {
   switch (p.form) {
     case Fp8Form::STREAM_1: return launch_stream<8, 1, 2, EPI>(a, blocks, st);
+    case Fp8Form::TILE_64: return launch_tile<1, 4, 4, 2, 4, EPI>(a, blocks, st);
+    case Fp8Form::TILE_128: return launch_tile<2, 2, 4, 4, 2, EPI>(a, blocks, st);
+    case Fp8Form::TILE_256: return launch_tile<2, 4, 8, 4, 2, EPI>(a, blocks, st);
   }
 }
 
@@ -259,6 +533,8 @@ int launch_fp8_gemm(const ProductLaunch& L, hipStream_t st) {
   a.x_row = (uint32_t)(L.ldx * 2);
   a.x_bytes = (uint32_t)x_bytes;
   a.split = p.split;
+  // results of more than the L2s hold go past them, so that the weights stay
+  a.past = L.offsets && (int64_t)L.M * L.N * (L.epi == OUT_ROWS ? 4 : 2) > (32 << 20);
   a.pieces = L.K / 16;
   a.offsets = L.offsets;
   a.E = L.E;
@@ -280,7 +556,7 @@ bool fp8_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped) {
     const Fp8Plan p = plan_fp8_gemm(M, E, K, N, swiglu, grouped, raw);
     const int64_t blocks = grouped ? row_blocks(M, E, p.tm) : (M + p.tm - 1) / p.tm;
     const int64_t columns = ((int64_t)N * (swiglu ? 2 : 1) + kColumnsOf[(int)p.form] - 1) / kColumnsOf[(int)p.form];
-    if (blocks * columns * 512 >= 1ll << 32) return false;
+    if (blocks * columns * kThreadsOf[(int)p.form] >= 1ll << 32) return false;
   }
   return true;
 }

@@ -40,7 +40,7 @@ bool fp8_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped);
 size_t fp8_rows_bytes(int M, int E, int K, int N);
 size_t fp8_rows_bytes_most(int64_t M, int K, int N);
 // The form of a product, the rows of its row blocks and the shares of K.
-enum class Fp8Form { STREAM_1 };
+enum class Fp8Form { STREAM_1, TILE_64, TILE_128, TILE_256 };
 struct Fp8Plan {
   Fp8Form form;
   int tm, split;
