@@ -38,6 +38,15 @@ __device__ __forceinline__ f32x4 mfma_fp8(const u32x4 (&w)[2], const u32x4 (&a)[
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, J, (int)as);
 }
 
+// the largest of the lanes kq*16 + i with the same i
+__device__ __forceinline__ uint32_t max_of_kq(uint32_t m) {
+  typedef uint32_t Two __attribute__((ext_vector_type(2)));
+  Two t = __builtin_amdgcn_permlane16_swap(m, m, false, false);  // rows of 16 lanes 0 0 2 2 and 1 1 3 3
+  m = max(t[0], t[1]);
+  t = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return max(t[0], t[1]);
+}
+
 struct Fp8Args : ProductArgs {
   const uint8_t *w0, *w1;      // codes; the scales follow all codes
   const float *s0, *s1;
@@ -54,7 +63,9 @@ struct Fp8Args : ProductArgs {
 // added in wave order.  Nothing is staged: a weight block is two coalesced
 // kilobytes, read once from memory by the wave that multiplies it, U groups of
 // each tile at a time and the next U on their way.
-template <int W, int MT, int NT, int U, Epilogue EPI>
+// RAW: a single launch for very few rows, which each wave quantises itself as it
+// reads them; the block's expert is found from the offsets.
+template <int W, int MT, int NT, int U, bool RAW, Epilogue EPI>
 __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
   constexpr bool SW = EPI == OUT_SWIGLU;
   constexpr int kC = SW ? NT / 2 : NT;
@@ -63,7 +74,9 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int rb = blockIdx.x / a.col_blocks, cb = blockIdx.x - rb * a.col_blocks;
-  const RowBlock b = row_block(a, rb, 16 * MT);
+  // RAW: at most 16 rows, whose list is read beside the offsets
+  const int listed = RAW && a.rows && lane < a.M ? a.rows[lane] : 0;
+  const RowBlock b = RAW ? find_block(a, rb, 16 * MT, blockIdx.x == 0 && wave == 0) : row_block(a, rb, 16 * MT);
   if (b.n <= 0) return;
   const int t0 = cb * kC;
   const int C = (a.G + U - 1) / U;  // chunks of U groups
@@ -72,9 +85,10 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
   const auto rw0 = buffer_rsrc(a.w0 + b.e * a.w_stride, wb), rs0 = buffer_rsrc(reinterpret_cast<const uint8_t*>(a.s0) + b.e * a.s_stride, sb);
   const auto rw1 = buffer_rsrc((SW ? a.w1 : a.w0) + b.e * a.w_stride, wb);
   const auto rs1 = buffer_rsrc(reinterpret_cast<const uint8_t*>(SW ? a.s1 : a.s0) + b.e * a.s_stride, sb);
-  const auto ra = buffer_rsrc(a.a, a.a_bytes), ras = buffer_rsrc(a.as, a.as_bytes);
+  const auto ra = RAW ? buffer_rsrc(a.x, a.x_bytes) : buffer_rsrc(a.a, a.a_bytes);
+  const auto ras = buffer_rsrc(a.as, RAW ? 0u : a.as_bytes);
   struct Stage {
-    u32x4 w[U][NT][2], x[U][MT][2];
+    u32x4 w[U][NT][2], x[U][MT][RAW ? 4 : 2];
     uint32_t ws[U][NT], xs[MT];
   };
   auto load_weights = [&](Stage& s, int c) {
@@ -102,10 +116,15 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int m = 16 * mt + r16;
-    const int src = m >= b.n ? -1 : source_row(a, b.m0 + m);
+    const int row = RAW && a.rows ? __shfl(listed, (b.m0 + m) & 63, kWave) : 0;
+    const int src = m >= b.n ? -1 : RAW && a.rows ? source_of(a, row) : source_row(a, b.m0 + m);
     live[mt] = src >= 0;
-    va[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G * 128) + (uint32_t)kq * 16u : kOutside;
-    vs[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G4 * 4) : kOutside;
+    if constexpr (RAW) {
+      va[mt] = live[mt] ? (uint32_t)src * a.x_row + (uint32_t)kq * 32u : kOutside;
+    } else {
+      va[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G * 128) + (uint32_t)kq * 16u : kOutside;
+      vs[mt] = live[mt] ? (uint32_t)src * (uint32_t)(a.G4 * 4) : kOutside;
+    }
   }
   f32x4 acc[MT][NT];
 #pragma unroll
@@ -117,33 +136,64 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint32_t g = (uint32_t)(c * U + u);
-        const bool in = g < (uint32_t)a.G;
+        const uint32_t g = (uint32_t)(c * U + u), at = g < (uint32_t)a.G ? g : 0u;
+        if constexpr (RAW) {
+          // pieces kq and kq + 4 of 16 values each, as far as the row has them
 #pragma unroll
-        for (int h = 0; h < 2; ++h) s.x[u][mt][h] = buffer_load_x4(ra, in ? va[mt] : kOutside, in ? g * 128u + 64u * h : 0u);
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t v = (int)(8 * g) + 4 * (q >> 1) + kq < a.pieces ? va[mt] : kOutside;
+            s.x[u][mt][q] = buffer_load_x4(ra, v, at * 256u + 128u * (q >> 1) + 16u * (q & 1));
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) s.x[u][mt][h] = buffer_load_x4(ra, g < (uint32_t)a.G ? va[mt] : kOutside, at * 128u + 64u * h);
+        }
       }
-      s.xs[mt] = buffer_load_x1(ras, vs[mt], (uint32_t)(c * U / 4) * 4u);
+      if constexpr (!RAW) s.xs[mt] = buffer_load_x1(ras, vs[mt], (uint32_t)(c * U / 4) * 4u);
     }
   };
   auto load = [&](Stage& s, int c) {
     load_weights(s, c);
     load_rows(s, c);
   };
-  auto multiply = [&](Stage& s, int c) {
-    const int sh = 8 * ((c * U) & 3);  // this chunk's bytes of its scale words
+  // the rows' operand of group u and its scale (RAW: in byte 0)
+  auto operand = [&](const Stage& s, int u, int mt, u32x4 (&x)[2], uint32_t& scale) {
+    if constexpr (RAW) {
+      const u32x4* v = s.x[u][mt];
+      const uint32_t m = max_of_kq(max(max(fp8_magnitude(v[0]), fp8_magnitude(v[1])), max(fp8_magnitude(v[2]), fp8_magnitude(v[3]))));
+      scale = fp8_scale_of(m);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) s.xs[mt] >>= sh;
+      for (int h = 0; h < 2; ++h) {
+        const u32x2 lo = fp8_codes(v[2 * h], scale), hi = fp8_codes(v[2 * h + 1], scale);
+        x[h] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      }
+    } else {
+      scale = s.xs[mt];
+      x[0] = s.x[u][mt][0];
+      x[1] = s.x[u][mt][1];
+    }
+  };
+  auto multiply = [&](Stage& s, int c) {
+    if constexpr (!RAW) {
+      const int sh = 8 * ((c * U) & 3);  // this chunk's bytes of its scale words
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) s.xs[mt] >>= sh;
+    }
     auto group = [&](auto uc) {
       constexpr int u = decltype(uc)::value;
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int mt = 0; mt < MT; ++mt) {
+        u32x4 x[2];
+        uint32_t xs;
+        operand(s, u, mt, x, xs);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const f32x4 p = mfma_fp8<u>(s.w[u][nt], s.x[u][mt], s.xs[mt]);
+          const f32x4 p = mfma_fp8<RAW ? 0 : u>(s.w[u][nt], x, xs);
           const float ws = bitcast<float>(s.ws[u][nt]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[mt][nt][i] = __builtin_fmaf(ws, p[i], acc[mt][nt][i]);
         }
+      }
     };
     group(std::integral_constant<int, 0>{});
     group(std::integral_constant<int, 1>{});
@@ -445,11 +495,11 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_tile_kernel(Fp8Args a) {
   }
 }
 
-template <int W, int MT, int NT, Epilogue EPI>
+template <int W, int MT, int NT, bool RAW, Epilogue EPI>
 void launch_stream(Fp8Args a, int blocks, hipStream_t st) {
   constexpr int kC = EPI == OUT_SWIGLU ? NT / 2 : NT;
   a.col_blocks = (a.Nt + kC - 1) / kC;
-  hipLaunchKernelGGL((fp8_stream_kernel<W, MT, NT, 2, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(64 * W), 0, st, a);
+  hipLaunchKernelGGL((fp8_stream_kernel<W, MT, NT, 2, RAW, EPI>), dim3((unsigned)blocks * a.col_blocks), dim3(64 * W), 0, st, a);
 }
 
 template <int WM, int WN, int MTW, int NTW, int ST, Epilogue EPI>
@@ -461,18 +511,33 @@ void launch_tile(Fp8Args a, int blocks, hipStream_t st) {
 }
 
 // of each Fp8Form
-constexpr int kRowsOf[] = {16, 64, 128, 256};
-constexpr int kColumnsOf[] = {32, 128, 128, 256};
-constexpr int kThreadsOf[] = {512, 256, 256, 512};
+constexpr int kRowsOf[] = {16, 16, 32, 64, 128, 256};
+constexpr int kColumnsOf[] = {32, 32, 32, 128, 128, 256};
+constexpr int kThreadsOf[] = {512, 512, 512, 256, 256, 512};
 
 }  // namespace
 
 Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
+  const int G4 = (fp8_blocks(K) + 3) / 4;
+  const int64_t weights = (int64_t)(E < M ? E : M) * K * N * (swiglu ? 2 : 1);  // bytes that are read, at most
   auto plan = [](Fp8Form f, int split = 1) { return Fp8Plan{f, kRowsOf[(int)f], split}; };
+  // shares of K that bring the tiles to one for each compute unit, each of at least
+  // `least` scale words (four groups each)
+  auto split_of = [&](int64_t tiles, int least) {
+    const int64_t want = 256 / tiles, most = G4 / least;
+    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+  };
+  auto tiles = [&](Fp8Form f) {
+    const int64_t rows = kRowsOf[(int)f], blocks = grouped ? M / rows + std::min(E, M) / 2 : (M + rows - 1) / rows;
+    return std::max<int64_t>(1, std::max<int64_t>(grouped ? std::min(E, M) : 1, blocks)) * ((N * (int64_t)(swiglu ? 2 : 1) + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]);
+  };
+  if (raw && M <= 8 && weights <= (64 << 20)) return plan(Fp8Form::STREAM_RAW);
   const int64_t avg = grouped ? M / E : M;
-  if (avg < 8) return plan(Fp8Form::STREAM_1);
-  if (avg <= 64) return plan(Fp8Form::TILE_64);
-  if (avg <= 256) return plan(Fp8Form::TILE_128);
+  if (grouped && M < 4ll * E) return plan(Fp8Form::STREAM_1);
+  if (!grouped && M <= 16) return plan(Fp8Form::STREAM_1);
+  if (!grouped && M <= 32) return plan(Fp8Form::STREAM_2);
+  if (avg <= 64) return plan(Fp8Form::TILE_64, swiglu ? 1 : split_of(tiles(Fp8Form::TILE_64), 2));
+  if (avg <= 256) return plan(Fp8Form::TILE_128, swiglu ? 1 : split_of(tiles(Fp8Form::TILE_128), 2));
   return plan(Fp8Form::TILE_256);
 }
 
@@ -481,7 +546,11 @@ namespace {
 template <Epilogue EPI>
 void launch_form(const Fp8Plan& p, const Fp8Args& a, int blocks, hipStream_t st) {
   switch (p.form) {
-    case Fp8Form::STREAM_1: return launch_stream<8, 1, 2, EPI>(a, blocks, st);
+    case Fp8Form::STREAM_RAW: return launch_stream<8, 1, 2, true, EPI>(a, blocks, st);
+    case Fp8Form::STREAM_1: return launch_stream<8, 1, 2, false, EPI>(a, blocks, st);
+    case Fp8Form::STREAM_2:
+      if constexpr (EPI == OUT_PLAIN || EPI == OUT_RESIDUAL) launch_stream<8, 2, 2, false, EPI>(a, blocks, st);
+      return;
     case Fp8Form::TILE_64: return launch_tile<1, 4, 4, 2, 4, EPI>(a, blocks, st);
     case Fp8Form::TILE_128: return launch_tile<2, 2, 4, 4, 2, EPI>(a, blocks, st);
     case Fp8Form::TILE_256: return launch_tile<2, 4, 8, 4, 2, EPI>(a, blocks, st);
@@ -494,6 +563,8 @@ int launch_fp8_gemm(const ProductLaunch& L, hipStream_t st) {
   // rows that the product may read itself: within a 2 GiB buffer, not overwritten
   const uint64_t x_bytes = ((uint64_t)(L.a_rows - 1) * L.ldx + L.K) * 2;
   const Fp8Plan p = plan_fp8_gemm(L.M, L.E, L.K, L.N, L.epi == OUT_SWIGLU, L.offsets, x_bytes < kOutside && !L.x_written);
+  // 32 rows a workgroup: one matrix whose K is whole
+  if (p.form == Fp8Form::STREAM_2 && (L.offsets || p.split > 1)) return 0;
   RowMap map = {};
   map.offsets = L.offsets;
   map.E = L.E;
@@ -502,7 +573,8 @@ int launch_fp8_gemm(const ProductLaunch& L, hipStream_t st) {
   map.blocks = L.offsets ? row_blocks(L.M, L.E, p.tm) : (L.M + p.tm - 1) / p.tm;
   map.map = L.map;
   map.ws = L.ws;
-  launch_fp8_prepare(L.x, L.a_rows, L.K, L.ldx, L.a, L.a_scales, L.rows ? nullptr : L.offsets, map, st);
+  if (p.form != Fp8Form::STREAM_RAW)
+    launch_fp8_prepare(L.x, L.a_rows, L.K, L.ldx, L.a, L.a_scales, L.rows ? nullptr : L.offsets, map, st);
   Fp8Args a = {};
   const size_t wq = fp8_code_bytes(L.N, L.K), wsb = fp8_matrix_scale_bytes(L.K, L.N);
   a.w0 = static_cast<const uint8_t*>(L.w0);
@@ -542,6 +614,9 @@ int launch_fp8_gemm(const ProductLaunch& L, hipStream_t st) {
     launch_form<OUT_SWIGLU>(p, a, map.blocks, st);
   } else if (L.epi == OUT_ROWS) {
     launch_form<OUT_ROWS>(p, a, map.blocks, st);
+  } else if (p.split > 1) {
+    launch_form<OUT_ROWS>(p, a, map.blocks, st);
+    launch_product_sum(L.part, p.split, L.M, L.N, L.y, L.ldy, L.res, L.ldr, st);
   } else if (L.res) {
     launch_form<OUT_RESIDUAL>(p, a, map.blocks, st);
   } else {
@@ -561,9 +636,30 @@ bool fp8_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped) {
   return true;
 }
 
-size_t fp8_part_bytes(int, int, int) { return 0; }
-size_t fp8_part_bytes_most(int, int, int) { return 0; }
-size_t fp8_rows_bytes(int M, int, int, int N) { return (size_t)M * N * sizeof(float); }
-size_t fp8_rows_bytes_most(int64_t M, int, int N) { return (size_t)M * N * sizeof(float); }
+size_t fp8_part_bytes(int M, int K, int N) {
+  const Fp8Plan p = plan_fp8_gemm(M, 1, K, N, false, false, false);
+  return p.split > 1 ? (size_t)p.split * M * N * sizeof(float) : 0;
+}
+
+size_t fp8_part_bytes_most(int M, int K, int N) {
+  // at most 256 tiles' worth of parts, and no more shares than plan_fp8_gemm allows
+  const int64_t G4 = (fp8_blocks(K) + 3) / 4;
+  auto most = [&](Fp8Form f, int64_t split) {
+    const int64_t all = 256ll * kRowsOf[(int)f] * kColumnsOf[(int)f], mine = split * M * N;
+    return split > 1 ? (size_t)(all < mine ? all : mine) * sizeof(float) : 0;
+  };
+  const size_t a = most(Fp8Form::TILE_128, G4 / 2), b = most(Fp8Form::TILE_256, G4 / 14);
+  return a > b ? a : b;
+}
+
+size_t fp8_rows_bytes(int M, int E, int K, int N) {
+  return (size_t)plan_fp8_gemm(M, E, K, N, false, true, false).split * M * N * sizeof(float);
+}
+
+size_t fp8_rows_bytes_most(int64_t M, int K, int N) {
+  // one part, or as many as plan_fp8_gemm allows of at most 256 tiles
+  const size_t one = (size_t)M * N * sizeof(float), all = std::max<int64_t>((fp8_blocks(K) + 3) / 4 / 2, 1) * one;
+  return std::max(one, std::min(all, (size_t)256 * 128 * 128 * sizeof(float)));
+}
 
 }  // namespace ss

@@ -39,8 +39,9 @@ bool fp8_grid_fits(int M, int E, int K, int N, bool swiglu, bool grouped);
 // of the fp32 rows of an experts' product (ROWS), exactly, and the most of up to M rows
 size_t fp8_rows_bytes(int M, int E, int K, int N);
 size_t fp8_rows_bytes_most(int64_t M, int K, int N);
-// The form of a product, the rows of its row blocks and the shares of K.
-enum class Fp8Form { STREAM_1, TILE_64, TILE_128, TILE_256 };
+// The form of a product, the rows of its row blocks and the shares of K.  raw: the
+// product may read the rows itself.
+enum class Fp8Form { STREAM_RAW, STREAM_1, STREAM_2, TILE_64, TILE_128, TILE_256 };
 struct Fp8Plan {
   Fp8Form form;
   int tm, split;

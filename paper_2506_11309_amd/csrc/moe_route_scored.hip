@@ -46,6 +46,34 @@ __device__ __forceinline__ float key_value(uint32_t key) {
   return bitcast<float>(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
+// e^x in 64 bits for -200 <= x <= 200: x = n log 2 + r with |r| <= 0.3466, e^r by its
+// series up to r^12 (what is left out is below 2^-52)
+__device__ __forceinline__ double exp64(double x) {
+  const float n = __builtin_rintf((float)x * 1.44269504f);
+  double r = __builtin_fma((double)n, -0x1.62e42fefa39efp-1, x);
+  r = __builtin_fma((double)n, -0x1.abc9e3b39803fp-56, r);
+  double y = 1.0 / 479001600;
+  y = __builtin_fma(y, r, 1.0 / 39916800);
+  y = __builtin_fma(y, r, 1.0 / 3628800);
+  y = __builtin_fma(y, r, 1.0 / 362880);
+  y = __builtin_fma(y, r, 1.0 / 40320);
+  y = __builtin_fma(y, r, 1.0 / 5040);
+  y = __builtin_fma(y, r, 1.0 / 720);
+  y = __builtin_fma(y, r, 1.0 / 120);
+  y = __builtin_fma(y, r, 1.0 / 24);
+  y = __builtin_fma(y, r, 1.0 / 6);
+  y = __builtin_fma(y, r, 0.5);
+  y = __builtin_fma(y, r, 1.0);
+  y = __builtin_fma(y, r, 1.0);
+  return __builtin_amdgcn_ldexp(y, (int)n);
+}
+// 1 / x for x >= 1, two of Newton's steps behind the instruction's own 2^-14 or better
+__device__ __forceinline__ double reciprocal64(double x) {
+  double y = __builtin_amdgcn_rcp(x);
+  y = __builtin_fma(__builtin_fma(-x, y, 1.0), y, y);
+  return __builtin_fma(__builtin_fma(-x, y, 1.0), y, y);
+}
+
 // score e of a row, +inf as the largest finite value
 template <typename T>
 __device__ __forceinline__ float score_at(const T* row, int e) {
@@ -69,28 +97,43 @@ __device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, i
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = l + 16 * i < a.E ? score_at(row, l + 16 * i) : -__builtin_inff();
   float top = 0.f;
-  double total = 1.0;
-  if constexpr (!SIGMOID) {
+  // e^-v of a gate, e^(v - top) of a probability; beyond these limits it is 0 or 1 in 32
+  // bits.  The difference has more than 24 bits.
+  auto power = [&](float v) {
+    return exp64(SIGMOID ? (double)__builtin_fminf(__builtin_fmaxf(-v, -100.f), 200.f) : __builtin_fmax((double)v - (double)top, -200.0));
+  };
+  double share = 1.0;  // of a softmax: 1 / the sum
+  uint32_t key[V];
+  if constexpr (SIGMOID) {
+    // one after the other: side by side their 64-bit values would not fit the registers
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float s = (float)reciprocal64(1.0 + power(x[i]));
+      const int e = l + 16 * i;
+      key[i] = x[i] > -__builtin_inff() ? value_key(s + (a.bias ? a.bias[e] : 0.f)) : 0u;
+      asm volatile("" : "+v"(key[i]));
+    }
+  } else {
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) m = max(m, value_key(x[i]));
     m = row_max(m);
     top = m ? key_value(m) : 0.f;
-    total = 0.0;
+    double total = 0.0;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (x[i] > -__builtin_inff()) total += exp((double)x[i] - (double)top);
+    for (int i = 0; i < V; ++i) {
+      if (x[i] > -__builtin_inff()) total += power(x[i]);
+      asm volatile("" : "+v"(total));
+    }
     total = row_sum(total);
-  }
-  auto gate = [&](float v) {
-    return (float)(SIGMOID ? 1.0 / (1.0 + exp(-(double)v)) : exp((double)v - (double)top) / total);
-  };
-  uint32_t key[V];
+    share = total >= 1.0 ? reciprocal64(total) : 0.0;
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = l + 16 * i;
-    key[i] = 0;
-    if (x[i] > -__builtin_inff()) key[i] = value_key(gate(x[i]) + (a.bias ? a.bias[e] : 0.f));
+    for (int i = 0; i < V; ++i) {
+      const float s = (float)(power(x[i]) * share);
+      const int e = l + 16 * i;
+      key[i] = x[i] > -__builtin_inff() ? value_key(s + (a.bias ? a.bias[e] : 0.f)) : 0u;
+      asm volatile("" : "+v"(key[i]));
+    }
   }
   if (a.top_groups < a.groups) {
 #pragma unroll
@@ -148,7 +191,11 @@ __device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, i
     for (int i = 0; i < V; ++i)
       if ((uint32_t)(l + 16 * i) == e) key[i] = 0;
   }
-  const float s = mine >= 0 ? gate(score_at(row, mine)) : 0.f;
+  float s = 0.f;
+  if (mine >= 0) {
+    const float v = score_at(row, mine);
+    s = (float)(SIGMOID ? reciprocal64(1.0 + power(v)) : power(v) * share);
+  }
   const double sum = a.renormalize ? row_sum((double)s) : 1.0;
   if (l < a.k && there) {
     a.experts[(int64_t)t * a.k + l] = mine;
