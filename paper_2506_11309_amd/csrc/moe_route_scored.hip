@@ -20,6 +20,9 @@ struct ScoredArgs : GroupArgs {
   const float* bias;
   int groups, size, top_groups, best;  // size: experts of a group
   uint32_t per;                        // ceil(2^18 / size): e * per >> 18 is e's group
+  int block;                           // experts of a lane: e = lane * block + i
+  int lanes;                           // lanes of a group if that is 1, 2, 4 or 8, otherwise 0
+  bool lines;                          // scores and bias can be read four at a time
   bool renormalize;
   float scale;
 };
@@ -40,33 +43,39 @@ __device__ __forceinline__ double row_sum(double v) {
 // ascending key of a float, 0 for -inf and NaN
 __device__ __forceinline__ uint32_t value_key(float c) {
   const uint32_t b = bitcast<uint32_t>(c);
-  return c > -__builtin_inff() ? (b & 0x80000000u ? ~b : b | 0x80000000u) : 0u;
+  const uint32_t key = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);  // all bits of a negative value, the sign of others
+  return c > -__builtin_inff() ? key : 0u;
 }
 __device__ __forceinline__ float key_value(uint32_t key) {
-  return bitcast<float>(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+  return bitcast<float>(key ^ (~(uint32_t)((int32_t)key >> 31) | 0x80000000u));
 }
 
 // e^x in 64 bits for -200 <= x <= 200: x = n log 2 + r with |r| <= 0.3466, e^r by its
-// series up to r^12 (what is left out is below 2^-52)
-__device__ __forceinline__ double exp64(double x) {
-  const float n = __builtin_rintf((float)x * 1.44269504f);
-  double r = __builtin_fma((double)n, -0x1.62e42fefa39efp-1, x);
-  r = __builtin_fma((double)n, -0x1.abc9e3b39803fp-56, r);
-  double y = 1.0 / 479001600;
-  y = __builtin_fma(y, r, 1.0 / 39916800);
-  y = __builtin_fma(y, r, 1.0 / 3628800);
-  y = __builtin_fma(y, r, 1.0 / 362880);
-  y = __builtin_fma(y, r, 1.0 / 40320);
-  y = __builtin_fma(y, r, 1.0 / 5040);
-  y = __builtin_fma(y, r, 1.0 / 720);
-  y = __builtin_fma(y, r, 1.0 / 120);
-  y = __builtin_fma(y, r, 1.0 / 24);
-  y = __builtin_fma(y, r, 1.0 / 6);
-  y = __builtin_fma(y, r, 0.5);
-  y = __builtin_fma(y, r, 1.0);
-  y = __builtin_fma(y, r, 1.0);
-  return __builtin_amdgcn_ldexp(y, (int)n);
-}
+// series up to r^12 (what is left out is below 2^-52).  The coefficients stay in scalar
+// registers: the compiler would move each into a vector register at every use.
+struct Exp64 {
+  double c[11];
+  __device__ __forceinline__ Exp64() {
+    double f = 1.0;
+#pragma unroll
+    for (int i = 0; i < 11; ++i) {
+      f /= i + 2;  // 1 / 2! ... 1 / 12!
+      c[i] = f;
+      asm volatile("" : "+s"(c[i]));
+    }
+  }
+  __device__ __forceinline__ double operator()(double x) const {
+    const float n = __builtin_rintf((float)x * 1.44269504f);
+    double r = __builtin_fma((double)n, -0x1.62e42fefa39efp-1, x);
+    r = __builtin_fma((double)n, -0x1.abc9e3b39803fp-56, r);
+    double y = c[10];
+#pragma unroll
+    for (int i = 9; i >= 0; --i) y = __builtin_fma(y, r, c[i]);
+    y = __builtin_fma(y, r, 1.0);
+    y = __builtin_fma(y, r, 1.0);
+    return __builtin_amdgcn_ldexp(y, (int)n);
+  }
+};
 // 1 / x for x >= 1, two of Newton's steps behind the instruction's own 2^-14 or better
 __device__ __forceinline__ double reciprocal64(double x) {
   double y = __builtin_amdgcn_rcp(x);
@@ -74,28 +83,96 @@ __device__ __forceinline__ double reciprocal64(double x) {
   return __builtin_fma(__builtin_fma(-x, y, 1.0), y, y);
 }
 
+__device__ __forceinline__ float finite(float x, float most) { return x == __builtin_inff() ? most : x; }
 // score e of a row, +inf as the largest finite value
 template <typename T>
 __device__ __forceinline__ float score_at(const T* row, int e) {
+  if constexpr (sizeof(T) == 2) return finite(h2f(row[e]), 65504.f);
+  else return finite(row[e], 3.4028234663852886e38f);
+}
+// scores e .. e + 3
+template <typename T>
+__device__ __forceinline__ void scores_at(const T* row, int e, float* x) {
   if constexpr (sizeof(T) == 2) {
-    const float x = h2f(row[e]);
-    return x == __builtin_inff() ? 65504.f : x;
+    const u32x2 v = *reinterpret_cast<const u32x2*>(row + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = finite(h2f((uint16_t)(v[i >> 1] >> (16 * (i & 1)))), 65504.f);
   } else {
-    const float x = row[e];
-    return x == __builtin_inff() ? 3.4028234663852886e38f : x;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(row + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = finite(v[i], 3.4028234663852886e38f);
   }
 }
 
-// 16 lanes take a token, V scores each: e = lane + 16 i.  room: V * 16 words of LDS of
+// The two largest of a and of what another lane holds.
+__device__ __forceinline__ void merge_two(uint32_t& first, uint32_t& second, uint32_t f, uint32_t s) {
+  second = max(min(first, f), max(second, s));
+  first = max(first, f);
+}
+template <int kCtrl>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, kCtrl, 0xF, 0xF, true);
+}
+template <int kBy>
+__device__ __forceinline__ void count_before(uint32_t v, uint32_t g, int& n) {
+  // the lane kBy before, round the row, and its group
+  const uint32_t w = rotated<kBy>(v), o = rotated<kBy>(g);
+  n += w > v || (w == v && o < g);
+  if constexpr (kBy < 15) count_before<kBy + 1>(v, g, n);
+}
+
+// Whether this lane's group of a.lanes neighbours is among the best: the lanes' two
+// largest keys are merged, and the lanes of better groups counted.
+template <int V>
+__device__ __forceinline__ bool group_taken(const ScoredArgs& a, const uint32_t (&key)[V]) {
+  uint32_t first = 0, second = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) merge_two(first, second, key[i], 0u);
+  if (a.lanes >= 2) merge_two(first, second, from_lane<0xB1>(first), from_lane<0xB1>(second));    // lane ^ 1
+  if (a.lanes >= 4) merge_two(first, second, from_lane<0x4E>(first), from_lane<0x4E>(second));    // lane ^ 2
+  if (a.lanes >= 8) merge_two(first, second, from_lane<0x141>(first), from_lane<0x141>(second));  // the other four of eight
+  if (a.best == 2 && second) first = value_key(key_value(first) + key_value(second));
+  const uint32_t g = (uint32_t)(lane_id() & 15) / (uint32_t)a.lanes;
+  int n = 0;
+  count_before<1>(first, g, n);
+  return n < a.top_groups * a.lanes;
+}
+
+// v[i] = v[i + N], round the array: a loop over N values at a time finds them in the same
+// registers, where unrolled it would be a page of code that a short kernel waits for
+template <int V, int N, typename T>
+__device__ __forceinline__ void rotate(T (&v)[V]) {
+  if constexpr (N < V) {
+    T t[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = v[(i + N) % V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = t[i];
+  }
+}
+
+// 16 lanes take a token, up to V neighbouring scores each.  room: V * 16 words of LDS of
 // this token.  Lane j < k keeps the j-th expert.  Where t >= T nothing is written.
 template <int V, bool SIGMOID, typename T>
 __device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, int* counts, int16_t* chosen, uint32_t* room) {
-  const int l = lane_id() & 15;
+  const int l = lane_id() & 15, e0 = l * a.block, n = max(0, min(a.block, a.E - e0));
+  constexpr int kStep = V < 4 ? V : 4;
   const bool there = t < a.T;
   const T* row = static_cast<const T*>(a.logits) + (int64_t)(there ? t : 0) * a.ldl;
   float x[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = l + 16 * i < a.E ? score_at(row, l + 16 * i) : -__builtin_inff();
+  for (int i = 0; i < V; ++i) x[i] = -__builtin_inff();
+  const bool lines = V >= 4 && a.lines;
+  if (lines) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4)
+      if (i < n) scores_at(row, e0 + i, x + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < n) x[i] = score_at(row, e0 + i);
+  }
+  const Exp64 exp64;
   float top = 0.f;
   // e^-v of a gate, e^(v - top) of a probability; beyond these limits it is 0 or 1 in 32
   // bits.  The difference has more than 24 bits.
@@ -104,41 +181,61 @@ __device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, i
   };
   double share = 1.0;  // of a softmax: 1 / the sum
   uint32_t key[V];
-  if constexpr (SIGMOID) {
-    // one after the other: side by side their 64-bit values would not fit the registers
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float s = (float)reciprocal64(1.0 + power(x[i]));
-      const int e = l + 16 * i;
-      key[i] = x[i] > -__builtin_inff() ? value_key(s + (a.bias ? a.bias[e] : 0.f)) : 0u;
-      asm volatile("" : "+v"(key[i]));
-    }
-  } else {
+  if constexpr (!SIGMOID) {
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) m = max(m, value_key(x[i]));
     m = row_max(m);
     top = m ? key_value(m) : 0.f;
     double total = 0.0;
+#pragma unroll 1
+    for (int q = 0; q < V; q += kStep) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (x[i] > -__builtin_inff()) total += power(x[i]);
-      asm volatile("" : "+v"(total));
+      for (int i = 0; i < kStep; ++i) {
+        double p = power(x[i]);
+        asm volatile("" : "+v"(p));  // one after the other: side by side the 64-bit values would not fit the registers
+        total += x[i] > -__builtin_inff() ? p : 0.0;
+      }
+      rotate<V, kStep>(x);
     }
     total = row_sum(total);
     share = total >= 1.0 ? reciprocal64(total) : 0.0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float s = (float)(power(x[i]) * share);
-      const int e = l + 16 * i;
-      key[i] = x[i] > -__builtin_inff() ? value_key(s + (a.bias ? a.bias[e] : 0.f)) : 0u;
-      asm volatile("" : "+v"(key[i]));
-    }
   }
-  if (a.top_groups < a.groups) {
+  auto score = [&](float v) { return (float)(SIGMOID ? reciprocal64(1.0 + power(v)) : power(v) * share); };
+#pragma unroll 1
+  for (int q = 0; q < V; q += kStep) {
+    float b[kStep] = {};
+    if (a.bias) {
+      if (lines) {
+        if (q < n) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(a.bias + e0 + q);
+#pragma unroll
+          for (int i = 0; i < kStep; ++i) b[i] = v[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) b[i] = q + i < n ? a.bias[e0 + q + i] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kStep; ++i) {
+      float s = score(x[i]);
+      asm volatile("" : "+v"(s));
+      // a masked score makes the sum -inf
+      key[i] = value_key(x[i] > -__builtin_inff() ? s + b[i] : -__builtin_inff());
+    }
+    rotate<V, kStep>(x);
+    rotate<V, kStep>(key);
+  }
+  if (a.lanes) {
+    if (!group_taken<V>(a, key)) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) key[i] = 0;
+    }
+  } else if (a.top_groups < a.groups) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (l + 16 * i < a.E) room[l + 16 * i] = key[i];
+      if (i < n) room[e0 + i] = key[i];
     __builtin_amdgcn_wave_barrier();
     for (int g = l; g < a.groups; g += 16) {
       // its two largest; the lanes start at different members, so that they read
@@ -171,7 +268,7 @@ __device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, i
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int e = min(l + 16 * i, a.E - 1);
+      const int e = min(e0 + i, a.E - 1);
       if (!room[((uint32_t)e * a.per >> 18) * a.size]) key[i] = 0;
     }
     __builtin_amdgcn_wave_barrier();
@@ -183,19 +280,16 @@ __device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, i
     for (int i = 0; i < V; ++i) m = max(m, key[i]);
     m = row_max(m);
 #pragma unroll
-    for (int i = V - 1; i >= 0; --i) e = key[i] == m ? (uint32_t)(l + 16 * i) : e;
+    for (int i = V - 1; i >= 0; --i) e = key[i] == m ? (uint32_t)(e0 + i) : e;
     e = row_min(e);
     if (!m) break;  // of this token: its lanes leave together
     if (l == j) mine = (int)e;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if ((uint32_t)(l + 16 * i) == e) key[i] = 0;
+      key[i] = (uint32_t)i == e - (uint32_t)e0 ? 0u : key[i];
   }
   float s = 0.f;
-  if (mine >= 0) {
-    const float v = score_at(row, mine);
-    s = (float)(SIGMOID ? reciprocal64(1.0 + power(v)) : power(v) * share);
-  }
+  if (mine >= 0) s = score(score_at(row, mine));
   const double sum = a.renormalize ? row_sum((double)s) : 1.0;
   if (l < a.k && there) {
     a.experts[(int64_t)t * a.k + l] = mine;
@@ -278,6 +372,11 @@ void launch_moe_route_scored(const ScoredLaunch& L, hipStream_t st) {
   a.top_groups = L.top_groups;
   a.best = L.best;
   a.per = ((1u << 18) + a.size - 1) / a.size;
+  a.block = (a.E + 15) / 16;
+  const int lanes = a.size % a.block ? 0 : a.size / a.block;
+  a.lanes = a.top_groups < a.groups && (lanes == 1 || lanes == 2 || lanes == 4 || lanes == 8) && lanes * a.groups <= 16 ? lanes : 0;
+  a.lines = a.block % 4 == 0 && a.E % 4 == 0 && a.ldl % 4 == 0 && reinterpret_cast<uintptr_t>(a.logits) % (L.wide ? 16 : 8) == 0 &&
+            reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
   a.renormalize = L.renormalize;
   a.scale = L.scale;
   if (L.sigmoid) L.wide ? launch_width<true, float>(a, st) : launch_width<true, uint16_t>(a, st);
