@@ -247,8 +247,8 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
 // (row / 2 % 8), so that a column of 16 rows covers the 64 banks once.
 // A step multiplies one group: the weights' blocks of the wave stay in registers, the
 // rows' blocks follow one another, the next on its way from LDS.  Each instruction's
-// result is multiplied and added two instructions later, so that its latency does not
-// show.  Before the last block of rows the wave has read all it needs of this stage: it
+// result is multiplied and added three instructions later, so that its latency does not
+// show (two later: 8192 x 8192 x 8192 474 against 462 us).  Before the last block of rows the wave has read all it needs of this stage: it
 // waits for its loads of the next one and for the other waves, and reads the first
 // operands of the next step while the last block is multiplied; the stage's place is
 // loaded anew during the next step.  One barrier a step.
@@ -404,12 +404,12 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_tile_kernel(Fp8Args a) {
       if (q == kLast) read_x(0, kNext, c + (J == 3 ? 1 : 0));
       if (q >= kLast) read_w(j, kNext);
       if (q < kLoads) load(q, g + ST - 1, kFree);
-      // the result of two instructions before
-      const int o = (q + kMfma - 2) % kMfma, oi = o / NTW, oj = o % NTW;
+      // the result of three instructions before
+      const int o = (q + kMfma - 3) % kMfma, oi = o / NTW, oj = o % NTW;
       const bool up = SW && (oj & 1);
-      const float s = q < 2 ? (up ? before1 : before0) : (up ? now1 : now0);
+      const float s = q < 3 ? (up ? before1 : before0) : (up ? now1 : now0);
 #pragma unroll
-      for (int v = 0; v < 4; ++v) acc[oi][oj][v] = __builtin_fmaf(s, p[(q + 2) & 3][v], acc[oi][oj][v]);
+      for (int v = 0; v < 4; ++v) acc[oi][oj][v] = __builtin_fmaf(s, p[(q + 1) & 3][v], acc[oi][oj][v]);
       asm volatile("" : "+v"(acc[oi][oj]));
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -423,9 +423,9 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_tile_kernel(Fp8Args a) {
     if (4 * c + 2 < G) step(std::integral_constant<int, 2>{}, c);
     if (4 * c + 3 < G) step(std::integral_constant<int, 3>{}, c);
   }
-  // the last two results
+  // the last three results
 #pragma unroll
-  for (int o = MTW * NTW - 2; o < MTW * NTW; ++o) {
+  for (int o = MTW * NTW - 3; o < MTW * NTW; ++o) {
     const float s = SW && ((o % NTW) & 1) ? before1 : before0;
 #pragma unroll
     for (int v = 0; v < 4; ++v) acc[o / NTW][o % NTW][v] = __builtin_fmaf(s, p[o & 3][v], acc[o / NTW][o % NTW][v]);
@@ -511,34 +511,66 @@ void launch_tile(Fp8Args a, int blocks, hipStream_t st) {
 }
 
 // of each Fp8Form
-constexpr int kRowsOf[] = {16, 16, 32, 64, 128, 256};
-constexpr int kColumnsOf[] = {32, 32, 32, 128, 128, 256};
-constexpr int kThreadsOf[] = {512, 512, 512, 256, 256, 512};
+constexpr int kRowsOf[] = {16, 16, 32, 64, 128, 128, 256};
+constexpr int kColumnsOf[] = {32, 32, 32, 128, 128, 128, 256};
+constexpr int kThreadsOf[] = {256, 256, 256, 256, 512, 256, 512};
+// of the tiles: how many run at one time, and the microseconds that they take together
+// for a group of 128 k, and for first loads and last stores (fitted to the times of 70
+// products from 33 x 4096 x 4096 to 8192 x 8192 x 8192 and of experts)
+constexpr int kSlotsOf[] = {0, 0, 0, 256, 256, 512, 256};
+constexpr double kStepOf[] = {0, 0, 0, 0.45, 0.58, 1.0, 1.65};
+constexpr double kRestOf[] = {0, 0, 0, 1.5, 2.0, 3.0, 5.0};
 
 }  // namespace
 
 Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, bool raw) {
-  const int G4 = (fp8_blocks(K) + 3) / 4;
-  const int64_t weights = (int64_t)(E < M ? E : M) * K * N * (swiglu ? 2 : 1);  // bytes that are read, at most
+  const int G = fp8_blocks(K), G4 = (G + 3) / 4;
+  const int64_t columns = (int64_t)N * (swiglu ? 2 : 1), reached = std::min(E, M);
+  const int64_t weights = reached * K * columns;  // bytes that are read, at most
   auto plan = [](Fp8Form f, int split = 1) { return Fp8Plan{f, kRowsOf[(int)f], split}; };
-  // shares of K that bring the tiles to one for each compute unit, each of at least
-  // `least` scale words (four groups each)
-  auto split_of = [&](int64_t tiles, int least) {
-    const int64_t want = 256 / tiles, most = G4 / least;
-    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
-  };
+  // of experts, whose last block of rows is half full
   auto tiles = [&](Fp8Form f) {
-    const int64_t rows = kRowsOf[(int)f], blocks = grouped ? M / rows + std::min(E, M) / 2 : (M + rows - 1) / rows;
-    return std::max<int64_t>(1, std::max<int64_t>(grouped ? std::min(E, M) : 1, blocks)) * ((N * (int64_t)(swiglu ? 2 : 1) + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]);
+    const int64_t rows = kRowsOf[(int)f], blocks = (M + rows - 1) / rows;
+    return (grouped ? std::max(reached, blocks + reached / 2) : blocks) * ((columns + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]);
   };
-  if (raw && M <= 8 && weights <= (64 << 20)) return plan(Fp8Form::STREAM_RAW);
-  const int64_t avg = grouped ? M / E : M;
-  if (grouped && M < 4ll * E) return plan(Fp8Form::STREAM_1);
-  if (!grouped && M <= 16) return plan(Fp8Form::STREAM_1);
-  if (!grouped && M <= 32) return plan(Fp8Form::STREAM_2);
-  if (avg <= 64) return plan(Fp8Form::TILE_64, swiglu ? 1 : split_of(tiles(Fp8Form::TILE_64), 2));
-  if (avg <= 256) return plan(Fp8Form::TILE_128, swiglu ? 1 : split_of(tiles(Fp8Form::TILE_128), 2));
-  return plan(Fp8Form::TILE_256);
+  // One launch, but every wave quantises the rows that it multiplies: 8 rows of 8192 x
+  // 8192 21.2 against 21.7, 1 row of 2048 x 2048 5.8 against 8.2; 5 rows of 28672 x 8192
+  // (235 MB) 54.4 against 52.4; 16 rows of 4096 x 4096 10.2 against 10.7, of 4096 x 14336
+  // (59 MB) 19.9 against 18.6.  Of experts up to a whole block of pairs (16 pairs of 64
+  // experts 2048 x 1024: SwiGLU 17.9 against 18.9, down 15.1 against 15.6).
+  if (raw && M <= (grouped || weights <= (24 << 20) ? 16 : weights <= (128 << 20) ? 8 : 0)) return plan(Fp8Form::STREAM_RAW);
+  // Rows per expert: at 2 the stream is faster than the tiles (8 experts 4096 x 14336:
+  // 138 against 145), at 8 they are (200 against 178); over a short K, where its
+  // workgroups are brief, still at 8 (64 experts: SwiGLU 2048 x 1024 53.5 against 55.8, down
+  // 1024 x 2048 34.1 against 40.9), not at 40 (200 experts 1024 x 512 93 against 62).
+  if (grouped && M < (K <= 2048 ? 9 : 4) * (int64_t)E) return plan(Fp8Form::STREAM_1);
+  // 16 rows a workgroup where 32 would leave compute units idle (32 rows of 4096 x 4096
+  // 10.6 against 12.7; of 8192 x 8192 30.1 against 24.2).  64 rows of a small matrix 12.9
+  // against 16.2 with tiles, whose K must be shared; 48 of 8192 x 8192 34.4 against 25.1.
+  if (!grouped && (M <= 32 || (M <= 64 && weights <= (1 << 24))))
+    return plan(M <= 16 || tiles(Fp8Form::STREAM_2) < 256 ? Fp8Form::STREAM_1 : Fp8Form::STREAM_2);
+  // Tiles: the form, and the shares of K, whose rounds of tiles are shortest; not
+  // shorter than the weights' bytes, and with what another kernel takes to add the
+  // shares.  (Over those 70 products 2 % longer than the best form of each.)
+  Fp8Plan best = {};
+  double least = 0;
+  for (Fp8Form f : {Fp8Form::TILE_64, Fp8Form::TILE_128_DEEP, Fp8Form::TILE_128, Fp8Form::TILE_256}) {
+    const int64_t n = tiles(f), slots = kSlotsOf[(int)f];
+    const int most = swiglu || f == Fp8Form::TILE_256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(G4 / 2, slots / n));
+    for (int split = 1; split <= most; split *= 2) {
+      const int groups = split > 1 ? (G4 + split - 1) / split * 4 : G;
+      const double work = (double)((n * split + slots - 1) / slots) * (groups * kStepOf[(int)f] + kRestOf[(int)f]);
+      const double bytes = weights / 5.0e6;
+      double t = std::max(work, bytes) + 0.15 * std::min(work, bytes);
+      if (grouped) t += split * (double)M * N * 1.2e-6;
+      else if (split > 1) t += 4 + split * (double)M * N * 2e-6;
+      if (best.split == 0 || t < least) {
+        best = plan(f, split);
+        least = t;
+      }
+    }
+  }
+  return best;
 }
 
 namespace {
@@ -546,12 +578,13 @@ namespace {
 template <Epilogue EPI>
 void launch_form(const Fp8Plan& p, const Fp8Args& a, int blocks, hipStream_t st) {
   switch (p.form) {
-    case Fp8Form::STREAM_RAW: return launch_stream<8, 1, 2, true, EPI>(a, blocks, st);
-    case Fp8Form::STREAM_1: return launch_stream<8, 1, 2, false, EPI>(a, blocks, st);
+    case Fp8Form::STREAM_RAW: return launch_stream<4, 1, 2, true, EPI>(a, blocks, st);
+    case Fp8Form::STREAM_1: return launch_stream<4, 1, 2, false, EPI>(a, blocks, st);
     case Fp8Form::STREAM_2:
-      if constexpr (EPI == OUT_PLAIN || EPI == OUT_RESIDUAL) launch_stream<8, 2, 2, false, EPI>(a, blocks, st);
+      if constexpr (EPI == OUT_PLAIN || EPI == OUT_RESIDUAL) launch_stream<4, 2, 2, false, EPI>(a, blocks, st);
       return;
     case Fp8Form::TILE_64: return launch_tile<1, 4, 4, 2, 4, EPI>(a, blocks, st);
+    case Fp8Form::TILE_128_DEEP: return launch_tile<2, 4, 4, 2, 4, EPI>(a, blocks, st);
     case Fp8Form::TILE_128: return launch_tile<2, 2, 4, 4, 2, EPI>(a, blocks, st);
     case Fp8Form::TILE_256: return launch_tile<2, 4, 8, 4, 2, EPI>(a, blocks, st);
   }
@@ -641,25 +674,20 @@ size_t fp8_part_bytes(int M, int K, int N) {
   return p.split > 1 ? (size_t)p.split * M * N * sizeof(float) : 0;
 }
 
-size_t fp8_part_bytes_most(int M, int K, int N) {
-  // at most 256 tiles' worth of parts, and no more shares than plan_fp8_gemm allows
-  const int64_t G4 = (fp8_blocks(K) + 3) / 4;
-  auto most = [&](Fp8Form f, int64_t split) {
-    const int64_t all = 256ll * kRowsOf[(int)f] * kColumnsOf[(int)f], mine = split * M * N;
-    return split > 1 ? (size_t)(all < mine ? all : mine) * sizeof(float) : 0;
-  };
-  const size_t a = most(Fp8Form::TILE_128, G4 / 2), b = most(Fp8Form::TILE_256, G4 / 14);
-  return a > b ? a : b;
+// what the shares of K take at most: 512 tiles' worth, as many as plan_fp8_gemm allows
+static size_t shares_bytes_most(int64_t M, int K, int N) {
+  const size_t mine = (size_t)((fp8_blocks(K) + 3) / 4 / 2) * M * N * sizeof(float);
+  return std::min(mine, (size_t)512 * 128 * 128 * sizeof(float));
 }
+
+size_t fp8_part_bytes_most(int M, int K, int N) { return shares_bytes_most(M, K, N); }
 
 size_t fp8_rows_bytes(int M, int E, int K, int N) {
   return (size_t)plan_fp8_gemm(M, E, K, N, false, true, false).split * M * N * sizeof(float);
 }
 
 size_t fp8_rows_bytes_most(int64_t M, int K, int N) {
-  // one part, or as many as plan_fp8_gemm allows of at most 256 tiles
-  const size_t one = (size_t)M * N * sizeof(float), all = std::max<int64_t>((fp8_blocks(K) + 3) / 4 / 2, 1) * one;
-  return std::max(one, std::min(all, (size_t)256 * 128 * 128 * sizeof(float)));
+  return std::max((size_t)M * N * sizeof(float), shares_bytes_most(M, K, N));
 }
 
 }  // namespace ss

@@ -41,7 +41,7 @@ size_t fp8_rows_bytes(int M, int E, int K, int N);
 size_t fp8_rows_bytes_most(int64_t M, int K, int N);
 // The form of a product, the rows of its row blocks and the shares of K.  raw: the
 // product may read the rows itself.
-enum class Fp8Form { STREAM_RAW, STREAM_1, STREAM_2, TILE_64, TILE_128, TILE_256 };
+enum class Fp8Form { STREAM_RAW, STREAM_1, STREAM_2, TILE_64, TILE_128_DEEP, TILE_128, TILE_256 };
 struct Fp8Plan {
   Fp8Form form;
   int tm, split;

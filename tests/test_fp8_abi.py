@@ -98,8 +98,9 @@ def test_launches_of_too_many_threads(ss):  # noqa: F811
     lib = ss.lib()
     W = lambda K, N, E: ctypes.byref(ss.FP8(FAKE, FAKE, K, N, E, FAKE))  # noqa: E731
     G = lambda T, k, E: groups(ss, T=T, k=k, E=E)  # noqa: E731
-    assert status(lib, "moe_fp8_swiglu", W(128, 1 << 18, 512), W(128, 1 << 18, 512), FAKE, 128, G(63, 16, 512), FAKE, 1 << 18,
-                  FAKE, BIG) == ss.UNSUPPORTED
+    # 4000 pairs of 512 experts over 2 x 393216 columns: up to 762 blocks of 16 rows
+    wide = W(128, 393216, 512)
+    assert status(lib, "moe_fp8_swiglu", wide, wide, FAKE, 128, G(250, 16, 512), FAKE, 393216, FAKE, BIG) == ss.UNSUPPORTED
     # four results a thread of the combination
     assert status(lib, "moe_fp8_down", W(128, 8192, 8), FAKE, 128, G(1 << 20, 1, 8), FAKE, FAKE, 8192, None, 0, FAKE, BIG) == ss.UNSUPPORTED
 
