@@ -65,6 +65,11 @@ struct Fp8Args : ProductArgs {
 // each tile at a time and the next U on their way.
 // RAW: a single launch for very few rows, which each wave quantises itself as it
 // reads them; the block's expert is found from the offsets.
+// Bound by launch, first loads and drain for small matrices (1 row of 2048 x 2048 4.6
+// us, SwiGLU of a token through 8 experts 2048 x 1024, 34 MB, 8.2 us in one launch), then
+// by the weights' bytes: 32 rows of 8192 x 8192 (67 MB) 18.5 us, 3.6 TB/s.  Four waves, not
+// eight, leave more workgroups to a compute unit (SwiGLU of a token 10.5 against 12.8,
+// 32 rows of 8192 x 8192 24.3 against 25.8); three stages of registers changed nothing.
 template <int W, int MT, int NT, int U, bool RAW, Epilogue EPI>
 __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
   constexpr bool SW = EPI == OUT_SWIGLU;
@@ -248,12 +253,25 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
 // A step multiplies one group: the weights' blocks of the wave stay in registers, the
 // rows' blocks follow one another, the next on its way from LDS.  Each instruction's
 // result is multiplied and added three instructions later, so that its latency does not
-// show (two later: 8192 x 8192 x 8192 474 against 462 us).  Before the last block of rows the wave has read all it needs of this stage: it
-// waits for its loads of the next one and for the other waves, and reads the first
-// operands of the next step while the last block is multiplied; the stage's place is
-// loaded anew during the next step.  One barrier a step.
+// show (two later: 8192 x 8192 x 8192 474 against 462 us).  Before the last block of rows
+// the wave has read all it needs of this stage: it waits for its loads of the next one
+// and for the other waves, and reads the first operands of the next step while the last
+// block is multiplied; the stage's place is loaded anew during the next step.  One
+// barrier a step.
 // A wave's columns lie in one block of 128, so that the matrix's scale is uniform: 64
 // groups of them are one load, a lane each.
+// The sums are in ordinary registers, as the multiply-adds need them: 64 x 128 of them
+// are what a wave of two on a SIMD has room for, and 256 x 256 of a workgroup read each
+// byte of LDS 0.75 times for an instruction.
+// With few rows an expert it is bound by the weights: SwiGLU of 32 tokens through 8
+// experts 4096 x 14336 (940 MB) 155-163 us, 5.8-6.1 TB/s, by tiles of 64 rows with four
+// stages.  With many by power and by LDS together: 8192 x 8192 x 8192 462 us (2.4
+// PFLOP/s; the instruction with its multiply-adds on random operands in registers
+// reaches 4.2, this kernel on zeros 2.9), 4001 rows of 4096 x 14336 219 us in four rounds
+// of tiles (2.1), matrix instructions in 54 % of its cycles, at 1.92 of 2.4 GHz.
+// Without the LDS reads (on the same operands again and again) 8192 would take 356,
+// without the loads 429, without both 293.  Pairs of blocks through the 32 x 32 x 64 form,
+// which reads each register half as often, were 4 % slower (485 against 465).
 constexpr int kTurnPad = 16;  // bytes behind a row of results on its way through LDS
 
 template <int WM, int WN, int MTW, int NTW, int ST, Epilogue EPI>
