@@ -546,10 +546,11 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
   const int64_t columns = (int64_t)N * (swiglu ? 2 : 1), reached = std::min(E, M);
   const int64_t weights = reached * K * columns;  // bytes that are read, at most
   auto plan = [](Fp8Form f, int split = 1) { return Fp8Plan{f, kRowsOf[(int)f], split}; };
-  // of experts, whose last block of rows is half full
+  // of experts, whose last block of rows is half full or, by chance, one more (256 pairs
+  // of 8 experts 4096 x 14336 have 9 blocks of 64 rows: down 137 us, of 128 rows 109)
   auto tiles = [&](Fp8Form f) {
     const int64_t rows = kRowsOf[(int)f], blocks = (M + rows - 1) / rows;
-    return (grouped ? std::max(reached, blocks + reached / 2) : blocks) * ((columns + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]);
+    return (grouped ? std::max(reached, blocks + reached * 5 / 8) : blocks) * ((columns + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]);
   };
   // One launch, but every wave quantises the rows that it multiplies: 8 rows of 8192 x
   // 8192 21.2 against 21.7, 1 row of 2048 x 2048 5.8 against 8.2; 5 rows of 28672 x 8192
