@@ -537,7 +537,7 @@ int swiftspec_fp8_prepack(const swiftspec_fp8* W, void* packed, size_t packed_by
  * a: s is the least power of two with a <= 448 s, every value goes to the nearest
  * code of v / s, ties to the even code; a = 0: s = 1.  A block that holds an
  * infinity or a NaN gets s = NaN and codes 0: it stands for NaN.  K % 16 == 0;
- * M K, K rounded up to 128, < 2^35 (also of dequantize). */
+ * K, rounded up to 128, < 2^31, and M such rows < 2^35 values (also of dequantize). */
 int swiftspec_fp8_quantize(const uint16_t* x, int64_t M, int32_t K, int64_t ldx, int32_t block_rows, uint8_t* codes,
                            float* scales, void* stream);
 /* y [M][ldy] fp16 (16-byte aligned, ldy % 8 == 0): code times scale, rounded once,

@@ -384,12 +384,14 @@ int check_prepack(const Format& f, const W* w, void* packed, size_t bytes) {
   return bytes < f.packed_bytes(w->K, w->N, w->E) ? SWIFTSPEC_WORKSPACE_TOO_SMALL : SWIFTSPEC_OK;
 }
 
-// rows of K columns, rounded up to `unit`: below 2^35 values, 16 of which a thread
-// takes: a launch has fewer than 2^32 threads
+// rows of K columns, rounded up to `unit`: below 2^31 a row, whose columns the kernels
+// count in 32 bits, and below 2^35 values.  A thread takes 16 of them, in blocks of 128
+// rows 64, or half a value where only one row is there: a launch has fewer than 2^32
+// threads.
 int check_quantized_rows(int64_t M, int32_t K, int64_t ld, int k_step, int unit) {
   if (M < 0 || K <= 0 || ld < K) return SWIFTSPEC_INVALID_ARG;
   const int64_t columns = ((int64_t)K + unit - 1) / unit * unit;
-  if (K % k_step || M > (((int64_t)1 << 35) - 1) / columns) return SWIFTSPEC_UNSUPPORTED;
+  if (K % k_step || columns >= (int64_t)1 << 31 || M > (((int64_t)1 << 35) - 1) / columns) return SWIFTSPEC_UNSUPPORTED;
   return SWIFTSPEC_OK;
 }
 

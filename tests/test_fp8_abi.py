@@ -47,6 +47,8 @@ def test_matrix_refusals(ss):  # noqa: F811
     for f in (quant, back):
         assert f(x=None) == f(c=None) == f(s=None) == f(M=-1) == f(K=0) == f(ld=32) == f(b=0) == f(b=64) == ss.INVALID_ARG
         assert f(K=40) == f(M=1 << 50) == f(M=(1 << 35) // 128) == ss.UNSUPPORTED
+        for b in (1, 128):  # 2^31 columns and more, rounded up to whole blocks
+            assert f(M=1, K=(1 << 31) - 16, ld=1 << 31, b=b) == f(M=1, K=(1 << 31) - 112, ld=1 << 31, b=b) == ss.UNSUPPORTED
         assert f(x=FAKE + 2) == f(ld=68) == f(c=FAKE + 4) == f(s=FAKE + 2) == ss.MISALIGNED
         assert f(M=0) == f(M=0, b=128) == ss.OK
 

@@ -228,6 +228,23 @@ def test_gemm_uses_the_callers_stream():
     check(y, *ref.gemm(v, w))
 
 
+@pytest.mark.parametrize("rows", [1, 128])
+def test_the_longest_row(rows):
+    """A row of 2^31 - 128 columns, the most."""
+    K = 2**31 - 128
+    x = torch.zeros(1, K, dtype=torch.float16, device=dev())
+    codes, scales = torch.empty(1, K, dtype=torch.uint8, device=dev()), torch.empty(1, 2**24 - 1, device=dev())
+    for at, v in ((0, 3.0), (2**30 + 5, 500.0), (K - 1, -900.0)):
+        x[0, at] = v
+    ss.fp8_quantize(x, codes, scales, rows=rows)
+    assert [scales[0, i].item() for i in (0, 1, 2**23, 2**24 - 3, 2**24 - 2)] == [2.0**-7, 1.0, 2.0, 1.0, 4.0]
+    assert torch.count_nonzero(codes).item() == 3 and torch.count_nonzero(scales == 1).item() == 2**24 - 4
+    y = torch.empty_like(x)
+    ss.fp8_dequantize(codes, scales, y, rows=rows)
+    assert [y[0, at].item() for at in (0, 2**30 + 5, K - 1)] == [3.0, 512.0, -896.0]
+    assert torch.count_nonzero(y).item() == 3
+
+
 def test_refusals_of_the_binding():
     rng = np.random.default_rng(1)
     W, keep, w = matrix(rng, 64, 128)
