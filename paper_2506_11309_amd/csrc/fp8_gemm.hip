@@ -567,9 +567,10 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
   // 10.6 against 12.7; of 8192 x 8192 30.1 against 24.2).  64 rows of a small matrix 12.9
   // against 16.2 with tiles, whose K must be shared; 48 of 8192 x 8192 34.4 against 25.1.
   // Every workgroup of a stream reads all rows, for few columns: 32 of a large matrix
-  // are faster in tiles (8192 x 14336, 117 MB, 38.0 against 33.3; 28672 x 8192 60.0
-  // against 51.7), 16 are not (54.1 against 55.2).
-  if (!grouped && (M <= 16 || (M <= 32 && weights <= (96 << 20)) || (M <= 64 && weights <= (1 << 24))))
+  // are faster in tiles (6144 x 6144, 38 MB, 17.4 against 17.5; 14336 x 4096, 59 MB, 23.7
+  // against 21.2; 8192 x 8192 24.5 against 22.9; 28672 x 8192 60.0 against 51.7), 16 are
+  // not (54.1 against 55.2).
+  if (!grouped && (M <= 16 || (M <= 32 && weights <= (48 << 20)) || (M <= 64 && weights <= (1 << 24))))
     return plan(M <= 16 || tiles(Fp8Form::STREAM_2) < 256 ? Fp8Form::STREAM_1 : Fp8Form::STREAM_2);
   // Tiles: the form, and the shares of K, whose rounds of tiles are shortest; not
   // shorter than the weights' bytes, and with what another kernel takes to add the

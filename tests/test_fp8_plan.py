@@ -73,7 +73,7 @@ def test_forms_of_one_matrix_and_of_experts(plan):
 # Both sides of the plan's lines.
 @pytest.mark.parametrize("M,K,N,form,split", [
     (8, 8192, 8192, "raw", 1), (9, 8192, 8192, "stream", 1), (8, 8192, 28672, "stream", 1), (16, 4096, 4096, "raw", 1), (16, 4096, 14336, "stream", 1),
-    (17, 4096, 4096, "stream", 1), (32, 8192, 8192, "stream 32", 1), (16, 28672, 8192, "stream", 1),
+    (17, 4096, 4096, "stream", 1), (32, 6144, 8192, "stream 32", 1), (32, 8192, 8192, "tile 64", 4), (16, 28672, 8192, "stream", 1),
     (32, 28672, 8192, "tile 64", 4), (32, 8192, 14336, "tile 64", 2), (64, 4096, 4096, "stream 32", 1), (65, 4096, 4096, "tile 64", 4),
     (64, 8192, 8192, "tile 64", 4), (256, 8192, 8192, "tile 64", 1), (512, 8192, 8192, "tile 128 deep", 1), (1024, 4096, 4096, "tile 128 deep", 1),
     (1500, 4096, 4096, "tile 128", 1), (1024, 8192, 8192, "tile 128", 1), (2048, 8192, 8192, "tile 256", 1), (4001, 4096, 14336, "tile 256", 1)])

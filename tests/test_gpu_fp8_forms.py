@@ -39,7 +39,7 @@ class Matrix:
 
 
 # M, K, N, form, shares of K
-GEMM = [(1, 8464, 144, "raw", 1), (1, 544, 144, "raw", 1), (18, 9248, 144, "stream", 1), (17, 8608, 8752, "stream 32", 1), (37, 544, 4240, "stream 32", 1),
+GEMM = [(1, 8464, 144, "raw", 1), (1, 544, 144, "raw", 1), (18, 9248, 144, "stream", 1), (17, 5408, 8752, "stream 32", 1), (37, 544, 4240, "stream 32", 1),
         (70, 528, 144, "tile 64", 1), (74, 8912, 144, "tile 64", 8), (131, 8640, 8384, "tile 64", 1), (137, 528, 11488, "tile 128 deep", 1),
         (137, 9360, 11168, "tile 128 deep", 1), (1193, 8656, 144, "tile 128 deep", 8), (1169, 528, 3392, "tile 128", 1), (2112, 8496, 2000, "tile 128", 1),
         (1292, 528, 6160, "tile 256", 1), (1309, 8496, 6160, "tile 256", 1)]
