@@ -552,25 +552,33 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
     const int64_t rows = kRowsOf[(int)f], blocks = (M + rows - 1) / rows;
     return (grouped ? std::max(reached, blocks + reached * 5 / 8) : blocks) * ((columns + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]);
   };
-  // One launch, but every wave quantises the rows that it multiplies: 8 rows of 8192 x
-  // 8192 21.2 against 21.7, 1 row of 2048 x 2048 5.8 against 8.2; 5 rows of 28672 x 8192
-  // (235 MB) 54.4 against 52.4; 16 rows of 4096 x 4096 10.2 against 10.7, of 4096 x 14336
-  // (59 MB) 19.9 against 18.6.  Of experts up to a whole block of pairs (16 pairs of 64
-  // experts 2048 x 1024: SwiGLU 17.9 against 18.9, down 15.1 against 15.6).
-  if (raw && M <= (grouped || weights <= (24 << 20) ? 16 : weights <= (128 << 20) ? 8 : 0)) return plan(Fp8Form::STREAM_RAW);
+  // One launch, but every wave quantises the rows that it multiplies, all the more of them
+  // the longer K is (1 row of 2048 x 2048 5.8 against 8.2, of 5120 x 5120 10.7 against 11.0,
+  // of 6144 x 4096 11.7 against 11.2, of 8192 x 4096 15.4 against 14.4; a token of 8 experts
+  // 2 wide 4096 x 2048 down 13.9 against 15.3, 8192 x 2048 18.6 against 17.1); 16 rows of 4096 x
+  // 4096 10.2 against 10.7, of 4096 x 14336 (59 MB) 19.9 against 18.6.  Of experts up to a
+  // whole block of pairs (16 pairs of 64 experts 2048 x 1024: SwiGLU 17.9 against 18.9, down
+  // 15.1 against 15.6).
+  if (raw && K <= 5120 && M <= (grouped || weights <= (24 << 20) ? 16 : weights <= (128 << 20) ? 8 : 0)) return plan(Fp8Form::STREAM_RAW);
   // Rows per expert: at 2 the stream is faster than the tiles (8 experts 4096 x 14336:
   // 138 against 145), at 8 they are (200 against 178); over a short K, where its
   // workgroups are brief, still at 8 (64 experts: SwiGLU 2048 x 1024 53.5 against 55.8, down
   // 1024 x 2048 34.1 against 40.9), not at 40 (200 experts 1024 x 512 93 against 62).
   if (grouped && M < (K <= 2048 ? 9 : 4) * (int64_t)E) return plan(Fp8Form::STREAM_1);
   // 16 rows a workgroup where 32 would leave compute units idle (32 rows of 4096 x 4096
-  // 10.6 against 12.7; of 8192 x 8192 30.1 against 24.2).  64 rows of a small matrix 12.9
+  // 10.6 against 12.7; of 4096 x 14336 24.5 against 21.9).  64 rows of a small matrix 12.9
   // against 16.2 with tiles, whose K must be shared; 48 of 8192 x 8192 34.4 against 25.1.
   // Every workgroup of a stream reads all rows, for few columns: 32 of a large matrix
-  // are faster in tiles (6144 x 6144, 38 MB, 17.4 against 17.5; 14336 x 4096, 59 MB, 23.7
-  // against 21.2; 8192 x 8192 24.5 against 22.9; 28672 x 8192 60.0 against 51.7), 16 are
-  // not (54.1 against 55.2).
-  if (!grouped && (M <= 16 || (M <= 32 && weights <= (48 << 20)) || (M <= 64 && weights <= (1 << 24))))
+  // are faster in tiles (6144 x 8192, 50 MB, 18.7 against 19.4; 8192 x 8192 24.5 against
+  // 22.9; 28672 x 8192 60.0 against 51.7), 16 are not (54.1 against 55.2).
+  // A stream's four waves take all of K.  Long ones of few columns are faster in shares,
+  // which only tiles have (1 and 16 rows: 28672 x 4096 32.7 and 39.3 against 28.9 and 31.4,
+  // 16384 x 1024 18.5 and 22.6 against 13.1 and 13.9; 4 of 10240 x 4096 17.8 against 17.4; 1 of
+  // 8192 x 1024 9.8 against 12.4, 16 of 8192 x 4096 17.0 against 15.3, of 6144 x 4096 13.3
+  // against 15.7; of more columns, 12288 x 6144, 20.8 and 25.1 against 23.3 and 25.6, but 32
+  // rows 33.7 against 26.8).
+  const bool shares = K >= (M > 8 ? 8192 : 10240) && (M > 16 || N <= 4096);
+  if (!grouped && !shares && (M <= 16 || (M <= 32 && weights <= (48 << 20)) || (M <= 64 && weights <= (1 << 24))))
     return plan(M <= 16 || tiles(Fp8Form::STREAM_2) < 256 ? Fp8Form::STREAM_1 : Fp8Form::STREAM_2);
   // Tiles: the form, and the shares of K, whose rounds of tiles are shortest; not
   // shorter than the weights' bytes, and with what another kernel takes to add the

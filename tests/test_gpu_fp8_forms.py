@@ -39,7 +39,8 @@ class Matrix:
 
 
 # M, K, N, form, shares of K
-GEMM = [(1, 8464, 144, "raw", 1), (1, 544, 144, "raw", 1), (18, 9248, 144, "stream", 1), (17, 5408, 8752, "stream 32", 1), (37, 544, 4240, "stream 32", 1),
+GEMM = [(1, 5104, 144, "raw", 1), (1, 544, 144, "raw", 1), (1, 10384, 144, "tile 64", 8), (14, 9248, 4240, "stream", 1),
+        (18, 9248, 144, "tile 64", 8), (17, 5408, 8752, "stream 32", 1), (37, 544, 4240, "stream 32", 1),
         (70, 528, 144, "tile 64", 1), (74, 8912, 144, "tile 64", 8), (131, 8640, 8384, "tile 64", 1), (137, 528, 11488, "tile 128 deep", 1),
         (137, 9360, 11168, "tile 128 deep", 1), (1193, 8656, 144, "tile 128 deep", 8), (1169, 528, 3392, "tile 128", 1), (2112, 8496, 2000, "tile 128", 1),
         (1292, 528, 6160, "tile 256", 1), (1309, 8496, 6160, "tile 256", 1)]
@@ -62,7 +63,8 @@ def test_gemm_forms(M, K, N, form, split, residual):
 
 
 # T, E, k, K, N, kind, form
-SWIGLU = [(1, 2, 2, 8464, 144, "random", "raw"), (7, 8, 2, 560, 144, "padded", "raw"), (9, 6, 2, 9232, 144, "padded", "stream"), (20, 2, 1, 9040, 144, "random", "tile 64"),
+SWIGLU = [(1, 2, 2, 5104, 144, "random", "raw"), (1, 2, 2, 8464, 144, "random", "stream"),
+          (7, 8, 2, 560, 144, "padded", "raw"), (9, 6, 2, 9232, 144, "padded", "stream"), (20, 2, 1, 9040, 144, "random", "tile 64"),
           (90, 4, 2, 528, 3536, "twice", "tile 128 deep"), (33, 2, 2, 10064, 5488, "random", "tile 128 deep"), (36, 2, 2, 576, 10896, "random", "tile 128"),
           (33, 2, 2, 9744, 11376, "padded", "tile 128"), (455, 12, 2, 544, 2640, "random", "tile 256"), (147, 3, 2, 9120, 8720, "random", "tile 256"),
           # h of more than 32 MiB, whose stores go past the caches
@@ -90,7 +92,8 @@ def test_swiglu_forms(T, E, k, K, N, kind, form):
 
 
 # T, E, k, K, N, kind, form, shares of K
-DOWN = [(1, 2, 2, 8464, 160, "random", "raw", 1), (1, 16, 8, 1056, 528, "random", "raw", 1), (10, 9, 2, 8592, 144, "padded", "stream", 1),
+DOWN = [(1, 2, 2, 5104, 160, "random", "raw", 1), (1, 2, 2, 8464, 160, "random", "stream", 1),
+        (1, 16, 8, 1056, 528, "random", "raw", 1), (10, 9, 2, 8592, 144, "padded", "stream", 1),
         (56, 13, 1, 9888, 1184, "random", "tile 64", 1), (25, 1, 1, 9200, 144, "padded", "tile 64", 8), (43, 2, 2, 672, 11200, "padded", "tile 128 deep", 1),
         (35, 2, 2, 1712, 5616, "random", "tile 128 deep", 2), (502, 13, 2, 8496, 144, "padded", "tile 128 deep", 8),
         (1080, 47, 2, 544, 1136, "twice", "tile 128", 1), (749, 51, 4, 9440, 144, "random", "tile 128", 4), (601, 9, 2, 528, 4624, "padded", "tile 256", 1),
