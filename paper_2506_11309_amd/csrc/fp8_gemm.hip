@@ -67,9 +67,10 @@ struct Fp8Args : ProductArgs {
 // reads them; the block's expert is found from the offsets.
 // Bound by launch, first loads and drain for small matrices (1 row of 2048 x 2048 4.6
 // us, SwiGLU of a token through 8 experts 2048 x 1024, 34 MB, 8.2 us in one launch), then
-// by the weights' bytes: 32 rows of 8192 x 8192 (67 MB) 18.5 us, 3.6 TB/s.  Four waves, not
-// eight, leave more workgroups to a compute unit (SwiGLU of a token 10.5 against 12.8,
-// 32 rows of 8192 x 8192 24.3 against 25.8); three stages of registers changed nothing.
+// by the weights' bytes: with their quantisation 16 rows of 4096 x 14336 (59 MB) 18.5 us, 1
+// row of 28672 x 8192 (235 MB) 48.5 us, 4.8 TB/s.  Four waves, not eight, leave more
+// workgroups to a compute unit (SwiGLU of a token 10.5 against 12.8, 32 rows of 8192 x
+// 8192 24.3 against 25.8); three stages of registers changed nothing.
 template <int W, int MT, int NT, int U, bool RAW, Epilogue EPI>
 __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
   constexpr bool SW = EPI == OUT_SWIGLU;
@@ -548,10 +549,11 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
   auto plan = [](Fp8Form f, int split = 1) { return Fp8Plan{f, kRowsOf[(int)f], split}; };
   // of experts, whose last block of rows is half full or, by chance, one more (256 pairs
   // of 8 experts 4096 x 14336 have 9 blocks of 64 rows: down 137 us, of 128 rows 109)
-  auto tiles = [&](Fp8Form f) {
+  auto row_blocks = [&](Fp8Form f) {
     const int64_t rows = kRowsOf[(int)f], blocks = (M + rows - 1) / rows;
-    return (grouped ? std::max(reached, blocks + reached * 5 / 8) : blocks) * ((columns + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]);
+    return grouped ? std::max(reached, blocks + reached * 5 / 8) : blocks;
   };
+  auto tiles = [&](Fp8Form f) { return row_blocks(f) * ((columns + kColumnsOf[(int)f] - 1) / kColumnsOf[(int)f]); };
   // One launch, but every wave quantises the rows that it multiplies, all the more of them
   // the longer K is (1 row of 2048 x 2048 5.8 against 8.2, of 5120 x 5120 10.7 against 11.0,
   // of 6144 x 4096 11.7 against 11.2, of 8192 x 4096 15.4 against 14.4; a token of 8 experts
@@ -591,7 +593,10 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
     for (int split = 1; split <= most; split *= 2) {
       const int groups = split > 1 ? (G4 + split - 1) / split * 4 : G;
       const double work = (double)((n * split + slots - 1) / slots) * (groups * kStepOf[(int)f] + kRestOf[(int)f]);
-      const double bytes = weights / 5.0e6;
+      // several blocks of rows of an expert read its weights at different times (SwiGLU of
+      // those 256 pairs: blocks of 64 rows 214 us, of 128 rows 180)
+      const double again = grouped ? std::min(1.15, (double)row_blocks(f) / reached) : 1.0;
+      const double bytes = again * weights / 5.0e6;
       double t = std::max(work, bytes) + 0.15 * std::min(work, bytes);
       if (grouped) t += split * (double)M * N * 1.2e-6;
       else if (split > 1) t += 4 + split * (double)M * N * 2e-6;

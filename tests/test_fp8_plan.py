@@ -87,7 +87,7 @@ def test_lines_of_one_matrix(plan, M, K, N, form, split):
     (16, 8, 4096, 14336, True, "raw"), (17, 8, 4096, 14336, True, "stream"), (31, 8, 4096, 14336, True, "stream"), (32, 8, 4096, 14336, True, "tile 64"),
     (9 * 64 - 1, 64, 2048, 1024, True, "stream"), (9 * 64, 64, 2048, 1024, True, "tile 64"), (64 * 128, 64, 2048, 1024, True, "tile 128"),
     (64 * 1024, 64, 2048, 1024, True, "tile 256"), (1400, 8, 4096, 14336, True, "tile 128"),
-    (2048, 8, 4096, 14336, True, "tile 256"), (600, 5, 4096, 1024, True, "tile 64")])
+    (192, 8, 4096, 14336, True, "tile 64"), (256, 8, 4096, 14336, True, "tile 128"), (2048, 8, 4096, 14336, True, "tile 256"), (600, 5, 4096, 1024, True, "tile 64")])
 def test_lines_of_experts(plan, M, E, K, N, swiglu, form):
     assert plan(M, E, K, N, swiglu, True) == (form, 1)
 
