@@ -586,6 +586,7 @@ class DraftTree:
 _cuda = None  # (handle of a device's current stream, current device)
 _half = None  # torch.float16
 _single = None  # torch.float32
+_e4m3 = None  # the types of e4m3 codes
 _TOP = 2**31 - 1  # the largest number that the library takes for a size
 
 
@@ -750,14 +751,24 @@ def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
     _gemm("mx4_gemm", W, x, y, ws, residual, stream)
 
 
+def _e4m3_codes(where, codes):
+    """Refuse codes of a type that stands for other values than e4m3."""
+    global _e4m3
+    if _e4m3 is None:
+        import torch
+        _e4m3 = frozenset((torch.uint8, torch.int8, torch.float8_e4m3fn))
+    if codes.dtype not in _e4m3:
+        raise SwiftSpecError(INVALID_ARG, where)
+
+
 def make_fp8(codes, scales, packed=None) -> FP8:
-    """Describe an 8-bit matrix held in device tensors codes [N][K] (e4m3: uint8 or
-    torch.float8_e4m3fn) and scales [ceil(N/128)][ceil(K/128)] float32, or E of them
-    (codes [E][N][K], scales [E][...][...]), and optionally its kernel-native copy
-    `packed` (see prepack_fp8), all of it: fp8_packed_bytes contiguous bytes."""
+    """Describe an 8-bit matrix held in device tensors codes [N][K] (e4m3: bytes,
+    signed or not, or torch.float8_e4m3fn) and scales [ceil(N/128)][ceil(K/128)]
+    float32, or E of them (codes [E][N][K], scales [E][...][...]), and optionally its
+    kernel-native copy `packed` (see prepack_fp8), all of it: fp8_packed_bytes
+    contiguous bytes."""
     _codes("make_fp8", codes)
-    if codes.dtype.is_floating_point and "e4m3fn" not in str(codes.dtype).split("_"):
-        raise SwiftSpecError(INVALID_ARG, "make_fp8")
+    _e4m3_codes("make_fp8", codes)
     _dense(scales, "make_fp8", (*codes.shape[:-2], -(-codes.shape[-2] // 128), -(-codes.shape[-1] // 128)), 4, real=True)
     return _matrix(FP8, "make_fp8", codes, scales, codes.shape[-1], packed)
 
@@ -777,12 +788,13 @@ def _fp8_convert(where, values, codes, scales, rows, stream):
     if rows not in (1, 128):
         raise SwiftSpecError(INVALID_ARG, where)
     _dense(codes, where, (M, K), 1)
+    _e4m3_codes(where, codes)
     _dense(scales, where, (-(-M // rows), -(-K // 128)), 4, real=True)
     return M, K, ld, _same_device(where, None, values, codes, scales)
 
 
 def fp8_quantize(x, codes, scales, rows=1, stream=None):
-    """x [M][K] fp16 (rows contiguous) -> codes [M][K] (e4m3 in bytes), scales
+    """x [M][K] fp16 (rows contiguous) -> codes [M][K] (e4m3, as make_fp8), scales
     [ceil(M/rows)][ceil(K/128)] float32 of blocks of `rows` (1 or 128) rows and 128
     columns."""
     M, K, ld, dev = _fp8_convert("fp8_quantize", x, codes, scales, rows, stream)
