@@ -300,7 +300,7 @@ __device__ __forceinline__ void route_scored_token(const ScoredArgs& a, int t, i
   const double sum = a.renormalize ? row_sum((double)s) : 1.0;
   if (l < a.k && there) {
     a.experts[(int64_t)t * a.k + l] = mine;
-    a.weights[(int64_t)t * a.k + l] = sum > 0.0 ? (float)((double)s / sum * (double)a.scale) : 0.f;
+    a.weights[(int64_t)t * a.k + l] = mine >= 0 && sum > 0.0 ? (float)((double)s / sum * (double)a.scale) : 0.f;
     if (chosen) chosen[t * a.k + l] = (int16_t)mine;
     if (mine >= 0) atomicAdd(counts + mine, 1);
   }
