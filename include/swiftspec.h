@@ -598,7 +598,8 @@ int swiftspec_moe_route(const uint16_t* logits, int32_t ldl, int32_t renormalize
  *   c_e = s_e + bias[e] in fp32 (bias NULL: s_e);
  *   experts e with the same e / (E / groups) form a group, whose value is its
  *         largest c, or with group_best = 2 the sum (fp32) of its two largest (of
- *         a single one itself); the top_groups groups of largest value compete;
+ *         a single one itself); the top_groups groups of largest value compete,
+ *         those whose sum is -inf or whose experts are all masked last, by index;
  *   the k experts of largest c among them go to d_experts [T][k], in that order
  *         (equal values: lower index first, of groups as of experts);
  *   d_weights [T][k] (float) = scale * s_e, with renormalize != 0
