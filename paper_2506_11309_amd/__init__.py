@@ -49,11 +49,13 @@ class W4(ctypes.Structure):
 class MX4(ctypes.Structure):
     _fields_ = [("codes", vp), ("scales", vp), ("K", i32), ("N", i32), ("E", i32), ("packed", vp)]
     device = None  # index of the GPU that make_mx4 found the codes on
+    unpacked = ()  # codes and scales, until prepack_mx4 has read them
 
 
 class FP8(ctypes.Structure):
     _fields_ = [("codes", vp), ("scales", vp), ("K", i32), ("N", i32), ("E", i32), ("packed", vp)]
     device = None  # index of the GPU that make_fp8 found the codes on
+    unpacked = ()  # codes and scales, until prepack_fp8 has read them
 
 
 class _Scoring(ctypes.Structure):
@@ -672,6 +674,8 @@ def _matrix(kind, where, codes, scales, K, packed):
         raise SwiftSpecError(INVALID_ARG, where)
     W = kind(codes.data_ptr(), scales.data_ptr(), K, N, E, packed.data_ptr() if packed is not None else None)
     W.device = _same_device(where, None, codes, scales, packed)
+    if packed is None:
+        W.unpacked = codes, scales
     return W
 
 
@@ -684,7 +688,8 @@ def make_mx4(codes, scales, packed=None) -> MX4:
     """Describe an MXFP4 matrix held in device tensors codes [N][K/2] u8 and
     scales [N][K/32] u8, or E of them (codes [E][N][K/2], scales [E][N][K/32]),
     and optionally its kernel-native copy `packed` (see prepack_mx4), all of it:
-    mx4_packed_bytes contiguous bytes."""
+    mx4_packed_bytes contiguous bytes.  The matrix keeps codes and scales until
+    prepack_mx4 has read them; it does not keep `packed`."""
     _codes("make_mx4", codes)
     _dense(scales, "make_mx4", (*codes.shape[:-1], codes.shape[-1] // 16), 1)
     return _matrix(MX4, "make_mx4", codes, scales, 2 * codes.shape[-1], packed)
@@ -697,7 +702,12 @@ def mx4_packed_bytes(K: int, N: int, E: int = 1) -> int:
 def _prepack(where, W, size, device, stream):
     import torch
     t = torch.empty(size, dtype=torch.uint8, device=device)
-    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, W, t), ctypes.byref(W), t.data_ptr(), t.numel())
+    dev = _same_device(where, W, t)
+    _run(where, getattr(_load(), "swiftspec_" + where), stream, dev, ctypes.byref(W), t.data_ptr(), t.numel())
+    for source in W.unpacked:
+        if source.is_cuda:  # its memory is not given away before the launch has read it
+            source.record_stream(torch.cuda.current_stream(dev) if stream is None else torch.cuda.ExternalStream(stream.cuda_stream, device=dev))
+    W.unpacked = ()
     W.packed = t.data_ptr()
     return t
 
@@ -766,7 +776,8 @@ def make_fp8(codes, scales, packed=None) -> FP8:
     signed or not, or torch.float8_e4m3fn) and scales [ceil(N/128)][ceil(K/128)]
     float32, or E of them (codes [E][N][K], scales [E][...][...]), and optionally its
     kernel-native copy `packed` (see prepack_fp8), all of it: fp8_packed_bytes
-    contiguous bytes."""
+    contiguous bytes.  The matrix keeps codes and scales until prepack_fp8 has read
+    them; it does not keep `packed`."""
     _codes("make_fp8", codes)
     _e4m3_codes("make_fp8", codes)
     _dense(scales, "make_fp8", (*codes.shape[:-2], -(-codes.shape[-2] // 128), -(-codes.shape[-1] // 128)), 4, real=True)
