@@ -743,7 +743,7 @@ def mx4_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
     return _size("mx4_gemm_workspace_bytes", M, K, N)
 
 
-def _gemm(where, W, x, y, ws, residual, stream):
+def _gemm(where, fn, W, x, y, ws, residual, stream):
     M, ldx = _rows(x, where, W.K)
     m, ldy = _rows(y, where, W.N)
     r, ldr, res = M, 0, None
@@ -752,13 +752,13 @@ def _gemm(where, W, x, y, ws, residual, stream):
         res = residual.data_ptr()
     if m != M or r != M:
         raise SwiftSpecError(INVALID_ARG, where)
-    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, W, x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M,
-         ldx, y.data_ptr(), ldy, res, ldr, ws.data_ptr(), ws.numel() * ws.element_size())
+    _run(where, fn, stream, _same_device(where, W, x, y, ws, residual), ctypes.byref(W), x.data_ptr(), M, ldx, y.data_ptr(), ldy, res, ldr,
+         ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def mx4_gemm(W: MX4, x, y, ws, residual=None, stream=None):
     """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
-    _gemm("mx4_gemm", W, x, y, ws, residual, stream)
+    _gemm("mx4_gemm", _load().swiftspec_mx4_gemm, W, x, y, ws, residual, stream)
 
 
 def _e4m3_codes(where, codes):
@@ -824,7 +824,7 @@ def fp8_gemm_workspace_bytes(M: int, K: int, N: int) -> int:
 
 def fp8_gemm(W: FP8, x, y, ws, residual=None, stream=None):
     """y = fp16(Q(x) . W'^T + residual): x [M][K], y and residual [M][N] fp16."""
-    _gemm("fp8_gemm", W, x, y, ws, residual, stream)
+    _gemm("fp8_gemm", _load().swiftspec_fp8_gemm, W, x, y, ws, residual, stream)
 
 
 class MoeGroups:
@@ -920,16 +920,16 @@ def moe_mx4_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> in
     return _size("moe_mx4_swiglu_workspace_bytes", T, k, E, K, N)
 
 
-def _swiglu(where, Wg, Wu, x, groups, h, ws, stream):
+def _swiglu(where, fn, Wg, Wu, x, groups, h, ws, stream):
     T, ldx = _rows(x, where, Wg.K)
     P, ldh = _rows(h, where, Wg.N)
     if T != groups.T or P != groups.T * groups.k or Wu.device not in (None, Wg.device):
         raise SwiftSpecError(INVALID_ARG, where)
-    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, Wg, groups.offsets, x, h, ws), ctypes.byref(Wg),
-         ctypes.byref(Wu), x.data_ptr(), ldx, groups._ref(), h.data_ptr(), ldh, ws.data_ptr(), ws.numel() * ws.element_size())
+    _run(where, fn, stream, _same_device(where, Wg, groups.offsets, x, h, ws), ctypes.byref(Wg), ctypes.byref(Wu), x.data_ptr(),
+         ldx, groups._ref(), h.data_ptr(), ldh, ws.data_ptr(), ws.numel() * ws.element_size())
 
 
-def _down(where, Wd, h, groups, weights, y, ws, residual, stream):
+def _down(where, fn, Wd, h, groups, weights, y, ws, residual, stream):
     P, ldh = _rows(h, where, Wd.K)
     T, ldy = _rows(y, where, Wd.N)
     r, ldr, res = T, 0, None
@@ -939,14 +939,13 @@ def _down(where, Wd, h, groups, weights, y, ws, residual, stream):
     if T != groups.T or r != T or P != T * groups.k:
         raise SwiftSpecError(INVALID_ARG, where)
     _dense(weights, where, (T, groups.k), 4, real=True)
-    _run(where, getattr(_load(), "swiftspec_" + where), stream, _same_device(where, Wd, groups.offsets, h, weights, y, ws, residual),
-         ctypes.byref(Wd), h.data_ptr(), ldh, groups._ref(), weights.data_ptr(), y.data_ptr(), ldy, res, ldr, ws.data_ptr(),
-         ws.numel() * ws.element_size())
+    _run(where, fn, stream, _same_device(where, Wd, groups.offsets, h, weights, y, ws, residual), ctypes.byref(Wd), h.data_ptr(),
+         ldh, groups._ref(), weights.data_ptr(), y.data_ptr(), ldy, res, ldr, ws.data_ptr(), ws.numel() * ws.element_size())
 
 
 def moe_mx4_swiglu(Wg: MX4, Wu: MX4, x, groups: MoeGroups, h, ws, stream=None):
     """x [T][K] fp16 -> h [T k][N] fp16, a row for each place of the groups."""
-    _swiglu("moe_mx4_swiglu", Wg, Wu, x, groups, h, ws, stream)
+    _swiglu("moe_mx4_swiglu", _load().swiftspec_moe_mx4_swiglu, Wg, Wu, x, groups, h, ws, stream)
 
 
 def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
@@ -956,7 +955,7 @@ def moe_mx4_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
 def moe_mx4_down(Wd: MX4, h, groups: MoeGroups, weights, y, ws, residual=None, stream=None):
     """h [T k][K] fp16 (as moe_mx4_swiglu wrote it), weights [T][k] float32 ->
     y [T][N] fp16, the weighted sum of each token's experts plus residual."""
-    _down("moe_mx4_down", Wd, h, groups, weights, y, ws, residual, stream)
+    _down("moe_mx4_down", _load().swiftspec_moe_mx4_down, Wd, h, groups, weights, y, ws, residual, stream)
 
 
 def moe_fp8_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
@@ -965,7 +964,7 @@ def moe_fp8_swiglu_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> in
 
 def moe_fp8_swiglu(Wg: FP8, Wu: FP8, x, groups: MoeGroups, h, ws, stream=None):
     """moe_mx4_swiglu with 8-bit matrices."""
-    _swiglu("moe_fp8_swiglu", Wg, Wu, x, groups, h, ws, stream)
+    _swiglu("moe_fp8_swiglu", _load().swiftspec_moe_fp8_swiglu, Wg, Wu, x, groups, h, ws, stream)
 
 
 def moe_fp8_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
@@ -974,7 +973,7 @@ def moe_fp8_down_workspace_bytes(T: int, k: int, E: int, K: int, N: int) -> int:
 
 def moe_fp8_down(Wd: FP8, h, groups: MoeGroups, weights, y, ws, residual=None, stream=None):
     """moe_mx4_down with 8-bit matrices."""
-    _down("moe_fp8_down", Wd, h, groups, weights, y, ws, residual, stream)
+    _down("moe_fp8_down", _load().swiftspec_moe_fp8_down, Wd, h, groups, weights, y, ws, residual, stream)
 
 
 def make_dims(H, Hq, Hkv, D, F, S_max, eps=1e-5, rope_theta=500000.0) -> Dims:
