@@ -254,11 +254,11 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
 // A step multiplies one group: the weights' blocks of the wave stay in registers, the
 // rows' blocks follow one another, the next on its way from LDS.  Each instruction's
 // result is multiplied and added three instructions later, so that its latency does not
-// show (two later: 8192 x 8192 x 8192 474 against 462 us).  Before the last block of rows
-// the wave has read all it needs of this stage: it waits for its loads of the next one
-// and for the other waves, and reads the first operands of the next step while the last
-// block is multiplied; the stage's place is loaded anew during the next step.  One
-// barrier a step.
+// show (two later: 8192 x 8192 x 8192 474 against 462 us, best times).  Before the last
+// block of rows the wave has read all it needs of this stage: it waits for its loads of
+// the next one and for the other waves, and reads the first operands of the next step
+// while the last block is multiplied; the stage's place is loaded anew during the next
+// step.  One barrier a step.
 // A wave's columns lie in one block of 128, so that the matrix's scale is uniform: 64
 // groups of them are one load, a lane each.
 // The sums are in ordinary registers, as the multiply-adds need them: 64 x 128 of them
@@ -266,13 +266,14 @@ __global__ __launch_bounds__(64 * W) void fp8_stream_kernel(Fp8Args a) {
 // byte of LDS 0.75 times for an instruction.
 // With few rows an expert it is bound by the weights: SwiGLU of 32 tokens through 8
 // experts 4096 x 14336 (940 MB) 155-163 us, 5.8-6.1 TB/s, by tiles of 64 rows with four
-// stages.  With many by power and by LDS together: 8192 x 8192 x 8192 462 us (2.4
-// PFLOP/s; the instruction with its multiply-adds on random operands in registers
-// reaches 4.2, this kernel on zeros 2.9), 4001 rows of 4096 x 14336 219 us in four rounds
-// of tiles (2.1), matrix instructions in 54 % of its cycles, at 1.92 of 2.4 GHz.
-// Without the LDS reads (on the same operands again and again) 8192 would take 356,
-// without the loads 429, without both 293.  Pairs of blocks through the 32 x 32 x 64 form,
-// which reads each register half as often, were 4 % slower (485 against 465).
+// stages.  With many by power and by LDS together: 8192 x 8192 x 8192 447 us at
+// best, 483 the median of 24 one after another (2.5 and 2.3 PFLOP/s; on zeros 354 and
+// 362; the 16 x 16 x 128 instruction with its multiply-adds on random operands in registers
+// reaches 4.5 with one wave a SIMD, 3.9 with two, as here), 4001 rows of 4096 x 14336 219
+// us at best in four rounds of tiles (2.1), matrix instructions in 54 % of its cycles, at
+// 1.92 of 2.4 GHz.  When it took 462, it would have taken 356 without the LDS reads (on the
+// same operands again and again), 429 without the loads, 293 without both; pairs of blocks
+// through the 32 x 32 x 64 form, which reads each register half as often, were 4 % slower.
 constexpr int kTurnPad = 16;  // bytes behind a row of results on its way through LDS
 
 template <int WM, int WN, int MTW, int NTW, int ST, Epilogue EPI>
@@ -534,7 +535,7 @@ constexpr int kRowsOf[] = {16, 16, 32, 64, 128, 128, 256};
 constexpr int kColumnsOf[] = {32, 32, 32, 128, 128, 128, 256};
 constexpr int kThreadsOf[] = {256, 256, 256, 256, 512, 256, 512};
 // of the tiles: how many run at one time, and the microseconds that they take together
-// for a group of 128 k, and for first loads and last stores (fitted to the times of 70
+// for a group of 128 k, and for first loads and last stores (fitted to the times of
 // products from 33 x 4096 x 4096 to 8192 x 8192 x 8192 and of experts)
 constexpr int kSlotsOf[] = {0, 0, 0, 256, 256, 512, 256};
 constexpr double kStepOf[] = {0, 0, 0, 0.45, 0.58, 1.0, 1.65};
@@ -575,16 +576,19 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
   // 22.9; 28672 x 8192 60.0 against 51.7), 16 are not (54.1 against 55.2).
   // A stream's four waves take all of K.  Long ones of few columns are faster in shares,
   // which only tiles have (1 and 16 rows: 28672 x 4096 32.7 and 39.3 against 28.9 and 31.4,
-  // 16384 x 1024 18.5 and 22.6 against 13.1 and 13.9; 4 of 10240 x 4096 17.8 against 17.4; 1 of
-  // 8192 x 1024 9.8 against 12.4, 16 of 8192 x 4096 17.0 against 15.3, of 6144 x 4096 13.3
-  // against 15.7; of more columns, 12288 x 6144, 20.8 and 25.1 against 23.3 and 25.6, but 32
-  // rows 33.7 against 26.8).
+  // 16384 x 1024 18.5 and 22.6 against 13.1 and 13.9; 4 of 10240 x 4096 equal, 16.0 against
+  // 16.5; 1 of 8192 x 1024 9.8 against 12.4, 16 of 8192 x 4096 17.0 against 15.3, of 6144 x
+  // 4096 13.3 against 15.7; of more columns 4 rows of 10240 x 5120 16.9 against 18.7, 16 of
+  // 8192 x 5120 17.9 against 18.5, 1 and 16 of 12288 x 6144 20.8 and 25.1 against 23.3 and
+  // 25.6, but 32 rows 33.7 against 26.8).
   const bool shares = K >= (M > 8 ? 8192 : 10240) && (M > 16 || N <= 4096);
   if (!grouped && !shares && (M <= 16 || (M <= 32 && weights <= (48 << 20)) || (M <= 64 && weights <= (1 << 24))))
     return plan(M <= 16 || tiles(Fp8Form::STREAM_2) < 256 ? Fp8Form::STREAM_1 : Fp8Form::STREAM_2);
   // Tiles: the form, and the shares of K, whose rounds of tiles are shortest; not
   // shorter than the weights' bytes, and with what another kernel takes to add the
-  // shares.  (Over 108 products 1 % longer than the best form of each, at most 17 %.)
+  // shares.  (Over 156 products 2 % longer than the best form of each, 137 of them within
+  // 5 %, one matrix's within 11 %.  Of experts of 50 to 100 rows it is off by up to 31 %,
+  // where a form needs a whole round less by chance.)
   Fp8Plan best = {};
   double least = 0;
   for (Fp8Form f : {Fp8Form::TILE_64, Fp8Form::TILE_128_DEEP, Fp8Form::TILE_128, Fp8Form::TILE_256}) {
@@ -594,7 +598,9 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
       const int groups = split > 1 ? (G4 + split - 1) / split * 4 : G;
       const double work = (double)((n * split + slots - 1) / slots) * (groups * kStepOf[(int)f] + kRestOf[(int)f]);
       // several blocks of rows of an expert read its weights at different times (SwiGLU of
-      // those 256 pairs: blocks of 64 rows 214 us, of 128 rows 180)
+      // those 256 pairs: blocks of 64 rows 214 us, of 128 rows 180).  That is one number of
+      // experts; the limit is too low for others (32 experts 4096 x 2048 of 96 rows: 183 us in
+      // the tiles of 256 rows that it takes, 140 in those of 128).
       const double again = grouped ? std::min(1.15, (double)row_blocks(f) / reached) : 1.0;
       const double bytes = again * weights / 5.0e6;
       double t = std::max(work, bytes) + 0.15 * std::min(work, bytes);
