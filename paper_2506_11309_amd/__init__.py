@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libswiftspec.so")
@@ -699,15 +700,29 @@ def mx4_packed_bytes(K: int, N: int, E: int = 1) -> int:
     return _size("mx4_packed_bytes", K, N, E)
 
 
+def _let_go(W, dev, stream):
+    """Codes and scales that W holds are not needed behind the launch on `stream` that
+    made its copy; in a graph every replay reads them, and W keeps them."""
+    import torch
+    if W.unpacked and W.unpacked[0].is_cuda:
+        used = torch.cuda.current_stream(dev) if stream is None else torch.cuda.ExternalStream(stream.cuda_stream, device=dev)
+        with torch.cuda.stream(used):
+            if torch.cuda.is_current_stream_capturing():
+                return
+        for source in W.unpacked:
+            # held by W's tuple, `source` and the argument alone: its memory goes now, but
+            # not to another stream before the launch has read it
+            if sys.getrefcount(source) <= 3:
+                source.record_stream(used)
+    W.unpacked = ()
+
+
 def _prepack(where, W, size, device, stream):
     import torch
     t = torch.empty(size, dtype=torch.uint8, device=device)
     dev = _same_device(where, W, t)
     _run(where, getattr(_load(), "swiftspec_" + where), stream, dev, ctypes.byref(W), t.data_ptr(), t.numel())
-    for source in W.unpacked:
-        if source.is_cuda:  # its memory is not given away before the launch has read it
-            source.record_stream(torch.cuda.current_stream(dev) if stream is None else torch.cuda.ExternalStream(stream.cuda_stream, device=dev))
-    W.unpacked = ()
+    _let_go(W, dev, stream)
     W.packed = t.data_ptr()
     return t
 

@@ -1,5 +1,6 @@
 """A described 4-bit or 8-bit matrix keeps its codes and scales until its kernel-native
 copy is made, and no longer."""
+import contextlib
 import weakref
 
 import numpy as np
@@ -41,6 +42,32 @@ def test_tensors_are_held_until_packed(ss, monkeypatch, kind):  # noqa: F811
     assert all(r() is None for r in refs)
 
 
+def test_the_allocator_hears_of_tensors_that_go(ss, monkeypatch):  # noqa: F811
+    """Only of those that nothing else holds: another holder's own streams are its own
+    business, and a stream noted for a long-lived tensor is waited for when that is freed."""
+    noted = []
+
+    class Source:
+        is_cuda = True
+
+        def record_stream(self, stream):
+            noted.append(stream)
+
+    class Matrix:
+        unpacked = ()
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: "current")
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    W, kept, capturing = Matrix(), Source(), False
+    W.unpacked = kept, Source()
+    ss._let_go(W, 0, None)
+    assert W.unpacked == () and noted == ["current"]
+    W.unpacked, capturing = (Source(), Source()), True
+    ss._let_go(W, 0, None)
+    assert len(W.unpacked) == 2 and noted == ["current"]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", ["mx4", "fp8"])
 @pytest.mark.parametrize("other_stream", [False, True])
@@ -60,3 +87,29 @@ def test_packing_a_matrix_of_temporaries(ss, kind, other_stream):  # noqa: F811
     over += [torch.zeros_like(v) for v in t for _ in range(3)]
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["mx4", "fp8"])
+def test_packing_in_a_graph(ss, kind):  # noqa: F811
+    """Each replay reads the codes again: the matrix keeps them."""
+    t, make, prepack = described(ss, kind, "cuda")
+    want = prepack(make(*t))
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        room = torch.empty_like(want)  # what the packing takes in the graph
+        W = make(*(v.clone() for v in t))
+        del room
+        st.synchronize()
+        graph = ss.Graph()
+        graph.begin()
+        got = prepack(W)
+        graph.end()
+        over = [torch.zeros_like(v) for v in t for _ in range(3)]  # noqa: F841
+        for _ in range(3):
+            got.zero_()
+            graph.launch()
+            st.synchronize()
+            assert torch.equal(got, want)
+    assert len(W.unpacked) == 2
