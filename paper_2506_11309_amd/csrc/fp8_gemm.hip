@@ -587,8 +587,10 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
   // Tiles: the form, and the shares of K, whose rounds of tiles are shortest; not
   // shorter than the weights' bytes, and with what another kernel takes to add the
   // shares.  (Over 156 products 2 % longer than the best form of each, 137 of them within
-  // 5 %, one matrix's within 11 %.  Of experts of 50 to 100 rows it is off by up to 31 %,
-  // where a form needs a whole round less by chance.)
+  // 5 %, one matrix's within 11 %.  Of experts of 50 to 100 rows it is off by up to 31 %:
+  // 8 of 50 rows are one round of tiles of 128 rows, not the two that the chance block
+  // makes, SwiGLU 4096 x 2048 33 us against 43 in tiles of 64; 32 of 96 rows take 183 us in
+  // tiles of 256 rows, not 132, and 140 in those of 128.)
   Fp8Plan best = {};
   double least = 0;
   for (Fp8Form f : {Fp8Form::TILE_64, Fp8Form::TILE_128_DEEP, Fp8Form::TILE_128, Fp8Form::TILE_256}) {
@@ -598,9 +600,7 @@ Fp8Plan plan_fp8_gemm(int M, int E, int K, int N, bool swiglu, bool grouped, boo
       const int groups = split > 1 ? (G4 + split - 1) / split * 4 : G;
       const double work = (double)((n * split + slots - 1) / slots) * (groups * kStepOf[(int)f] + kRestOf[(int)f]);
       // several blocks of rows of an expert read its weights at different times (SwiGLU of
-      // those 256 pairs: blocks of 64 rows 214 us, of 128 rows 180).  That is one number of
-      // experts; the limit is too low for others (32 experts 4096 x 2048 of 96 rows: 183 us in
-      // the tiles of 256 rows that it takes, 140 in those of 128).
+      // those 256 pairs: blocks of 64 rows 214 us, of 128 rows 180)
       const double again = grouped ? std::min(1.15, (double)row_blocks(f) / reached) : 1.0;
       const double bytes = again * weights / 5.0e6;
       double t = std::max(work, bytes) + 0.15 * std::min(work, bytes);

@@ -125,8 +125,9 @@ __device__ __forceinline__ RowBlock find_block(const ProductArgs& a, int rb, int
 // own L2.  Of one matrix the last tiles, fewer than 256, go to the chiplets in 8
 // stretches as well (128 rows of 8192 x 8192 in 8 bits 38.5 -> 32.0 us, 384 rows 55 ->
 // 50; in 4 bits 25.2 -> 21.8 and 34.4 -> 32.0, 512 rows of 8192 x 28672 82 -> 73, 3000 of
-// 4096 x 4096 and 8192 of 8192 x 8192 the same); of experts one by one, so that the empty row blocks at the end of their list are
-// no chiplet's alone (down for 100 tokens of 4 experts 4096 x 8192 43 against 58 us).
+// 4096 x 4096 and 8192 of 8192 x 8192 the same); of experts one by one, so that the empty
+// row blocks at the end of their list are no chiplet's alone (down for 100 tokens of 4
+// experts 4096 x 8192 43 against 58 us).
 __device__ __forceinline__ void place_of(const ProductArgs& a, int& rb, int& cb) {
   const int all = gridDim.x, x = blockIdx.x & 7, s = blockIdx.x >> 3;
   const int whole = all & ~255, rest = all - whole;
